@@ -324,6 +324,73 @@ enum {
 };
 int hcnn_measure_ceiling(hcnn_ctx* ctx, int which, double* value_out);
 
+/* ---- training of the plain network ------------------------------------------------------
+ * The weights that hcnn_ct_scalar_mac takes come from a network trained in the clear.  These calls are a training step's
+ * parts: the layers (a convolution is a product over its placements' gathered inputs) with the square activation and others, the loss with
+ * its gradient, the clipping of the gradients.  They need no ring and no primes: a handle of its own holds the stream and the
+ * work memory (grown to the largest call's need, with a wait for the stream; a call that needs no more allocates nothing, uses no memset
+ * and can be recorded into a graph).
+ * Numbers are of one type per call, HCNN_F32, HCNN_F16 (binary16) or HCNN_BF16; sums and statistics are held in 32 bits or more and
+ * rounded once, to nearest, ties to even.  Matrices are row by row, numbers of a row side by side, *_stride numbers from a row to the next:
+ * any stride for inputs (0: one row for all), at least the row's length for outputs.  Pointers need the alignment of one
+ * number only.  Sizes below 2^31 each; a size of zero is an empty matrix, and an empty sum is 0.  Outputs
+ * must not overlap inputs unless stated. */
+typedef struct hcnn_plain hcnn_plain;
+
+enum { HCNN_F32 = 0, HCNN_F16 = 1, HCNN_BF16 = 2 };
+enum {
+  HCNN_ACT_NONE = 0,
+  HCNN_ACT_SQUARE = 1,   /* z^2: the activation of the encrypted network (Sec. 3.2) */
+  HCNN_ACT_RELU = 2,     /* max(z, 0); slope 0 at 0                                  */
+  HCNN_ACT_GELU = 3,     /* z * P(X <= z), X normal (with erf)                       */
+  HCNN_ACT_SILU = 4      /* z / (1 + e^-z)                                           */
+};
+
+int hcnn_plain_create(hcnn_plain** out, void* hip_stream);
+int hcnn_plain_destroy(hcnn_plain* h);
+int hcnn_plain_set_stream(hcnn_plain* h, void* hip_stream);
+/* HCNN_STAT_SCRATCH_BYTES or HCNN_STAT_BAD_INPUT (synchronises): targets of the two cross-entropy calls that were neither a
+ * class nor the ignored value; their rows were taken as ignored. */
+int hcnn_plain_get_stat(hcnn_plain* h, int which, uint64_t* out);
+
+/* z = x w^T + bias;  y = act(z) + residual.
+ *   x_dev [rows][n_in], w_dev [n_out][n_in], bias_dev [n_out] or NULL, residual_dev [rows][n_out] or NULL (y_dev may be the same
+ *   buffer with the same stride); y_dev, z_dev [rows][n_out], z_dev or NULL (what hcnn_linear_grad needs unless the activation is NONE). */
+int hcnn_linear(hcnn_plain* h, int dtype, int activation, size_t rows, size_t n_in, size_t n_out,
+                const void* x_dev, size_t x_stride, const void* w_dev, size_t w_stride, const void* bias_dev,
+                const void* residual_dev, size_t residual_stride, void* y_dev, size_t y_stride, void* z_dev, size_t z_stride);
+
+/* Gradients of hcnn_linear for dy_dev [rows][n_out]: with dz = dy * act'(z),
+ *   dx = dz w,  dw = dz^T x,  db = sum over rows of dz   (the residual's is dy); NULL for those not wanted.
+ * dz is rounded to the call's type before the two products take it (and not for db).  z_dev may be NULL when the activation is NONE,
+ * w_dev without dx_dev, x_dev without dw_dev. */
+int hcnn_linear_grad(hcnn_plain* h, int dtype, int activation, size_t rows, size_t n_in, size_t n_out,
+                     const void* dy_dev, size_t dy_stride, const void* x_dev, size_t x_stride, const void* w_dev, size_t w_stride,
+                     const void* z_dev, size_t z_stride, void* dx_dev, size_t dx_stride, void* dw_dev, size_t dw_stride, void* db_dev);
+
+/* Softmax cross entropy of the scores s = x w^T of n_classes classes; the scores themselves are never stored.
+ *   x_dev [rows][n_in], w_dev [n_classes][n_in], targets_dev int32 or int64 (target_bytes 4 or 8) [rows].
+ * A row whose target is `ignore` takes no part, and nothing of it is read: it may hold anything.
+ *   row_lse[m] = log sum_v e^s[m][v], row_loss[m] = row_lse[m] - s[m][target] (both 0 where ignored; NULL if not wanted);
+ *   loss[0] = mean of row_loss over the other rows, 0 where there are none.  All three are 32-bit floats. */
+int hcnn_cross_entropy(hcnn_plain* h, int dtype, size_t rows, size_t n_in, size_t n_classes, const void* x_dev, size_t x_stride,
+                       const void* w_dev, size_t w_stride, const void* targets_dev, int target_bytes, int64_t ignore,
+                       float* row_loss_dev, float* row_lse_dev, float* loss_dev);
+
+/* The same with the gradients of scale * loss: dx_dev [rows][n_in] (0 in ignored rows), dw_dev [n_classes][n_in]; either may be NULL.
+ * The scores' gradients are formed in pieces of the classes, at most 512 MiB of them at a time (one piece has at least 256 classes), and
+ * rounded to the call's type for the products that take them. */
+int hcnn_cross_entropy_grad(hcnn_plain* h, int dtype, size_t rows, size_t n_in, size_t n_classes, const void* x_dev, size_t x_stride,
+                            const void* w_dev, size_t w_stride, const void* targets_dev, int target_bytes, int64_t ignore, float scale,
+                            float* row_loss_dev, float* loss_dev, void* dx_dev, size_t dx_stride, void* dw_dev, size_t dw_stride);
+
+/* norm[0] = sqrt of the sum of squares of all numbers of all tensors (summed in 64 bits), and every tensor times
+ * min(1, max_norm / (norm + eps)).  The arrays are host arrays of n_tensors device pointers, counts and types (one type each);
+ * outs_host NULL: in place, else where each result goes (a tensor's own place allowed).  A norm that is not finite: the factor is 0
+ * (infinity) or not a number, as the formula gives it. */
+int hcnn_clip_grad_norm(hcnn_plain* h, size_t n_tensors, const void* const* grads_host, const size_t* counts_host,
+                        const int* dtypes_host, void* const* outs_host, double max_norm, double eps, float* norm_dev);
+
 const char* hcnn_strerror(int code);
 
 #ifdef __cplusplus

@@ -13,6 +13,8 @@ PROF_CLASSES = ["ntt_fwd", "ntt_inv", "base_ext", "tensor", "scale", "digit", "r
 CEILINGS = ["copy_GBps", "read_GBps", "write_GBps", "mul_lo_u32_Tops", "mul_hi_u32_Tops", "mad_u64_u32_Tops",
             "mad_i64_i32_Tops", "add_u32_Tops"]
 MAX_LIMBS, MAX_FILTERS = 32, 16
+F32, F16, BF16 = 0, 1, 2
+ACTIVATIONS = {"none": 0, "square": 1, "relu": 2, "gelu": 3, "silu": 4}
 
 # name -> argtypes; every entry point returns int except hcnn_strerror
 SIGNATURES = {
@@ -42,6 +44,16 @@ SIGNATURES = {
     "hcnn_set_option": [ptr, C.c_int, C.c_uint64],
     "hcnn_profile_read": [ptr, C.c_int, u64p, u64p, C.POINTER(C.c_double)],
     "hcnn_measure_ceiling": [ptr, C.c_int, C.POINTER(C.c_double)],
+    "hcnn_plain_create": [C.POINTER(ptr), ptr],
+    "hcnn_plain_destroy": [ptr],
+    "hcnn_plain_set_stream": [ptr, ptr],
+    "hcnn_plain_get_stat": [ptr, C.c_int, u64p],
+    "hcnn_linear": [ptr, C.c_int, C.c_int] + [C.c_size_t] * 3 + [ptr, C.c_size_t, ptr, C.c_size_t, ptr, ptr, C.c_size_t, ptr, C.c_size_t, ptr, C.c_size_t],
+    "hcnn_linear_grad": [ptr, C.c_int, C.c_int] + [C.c_size_t] * 3 + [ptr, C.c_size_t] * 6 + [ptr],
+    "hcnn_cross_entropy": [ptr, C.c_int] + [C.c_size_t] * 3 + [ptr, C.c_size_t] * 2 + [ptr, C.c_int, C.c_int64, ptr, ptr, ptr],
+    "hcnn_cross_entropy_grad": [ptr, C.c_int] + [C.c_size_t] * 3 + [ptr, C.c_size_t] * 2 + [ptr, C.c_int, C.c_int64, C.c_float, ptr, ptr]
+                               + [ptr, C.c_size_t] * 2,
+    "hcnn_clip_grad_norm": [ptr, C.c_size_t, ptr, ptr, ptr, ptr, C.c_double, C.c_double, ptr],
     "hcnn_strerror": [C.c_int],
 }
 
@@ -134,3 +146,32 @@ class RawContext:
 
     def set_option(self, which, value):
         check(self.lib, self.lib.hcnn_set_option(self.handle, which, C.c_uint64(value)))
+
+
+class RawPlain:
+    """Thin owner of an hcnn_plain*.  Buffers are passed as integer addresses."""
+
+    def __init__(self, lib, stream=0):
+        self.lib = lib
+        h = ptr()
+        check(lib, lib.hcnn_plain_create(C.byref(h), ptr(stream)))
+        self.handle = h
+
+    def close(self):
+        if self.handle:
+            self.lib.hcnn_plain_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def call(self, name, *args):
+        check(self.lib, getattr(self.lib, name)(self.handle, *args))
+
+    def stat(self, which):
+        out = C.c_uint64(0)
+        check(self.lib, self.lib.hcnn_plain_get_stat(self.handle, which, C.byref(out)))
+        return int(out.value)

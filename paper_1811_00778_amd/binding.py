@@ -11,6 +11,7 @@ import torch
 
 from . import _capi
 from ._ops import OpsMixin
+from ._plain_ops import PlainOpsMixin
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "lib", "libhcnn.so")
 _lib = None
@@ -106,3 +107,69 @@ class Context(OpsMixin):
         torch.cuda.current_stream(self.device).synchronize()
         a = tensor.cpu().numpy()
         return a.view(np.uint64) if a.dtype == np.int64 else a.view(np.uint32)
+
+
+_PLAIN_DT = {torch.float32: _capi.F32, torch.float16: _capi.F16, torch.bfloat16: _capi.BF16}
+
+
+class PlainContext(PlainOpsMixin):
+    """An hcnn_plain bound to a torch device and stream: the training operators of the plain network (no ring, no keys).
+
+    Tensors are torch.float32, torch.float16 or torch.bfloat16 on the device, matrices with any row stride.  Streams follow
+    Context's rule: torch's current stream must be the one of the last use_stream (at first, of creation)."""
+
+    def __init__(self, device="cuda:0"):
+        if not torch.cuda.is_available():
+            raise RuntimeError("no GPU visible: the HIP path cannot run (there is no CPU fallback)")
+        self.device = torch.device(device)
+        torch.cuda.set_device(self.device)
+        self._stream = torch.cuda.current_stream(self.device).cuda_stream
+        self.raw = _capi.RawPlain(lib(), self._stream)
+
+    def use_stream(self, stream=None):
+        """Launch on `stream` (default: torch's current one) from now on; see Context.use_stream."""
+        stream = torch.cuda.current_stream(self.device) if stream is None else stream
+        self.raw.call("hcnn_plain_set_stream", ctypes.c_void_p(stream.cuda_stream))
+        self._stream = stream.cuda_stream
+
+    _pre_call = Context._pre_call
+
+    def _matrix(self, x, what):
+        if not isinstance(x, torch.Tensor) or x.dtype not in _PLAIN_DT or x.device != self.device or x.dim() != 2:
+            raise TypeError("%s must be a 2-D float32, float16 or bfloat16 tensor on %s" % (what, self.device))
+        rows, cols = x.shape
+        stride, step = x.stride()
+        if step != 1 and cols > 1 and rows:
+            raise TypeError("the numbers of a row of %s must lie side by side" % what)
+        return x.data_ptr(), rows, cols, stride, _PLAIN_DT[x.dtype]
+
+    def _flat(self, x, what):
+        if not isinstance(x, torch.Tensor) or x.dtype not in _PLAIN_DT or x.device != self.device or not x.is_contiguous():
+            raise TypeError("%s must be contiguous float32, float16 or bfloat16 tensors on %s" % (what, self.device))
+        return x.data_ptr(), x.numel(), _PLAIN_DT[x.dtype]
+
+    def _vector(self, x, what):
+        got = self._flat(x, what)
+        if x.dim() != 1:
+            raise TypeError("%s must be 1-D" % what)
+        return got
+
+    def _targets(self, x, what):
+        if not isinstance(x, torch.Tensor) or x.dtype not in (torch.int32, torch.int64) or x.device != self.device or x.dim() != 1 \
+                or not x.is_contiguous():
+            raise TypeError("%s must be a contiguous 1-D int32 or int64 tensor on %s" % (what, self.device))
+        return x.data_ptr(), x.numel(), x.element_size()
+
+    def _new(self, shape, like):
+        return torch.empty(shape, dtype=torch.float32 if like is None else like.dtype, device=self.device)
+
+    @staticmethod
+    def _address(x):
+        return None if x is None else x.data_ptr()
+
+    @staticmethod
+    def _span(x):
+        if x.numel() == 0:
+            return 0, 0
+        last = sum((n - 1) * s for n, s in zip(x.shape, x.stride()))
+        return x.data_ptr(), x.data_ptr() + (last + 1) * x.element_size()

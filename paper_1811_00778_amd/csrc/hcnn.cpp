@@ -1981,3 +1981,7 @@ void hcnn_emu_device(uint32_t units, size_t largest_allocation) { emu_units = un
 #endif
 
 }  // extern "C"
+
+#ifdef HCNN_HOSTEMU
+#include "plain.cpp"        // the checker is built from this file alone
+#endif

@@ -1,0 +1,1002 @@
+// Kernels of the plain (unencrypted) network's training: matrix products with what follows them, softmax cross entropy, the
+// norm of many gradients.  Sums, statistics and norms are held in 32 bits or more; 16-bit numbers are widened on the way in
+// and rounded once on the way out (to nearest, ties to even).
+#pragma once
+#include <cmath>
+#include <limits>
+
+#include "platform.h"
+
+namespace hcnn {
+
+// ---------------------------------------------------------------- numbers
+struct Half { uint16_t bits; };        // IEEE binary16
+struct Bfloat { uint16_t bits; };      // the upper half of a binary32
+
+HCNN_HD float bits_float(uint32_t b) { float f; __builtin_memcpy(&f, &b, 4); return f; }
+HCNN_HD uint32_t float_bits(float f) { uint32_t b; __builtin_memcpy(&b, &f, 4); return b; }
+
+template <class T> struct Num;
+template <> struct Num<float> {
+  HCNN_HD static float widen(float x) { return x; }
+  HCNN_HD static float narrow(float x) { return x; }
+};
+template <> struct Num<Bfloat> {
+  HCNN_HD static float widen(Bfloat x) { return bits_float((uint32_t)x.bits << 16); }
+  HCNN_HD static Bfloat narrow(float x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_bit_cast(Bfloat, (__bf16)x);
+#else
+    const uint32_t b = float_bits(x);
+    if ((b & 0x7fffffffu) > 0x7f800000u) return Bfloat{(uint16_t)(b >> 16 | 0x40)};       // a NaN stays one
+    return Bfloat{(uint16_t)((b + 0x7fffu + (b >> 16 & 1)) >> 16)};
+#endif
+  }
+};
+template <> struct Num<Half> {
+  HCNN_HD static float widen(Half x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return (float)__builtin_bit_cast(_Float16, x);
+#else
+    const uint32_t s = (uint32_t)(x.bits >> 15) << 31, e = x.bits >> 10 & 31, m = x.bits & 1023;
+    if (e == 31) return bits_float(s | 0x7f800000u | m << 13);
+    if (e) return bits_float(s | (e + 112) << 23 | m << 13);
+    const float v = (float)m * 5.9604644775390625e-8f;                                    // m * 2^-24
+    return s ? -v : v;
+#endif
+  }
+  HCNN_HD static Half narrow(float x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_bit_cast(Half, (_Float16)x);
+#else
+    const uint32_t b = float_bits(x), s = b >> 16 & 0x8000, a = b & 0x7fffffffu;
+    if (a > 0x7f800000u) return Half{(uint16_t)(s | 0x7e00)};
+    if (a >= 0x477ff000u) return Half{(uint16_t)(s | 0x7c00)};                            // rounds to 2^16 or more
+    if (a < 0x38800000u) {                                                                // below 2^-14: steps of 2^-24
+      const float steps = bits_float(a) * 16777216.0f;                                    // exact
+      return Half{(uint16_t)(s | (uint32_t)(int)std::nearbyint(steps))};
+    }
+    return Half{(uint16_t)(s | ((a + 0xfffu + (a >> 13 & 1)) - 0x38000000u) >> 13)};
+#endif
+  }
+};
+
+// 2^x and e^x to about one unit of the last place of the exponent function unit (e^x: and |x| 2^-24 for the product)
+HCNN_HD float exp2_of(float x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return __builtin_amdgcn_exp2f(x);
+#else
+  return std::exp2(x);
+#endif
+}
+HCNN_HD float exp_of(float x) { return exp2_of(x * 1.44269504088896340736f); }
+
+// ---------------------------------------------------------------- accesses of any alignment
+// The device's global accesses take any address; types of alignment 1 tell the compiler so.
+#if defined(__HIP_DEVICE_COMPILE__)
+typedef uint32_t hcnn_any4 __attribute__((ext_vector_type(4), aligned(1)));
+typedef uint32_t hcnn_any2 __attribute__((ext_vector_type(2), aligned(1)));
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Wold-style-cast"
+__device__ __forceinline__ U4 ld16(const char* p) {
+  const hcnn_any4 v = *(const hcnn_any4 __attribute__((address_space(1)))*)p;
+  U4 r; r.x = v.x; r.y = v.y; r.z = v.z; r.w = v.w;
+  return r;
+}
+__device__ __forceinline__ void st16(char* p, U4 v) { *(hcnn_any4 __attribute__((address_space(1)))*)p = hcnn_any4{v.x, v.y, v.z, v.w}; }
+__device__ __forceinline__ uint64_t ld8(const char* p) { return __builtin_bit_cast(uint64_t, (hcnn_any2)*(const hcnn_any2 __attribute__((address_space(1)))*)p); }
+__device__ __forceinline__ void st8(char* p, uint64_t v) { *(hcnn_any2 __attribute__((address_space(1)))*)p = __builtin_bit_cast(hcnn_any2, v); }
+#pragma clang diagnostic pop
+#else
+HCNN_HD U4 ld16(const char* p) { U4 v; __builtin_memcpy(&v, p, 16); return v; }
+HCNN_HD void st16(char* p, U4 v) { __builtin_memcpy(p, &v, 16); }
+HCNN_HD uint64_t ld8(const char* p) { uint64_t v; __builtin_memcpy(&v, p, 8); return v; }
+HCNN_HD void st8(char* p, uint64_t v) { __builtin_memcpy(p, &v, 8); }
+#endif
+
+// Four numbers in a row, widened
+template <class T>
+HCNN_HD void load4(const T* p, float (&v)[4]) {
+  T t[4];
+  if constexpr (sizeof(T) == 4) {
+    const U4 w = ld16(reinterpret_cast<const char*>(p));
+    __builtin_memcpy(t, &w, 16);
+  } else {
+    const uint64_t w = ld8(reinterpret_cast<const char*>(p));
+    __builtin_memcpy(t, &w, 8);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = Num<T>::widen(t[i]);
+}
+template <class T>
+HCNN_HD void store4(T* p, const float (&v)[4]) {
+  T t[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t[i] = Num<T>::narrow(v[i]);
+  if constexpr (sizeof(T) == 4) {
+    U4 w;
+    __builtin_memcpy(&w, t, 16);
+    st16(reinterpret_cast<char*>(p), w);
+  } else {
+    uint64_t w;
+    __builtin_memcpy(&w, t, 8);
+    st8(reinterpret_cast<char*>(p), w);
+  }
+}
+// ... of which only the first `left` exist
+template <class T>
+HCNN_HD void load4(const T* p, uint32_t left, float (&v)[4]) {
+  if (left >= 4) return load4(p, v);
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) v[i] = i < left ? Num<T>::widen(p[i]) : 0.0f;
+}
+template <class T>
+HCNN_HD void store4(T* p, uint32_t left, const float (&v)[4]) {
+  if (left >= 4) return store4(p, v);
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i)
+    if (i < left) p[i] = Num<T>::narrow(v[i]);
+}
+
+// ---------------------------------------------------------------- activations
+enum { kActNone = 0, kActSquare = 1, kActRelu = 2, kActGelu = 3, kActSilu = 4, kActCount = 5 };
+HCNN_HD float act_of(float z, int act) {
+  switch (act) {
+    case kActSquare: return z * z;
+    case kActRelu: return z > 0.0f || z != z ? z : 0.0f;
+    case kActGelu: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752440f));
+    case kActSilu: return z / (1.0f + exp_of(-z));
+  }
+  return z;
+}
+HCNN_HD float slope_of(float z, int act) {
+  switch (act) {
+    case kActSquare: return 2.0f * z;
+    case kActRelu: return z > 0.0f || z != z ? 1.0f : 0.0f;
+    case kActGelu: return 0.5f * (1.0f + erff(z * 0.70710678118654752440f)) + z * exp_of(-0.5f * z * z) * 0.39894228040143267794f;
+    case kActSilu: {
+      const float s = 1.0f / (1.0f + exp_of(-z));
+      return s * (1.0f + z * (1.0f - s));
+    }
+  }
+  return 1.0f;
+}
+
+// ---------------------------------------------------------------- matrix products
+// out[m][n] = sum_k a(m, k) b(n, k).  An operand is stored with its contraction index k contiguous (kAlongK: a[m][k]) or with
+// its output index contiguous (kAcrossK: a[k][m]).  A workgroup computes a tile of BM x BN outputs in WM x WN waves; a stage is 128
+// bytes of k (64 numbers of 16 bits, 32 of 32).  A stage's tiles go from memory to registers one stage ahead and from there to one
+// of two LDS buffers, so that a stage costs one barrier.
+//   kAlongK  in LDS [row][8 pieces of 16 bytes], piece p of a row at p ^ (row mod 8): the 16 rows x 4 pieces that a wave reads at once
+//            and the rows that it writes spread evenly over the banks
+//   kAcrossK in LDS [k][rows] as it lies in memory, in granules of 16 rows; 16-bit numbers are read with the transposing LDS read
+//            (16 lanes: 4 k x 16 rows in, 4 k of one row out), 32-bit ones word by word; granules are swapped by the bits of k in which the lanes
+//            of one read differ
+// Products: v_mfma_f32_16x16x32 (16 bits) and v_mfma_f32_16x16x4_f32.  A lane's 16 bytes of an operand are k 8 g .. 8 g + 7 (16 bits) or
+// 4 g .. 4 g + 3 (32 bits) of a row, g = lane / 16; both operands use the same order, so that the sum is the same whatever the instruction
+// calls these k.  b is the first operand: a lane then holds four consecutive n of a row m = lane mod 16.
+enum { kAlongK = 0, kAcrossK = 1 };
+enum { kGatherA = 1, kGatherB = 2, kScatterOut = 4 };      // which index goes through GemmArgs::rows: a's m, b's k, the output's m
+enum { kCountNone = 0, kCountM = 1, kCountK = 2 };         // what GemmArgs::count limits
+
+struct GemmArgs {
+  const void *a, *b;
+  size_t lda, ldb;             // numbers from one stored row to the next
+  size_t a_extent, b_extent;   // numbers from the first to the last one that exists, inclusive
+  uint32_t M, N, K;
+  const uint32_t* rows;        // indices for `gather`
+  const uint32_t* count;       // device count of the rows that take part, see count_of
+  uint32_t gather, count_of;
+  uint32_t splits;             // parts of k, each summed by workgroups of its own
+  // what becomes of the sums
+  float* sums;                 // [splits][M][ld_sums] where kEpiSums
+  size_t ld_sums;              // a multiple of 4
+  const float* addend;         // [M][ld_sums], added to the sums of the first part (may be null; may be `sums`)
+  const float* alpha;          // device factor of the sums (may be null)
+  int act;
+  const void* bias;            // [N]
+  const void* residual;
+  void *out, *z;
+  size_t ld_residual, ld_out, ld_z;
+  // softmax
+  float* stats;                // [tiles of n][2][ld_stats]: largest score, sum of exponentials relative to it
+  size_t ld_stats;
+  const uint32_t* target;      // [rows that take part]
+  float* target_score;
+  const float* lse;
+  float delta_scale;
+  uint32_t n_offset;           // class of column 0
+};
+
+// What the linear layer makes of four sums in a row of its output.
+template <class T>
+HCNN_HD void finish4(const GemmArgs& a, uint32_t m, uint32_t n, float (&v)[4]) {
+  if (n >= a.N) return;
+  const uint32_t left = a.N - n;
+  if (a.alpha) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] *= *a.alpha;
+  }
+  if (a.bias) {
+    float b[4];
+    load4(static_cast<const T*>(a.bias) + n, left, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += b[i];
+  }
+  const size_t row = a.gather & kScatterOut ? a.rows[m] : m;
+  if (a.z) store4(static_cast<T*>(a.z) + row * a.ld_z + n, left, v);
+  if (a.act != kActNone) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], a.act);
+  }
+  if (a.residual) {
+    float r[4];
+    load4(static_cast<const T*>(a.residual) + row * a.ld_residual + n, left, r);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += r[i];
+  }
+  store4(static_cast<T*>(a.out) + row * a.ld_out + n, left, v);
+}
+
+enum { kEpiOut = 0, kEpiSums = 1, kEpiStats = 2, kEpiDelta = 3 };
+
+template <class T> struct GemmNum {
+  static constexpr uint32_t kPer16 = 16 / sizeof(T);       // numbers in 16 bytes
+  static constexpr uint32_t kStage = 128 / sizeof(T);      // k of a stage
+};
+
+// One operand's way through a workgroup: BX rows of the output index, THREADS threads.
+template <class T, int LAYOUT, int BX, int THREADS>
+struct GemmOperand {
+  static constexpr uint32_t kPer16 = GemmNum<T>::kPer16, kStage = GemmNum<T>::kStage;
+  static constexpr int kPieces = BX * 8;                                       // of 16 bytes in a stage
+  static constexpr int kEach = (kPieces + THREADS - 1) / THREADS;
+  static constexpr uint32_t kRowPieces = LAYOUT == kAlongK ? 8 : BX / kPer16;  // in a stored row of the stage
+  static constexpr uint32_t kGranules = BX / 16;
+  static constexpr uint32_t kLdsBytes = BX * 128;
+
+  HCNN_HD static bool mine(int tid, int i) { return kPieces % THREADS == 0 || tid + i * THREADS < kPieces; }
+
+  // 16 bytes of the numbers at `off`; those that do not exist are left 0
+  HCNN_HD static U4 piece(const T* p, size_t off, size_t extent) {
+    if (off + kPer16 <= extent) return ld16(reinterpret_cast<const char*>(p + off));
+    T t[kPer16] = {};
+#pragma unroll
+    for (uint32_t e = 0; e < kPer16; ++e)
+      if (off + e < extent) t[e] = p[off + e];
+    U4 v;
+    __builtin_memcpy(&v, t, 16);
+    return v;
+  }
+  // the first `left` numbers of a piece
+  HCNN_HD static U4 first(U4 v, uint32_t left) {
+    uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) {
+      if constexpr (sizeof(T) == 4) w[i] = i < left ? w[i] : 0u;
+      else w[i] = 2 * i + 1 < left ? w[i] : 2 * i < left ? w[i] & 0xffffu : 0u;
+    }
+    U4 r; r.x = w[0]; r.y = w[1]; r.z = w[2]; r.w = w[3];
+    return r;
+  }
+  // Pieces of the stage that begins at k0, of the rows from x0 on.  Rows beyond X and what lies beyond them may hold anything (their sums
+  // are dropped), k beyond K are 0 in both operands.
+  HCNN_HD static void load(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, const uint32_t* rows, uint32_t x0, uint32_t k0,
+                           int tid, U4 (&r)[kEach]) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (!mine(tid, i)) continue;
+      const uint32_t c = (uint32_t)(tid + i * THREADS), line = c / kRowPieces, at = c % kRowPieces * kPer16;
+      U4 v{};
+      if constexpr (LAYOUT == kAlongK) {
+        uint32_t x = x0 + line;
+        if (x >= X) x = X - 1;
+        const uint32_t k = k0 + at;
+        if (k < K) {
+          const size_t row = rows ? rows[x] : x;
+          v = piece(p, row * ld + k, extent);
+          if (K - k < kPer16) v = first(v, K - k);
+        }
+      } else {
+        const uint32_t k = k0 + line, x = x0 + at;
+        if (k < K && x < X) {
+          const size_t row = rows ? rows[k] : k;
+          v = piece(p, row * ld + x, extent);
+        }
+      }
+      r[i] = v;
+    }
+  }
+  HCNN_HD static uint32_t place(uint32_t line, uint32_t pc) {                  // byte of piece pc of stored row `line`
+    if constexpr (LAYOUT == kAlongK) return line * 128 + ((pc ^ (line & 7)) << 4);
+    else if constexpr (sizeof(T) == 2) return line * (BX * 2) + ((pc / 2 ^ swap(line)) << 5) + (pc % 2 << 4);
+    else return line * (BX * 4) + ((pc / 4 ^ swap(line)) << 6) + (pc % 4 << 4);
+  }
+  // kAcrossK: granule g of stored row k lies at g ^ swap(k)
+  HCNN_HD static uint32_t swap(uint32_t k) {
+    return (sizeof(T) == 2 ? (k & 3) + (k >> 3 & 1) * 4 : k >> 2 & 3) & (kGranules & (kGranules - 1) ? 0 : kGranules - 1);
+  }
+  HCNN_HD static void store(char* lds, int tid, const U4 (&r)[kEach]) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (!mine(tid, i)) continue;
+      const uint32_t c = (uint32_t)(tid + i * THREADS);
+      *reinterpret_cast<U4*>(lds + place(c / kRowPieces, c % kRowPieces)) = r[i];
+    }
+  }
+  // 16 bytes of row `base + lane % 16`, step s (of two 64-byte steps) of the stage; base a multiple of 16
+#if defined(__HIP_DEVICE_COMPILE__)
+  __device__ __forceinline__ static hcnn_word4 read(const char* lds, uint32_t base, uint32_t s, uint32_t lane) {
+    const uint32_t g = lane / 16, i = lane % 16;
+    if constexpr (LAYOUT == kAlongK) {
+      return *reinterpret_cast<const hcnn_word4*>(lds + place(base + i, s * 4 + g));
+    } else if constexpr (sizeof(T) == 2) {
+      typedef short four __attribute__((ext_vector_type(4)));
+      typedef four __attribute__((address_space(3)))* lptr;
+      const uint32_t k = s * 32 + g * 8 + i / 4;
+      const four lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(lds + place(k, base / 8) + (i % 4) * 8));
+      const four hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(lds + place(k + 4, base / 8) + (i % 4) * 8));
+      typedef uint32_t two __attribute__((ext_vector_type(2)));
+      const two l = __builtin_bit_cast(two, lo), h = __builtin_bit_cast(two, hi);
+      return hcnn_word4{l.x, l.y, h.x, h.y};
+    } else {
+      hcnn_word4 v;
+#pragma unroll
+      for (uint32_t j = 0; j < 4; ++j)
+        v[j] = *reinterpret_cast<const uint32_t*>(lds + place(s * 16 + g * 4 + j, base / 4) + i * 4);
+      return v;
+    }
+  }
+#endif
+  // number (row, k) of the stage, for the checker
+  HCNN_HD static float at(const char* lds, uint32_t row, uint32_t k) {
+    T t;
+    if constexpr (LAYOUT == kAlongK) __builtin_memcpy(&t, lds + place(row, k / kPer16) + k % kPer16 * sizeof(T), sizeof(T));
+    else __builtin_memcpy(&t, lds + place(k, row / kPer16) + row % kPer16 * sizeof(T), sizeof(T));
+    return Num<T>::widen(t);
+  }
+};
+
+#if defined(__HIP_DEVICE_COMPILE__)
+typedef float hcnn_float4 __attribute__((ext_vector_type(4)));
+// acc += b (16 n) x a (16 m) over a 64-byte step
+template <class T>
+__device__ __forceinline__ void mma(hcnn_float4& acc, hcnn_word4 b, hcnn_word4 a) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__builtin_bit_cast(float, (uint32_t)b[j]), __builtin_bit_cast(float, (uint32_t)a[j]), acc, 0, 0, 0);
+  } else if constexpr (std::is_same_v<T, Half>) {
+    typedef _Float16 v8 __attribute__((ext_vector_type(8)));
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8, b), __builtin_bit_cast(v8, a), acc, 0, 0, 0);
+  } else {
+    typedef __bf16 v8 __attribute__((ext_vector_type(8)));
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8, b), __builtin_bit_cast(v8, a), acc, 0, 0, 0);
+  }
+}
+#else
+struct hcnn_float4 {
+  float v[4];
+  HCNN_HD float& operator[](int i) { return v[i]; }
+  HCNN_HD float operator[](int i) const { return v[i]; }
+};
+#endif
+
+template <class T, int LA, int LB, int BM, int BN, int WM, int WN, int EPI>
+struct Gemm {
+  static constexpr int kThreads = WM * WN * 64;
+  static constexpr int kLoopPhases = 1;
+  static constexpr int kPhases = EPI == kEpiStats ? 3 : 2;
+  static constexpr int kMinWavesPerSimd = 2;
+  static constexpr uint32_t kStage = GemmNum<T>::kStage;
+  static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+  typedef GemmOperand<T, LA, BM, kThreads> A;
+  typedef GemmOperand<T, LB, BN, kThreads> B;
+  static constexpr uint32_t kBuffer = A::kLdsBytes + B::kLdsBytes;
+  static constexpr size_t kLdsBytes = 2 * kBuffer;
+  static_assert(EPI != kEpiStats || BM * WN * 4 * 8 <= 2 * kBuffer, "the statistics fit the stages' memory");
+
+  struct Regs {
+    uint32_t iter;
+    uint32_t m0, n0, k_begin, k_end, M, split;
+    U4 ra[A::kEach], rb[B::kEach];
+    hcnn_float4 acc[FM][FN];
+  };
+
+  HCNN_HD static uint32_t counted(const GemmArgs& a, uint32_t which, uint32_t all) {
+    if (a.count_of != which) return all;
+    const uint32_t c = wave_uniform(*a.count);
+    return c < all ? c : all;
+  }
+  // stages of each part of k
+  HCNN_HD static uint32_t loop_count(const GemmArgs& a) {
+    const uint32_t stages = (counted(a, kCountK, a.K) + kStage - 1) / kStage;
+    return (stages + a.splits - 1) / a.splits;
+  }
+  // Workgroups go round the eight dies; each die takes a run of consecutive tiles, which walk through bands of eight tiles of m, so
+  // that the operands' rows that its workgroups read at a time are few.  Tiles beyond the counted rows are not in the order.
+  HCNN_HD static bool skip(const GemmArgs& a, unsigned bid) {
+    if (a.count_of != kCountM) return false;
+    const uint64_t tiles = (uint64_t)((counted(a, kCountM, a.M) + BM - 1) / BM) * ((a.N + BN - 1) / BN) * a.splits;
+    return bid >= tiles;
+  }
+  HCNN_HD static void place(const GemmArgs& a, unsigned bid, Regs& r) {
+    r.M = counted(a, kCountM, a.M);
+    const uint32_t tm = (r.M + BM - 1) / BM, tn = (a.N + BN - 1) / BN, all = tm * tn * a.splits;
+    const uint32_t die = bid % 8, each = all / 8, rest = all % 8;
+    uint32_t at = die * each + (die < rest ? die : rest) + bid / 8;
+    r.split = at / (tm * tn);
+    at -= r.split * (tm * tn);
+    constexpr uint32_t kBand = 8;
+    const uint32_t band = at / (kBand * tn), high = tm - band * kBand < kBand ? tm - band * kBand : kBand;
+    at -= band * kBand * tn;
+    r.m0 = (band * kBand + at % high) * BM;
+    r.n0 = at / high * BN;
+    const uint32_t K = counted(a, kCountK, a.K), run = loop_count(a) * kStage;
+    r.k_begin = r.split * run;
+    r.k_end = K < r.k_begin + run ? K : r.k_begin + run;
+  }
+  HCNN_HD static void fetch(const GemmArgs& a, uint32_t k0, int tid, Regs& r) {
+    A::load(static_cast<const T*>(a.a), a.lda, a.a_extent, r.M, r.k_end, a.gather & kGatherA ? a.rows : nullptr, r.m0, k0, tid, r.ra);
+    B::load(static_cast<const T*>(a.b), a.ldb, a.b_extent, a.N, r.k_end, a.gather & kGatherB ? a.rows : nullptr, r.n0, k0, tid, r.rb);
+  }
+  HCNN_HD static void keep(char* lds, int tid, const Regs& r) {
+    A::store(lds, tid, r.ra);
+    B::store(lds + A::kLdsBytes, tid, r.rb);
+  }
+  HCNN_HD static void begin(const GemmArgs& a, unsigned bid, int tid, uint32_t* lds, Regs& r) {
+    place(a, bid, r);
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.acc[i][j][e] = 0.0f;
+    fetch(a, r.k_begin, tid, r);
+    keep(reinterpret_cast<char*>(lds), tid, r);
+  }
+  HCNN_HD static void multiply(const char* lds, int tid, Regs& r) {
+    const uint32_t wave = (uint32_t)tid / 64, lane = (uint32_t)tid % 64;
+    const uint32_t mw = wave / WN * (FM * 16), nw = wave % WN * (FN * 16);
+    const char* lb = lds + A::kLdsBytes;
+#if defined(__HIP_DEVICE_COMPILE__)
+#pragma unroll
+    for (uint32_t s = 0; s < 2; ++s) {
+      hcnn_word4 fb[FN], fa[FM];
+#pragma unroll
+      for (int j = 0; j < FN; ++j) fb[j] = B::read(lb, nw + j * 16, s, lane);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) fa[i] = A::read(lds, mw + i * 16, s, lane);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) mma<T>(r.acc[i][j], fb[j], fa[i]);
+    }
+#else
+    for (int i = 0; i < FM; ++i)
+      for (int j = 0; j < FN; ++j)
+        for (uint32_t e = 0; e < 4; ++e)
+          for (uint32_t k = 0; k < kStage; ++k)
+            r.acc[i][j][e] += A::at(lds, mw + i * 16 + lane % 16, k) * B::at(lb, nw + j * 16 + lane / 16 * 4 + e, k);
+#endif
+  }
+
+  template <int PH>
+  HCNN_HD static void phase(const GemmArgs& a, unsigned, int tid, uint32_t* lds_words, Regs& r) {
+    char* lds = reinterpret_cast<char*>(lds_words);
+    const uint32_t wave = (uint32_t)tid / 64, lane = (uint32_t)tid % 64;
+    const uint32_t m_lane = wave / WN * (FM * 16) + lane % 16, n_lane = wave % WN * (FN * 16) + lane / 16 * 4;   // in the tile
+    if constexpr (PH == 0) {
+      const uint32_t k_next = r.k_begin + (r.iter + 1) * kStage;
+      const bool more = k_next < r.k_end;
+      if (more) fetch(a, k_next, tid, r);
+      if (r.k_begin + r.iter * kStage < r.k_end) multiply(lds + r.iter % 2 * kBuffer, tid, r);
+      if (more) keep(lds + (r.iter + 1) % 2 * kBuffer, tid, r);
+    } else if constexpr (EPI == kEpiOut || EPI == kEpiSums) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const uint32_t m = r.m0 + m_lane + i * 16;
+        if (m >= r.M) continue;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          const uint32_t n = r.n0 + n_lane + j * 16;
+          if (n >= a.N) continue;
+          float v[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = r.acc[i][j][e];
+          if (a.addend && r.split == 0) {
+            float old[4];
+            load4(a.addend + (size_t)m * a.ld_sums + n, old);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += old[e];
+          }
+          if constexpr (EPI == kEpiOut) finish4<T>(a, m, n, v);
+          else store4(a.sums + ((size_t)r.split * a.M + m) * a.ld_sums + n, v);
+        }
+      }
+    } else if constexpr (EPI == kEpiStats) {
+      float* part = reinterpret_cast<float*>(lds);                 // [2][WN * 4][BM]
+      if constexpr (PH == 1) {
+        // each lane's largest score of a row and the exponentials relative to it; the class's own score has one owner
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+          const uint32_t m = r.m0 + m_lane + i * 16;
+          const uint32_t t = m < r.M ? a.target[m] : 0xffffffffu;
+          float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (r.n0 + n_lane + j * 16 + e < a.N) top = fmaxf(top, r.acc[i][j][e]);
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t n = r.n0 + n_lane + j * 16 + e;
+              if (n < a.N) sum += exp_of(r.acc[i][j][e] - top);
+              if (n == t) a.target_score[m] = r.acc[i][j][e];
+            }
+          const uint32_t at = (wave % WN * 4 + lane / 16) * BM + m_lane + i * 16;
+          part[at] = top;
+          part[WN * 4 * BM + at] = sum;
+        }
+      } else if (tid < BM && r.m0 + tid < r.M) {
+        float top = -INFINITY, sum = 0.0f;
+        for (int w = 0; w < WN * 4; ++w) top = fmaxf(top, part[w * BM + tid]);
+        for (int w = 0; w < WN * 4; ++w) {
+          const float s = part[(WN * 4 + w) * BM + tid];
+          if (s != 0.0f) sum += s * exp_of(part[w * BM + tid] - top);
+        }
+        float* to = a.stats + (size_t)(r.n0 / BN) * 2 * a.ld_stats + r.m0 + tid;
+        to[0] = top;
+        to[a.ld_stats] = sum;
+      }
+    } else {
+      // the gradient of the row's loss for its scores, times delta_scale: what the two products after this take as an operand,
+      // so that it is rounded to their type here
+#pragma unroll
+      for (int i = 0; i < FM; ++i) {
+        const uint32_t m = r.m0 + m_lane + i * 16;
+        if (m >= r.M) continue;
+        const float lse = a.lse[m];
+        const uint32_t t = a.target[m] - a.n_offset;
+#pragma unroll
+        for (int j = 0; j < FN; ++j) {
+          const uint32_t n = r.n0 + n_lane + j * 16;
+          if (n >= a.N) continue;
+          float v[4];
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e) v[e] = (exp_of(r.acc[i][j][e] - lse) - (n + e == t ? 1.0f : 0.0f)) * a.delta_scale;
+          store4(static_cast<T*>(a.out) + (size_t)m * a.ld_out + n, a.N - n, v);
+        }
+      }
+    }
+  }
+};
+
+// Joins the parts of k: four outputs of a row per thread.
+template <class T>
+struct GemmJoin {
+  static constexpr int kThreads = 256;
+  static constexpr int kPhases = 1;
+  struct Regs {};
+  static size_t grid(const GemmArgs& a) { return ((size_t)a.M * ((a.N + 3) / 4) + kThreads - 1) / kThreads; }
+  template <int PH>
+  HCNN_HD static void phase(const GemmArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
+    const uint32_t quads = (a.N + 3) / 4;
+    const size_t at = (size_t)bid * kThreads + tid;
+    const size_t m = at / quads;
+    const uint32_t n = (uint32_t)(at - m * quads) * 4;
+    const uint32_t M = a.count_of == kCountM && *a.count < a.M ? *a.count : a.M;
+    if (m >= M) return;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (uint32_t s = 0; s < a.splits; ++s) {
+      float x[4];
+      load4(a.sums + ((size_t)s * a.M + m) * a.ld_sums + n, x);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += x[e];
+    }
+    finish4<T>(a, (uint32_t)m, n, v);
+  }
+};
+
+// ---------------------------------------------------------------- gradient of the activation and of the bias
+// dz = dy * act'(z) (written where z is there: rounded to T, the operand type of the two products that take it) and, per block of
+// rows, the columns' sums of it in 32 bits.  A workgroup takes `rows_each` rows and kCols columns: lanes along the row, four numbers each.
+struct ActGradArgs {
+  const void *dy, *z;
+  void* dz;
+  float* part;                // [row blocks][ld_part], null: no sums
+  size_t ld_dy, ld_z, ld_dz, ld_part;
+  uint32_t M, N, rows_each, col_blocks;
+  int act;
+};
+template <class T, int LANES>
+struct ActGrad {
+  static constexpr int kThreads = 256;
+  static constexpr int kPhases = 2;
+  static constexpr uint32_t kCols = LANES * 4, kLines = kThreads / LANES;
+  static constexpr size_t kLdsBytes = kThreads * 16;
+  struct Regs {};
+  template <int PH>
+  HCNN_HD static void phase(const ActGradArgs& a, unsigned bid, int tid, uint32_t* lds_words, Regs&) {
+    float* lds = reinterpret_cast<float*>(lds_words);              // [kLines][kCols]
+    const uint32_t cb = bid % a.col_blocks, rb = bid / a.col_blocks;
+    const uint32_t lane = (uint32_t)tid % LANES, line = (uint32_t)tid / LANES;
+    const uint32_t n = cb * kCols + lane * 4;
+    if constexpr (PH == 0) {
+      const uint32_t m0 = rb * a.rows_each, m1 = a.M - m0 < a.rows_each ? a.M : m0 + a.rows_each;
+      float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (n < a.N) {
+        const uint32_t left = a.N - n;
+#pragma unroll 4
+        for (uint32_t m = m0 + line; m < m1; m += kLines) {
+          float v[4];
+          load4(static_cast<const T*>(a.dy) + m * a.ld_dy + n, left, v);
+          if (a.z) {
+            float z[4];
+            load4(static_cast<const T*>(a.z) + m * a.ld_z + n, left, z);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] *= slope_of(z[e], a.act);
+            store4(static_cast<T*>(a.dz) + m * a.ld_dz + n, left, v);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[e] += v[e];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) lds[line * kCols + lane * 4 + e] = sum[e];
+    } else if (a.part) {
+      for (uint32_t c = tid; c < kCols; c += kThreads) {
+        float s = 0.0f;
+        for (uint32_t l = 0; l < kLines; ++l) s += lds[l * kCols + c];
+        if (cb * kCols + c < a.N) a.part[(size_t)rb * a.ld_part + cb * kCols + c] = s;
+      }
+    }
+  }
+};
+struct ColumnSumArgs {
+  const float* part;          // [blocks][ld_part]
+  size_t ld_part;
+  uint32_t blocks, N;
+  void* out;
+};
+// Sums of the blocks' sums: a workgroup takes 16 columns, 16 threads each.
+template <class T>
+struct ColumnSum {
+  static constexpr int kThreads = 256;
+  static constexpr int kPhases = 2;
+  static constexpr size_t kLdsBytes = kThreads * 4;
+  struct Regs {};
+  template <int PH>
+  HCNN_HD static void phase(const ColumnSumArgs& a, unsigned bid, int tid, uint32_t* lds_words, Regs&) {
+    float* lds = reinterpret_cast<float*>(lds_words);
+    const uint32_t n = bid * 16 + tid % 16;
+    if constexpr (PH == 0) {
+      float s = 0.0f;
+      if (n < a.N)
+        for (uint32_t b = tid / 16; b < a.blocks; b += 16) s += a.part[b * a.ld_part + n];
+      lds[tid] = s;
+    } else if (tid < 16 && n < a.N) {
+      float s = 0.0f;
+      for (int l = 0; l < 16; ++l) s += lds[l * 16 + tid];
+      static_cast<T*>(a.out)[n] = Num<T>::narrow(s);
+    }
+  }
+};
+
+// ---------------------------------------------------------------- rows whose target is a class
+struct KeepRowsArgs {
+  const void* targets;        // int32 or int64
+  int wide;
+  int64_t ignore;
+  uint32_t M, classes;
+  uint32_t* rows;             // [M] rows that take part, in order
+  uint32_t* target;           // [M] their classes
+  uint32_t* count;
+  unsigned long long* bad;    // targets that are neither a class nor the ignored value
+};
+// One workgroup: a run of consecutive rows per thread.
+struct KeepRows {
+  static constexpr int kThreads = 1024;
+  static constexpr int kPhases = 3;
+  static constexpr size_t kLdsBytes = (kThreads + 32) * 4;
+  struct Regs { uint32_t mine; };
+  HCNN_HD static int64_t target(const KeepRowsArgs& a, uint32_t m) {
+    return a.wide ? static_cast<const int64_t*>(a.targets)[m] : static_cast<const int32_t*>(a.targets)[m];
+  }
+  HCNN_HD static bool kept(const KeepRowsArgs& a, int64_t t) { return t != a.ignore && t >= 0 && t < (int64_t)a.classes; }
+  template <int PH>
+  HCNN_HD static void phase(const KeepRowsArgs& a, unsigned, int tid, uint32_t* lds, Regs& r) {
+    const uint32_t each = (a.M + kThreads - 1) / kThreads;
+    const uint32_t m0 = (uint32_t)tid * each < a.M ? tid * each : a.M, m1 = a.M - m0 < each ? a.M : m0 + each;
+    if constexpr (PH == 0) {
+      uint32_t n = 0;
+      for (uint32_t m = m0; m < m1; ++m) {
+        const int64_t t = target(a, m);
+        if (kept(a, t)) ++n;
+        else if (t != a.ignore) atomic_inc64(a.bad);
+      }
+      r.mine = n;
+      lds[tid] = n;
+    } else if constexpr (PH == 1) {
+      if (tid < 32) {
+        uint32_t s = 0;
+        for (int i = 0; i < 32; ++i) s += lds[tid * 32 + i];
+        lds[kThreads + tid] = s;
+      }
+    } else {
+      uint32_t at = 0;
+      for (int i = 0; i < tid / 32; ++i) at += lds[kThreads + i];
+      for (int i = tid / 32 * 32; i < tid; ++i) at += lds[i];
+      if (tid == kThreads - 1) *a.count = at + r.mine;
+      for (uint32_t m = m0; m < m1; ++m) {
+        const int64_t t = target(a, m);
+        if (!kept(a, t)) continue;
+        a.rows[at] = m;
+        a.target[at] = (uint32_t)t;
+        ++at;
+      }
+    }
+  }
+};
+
+// ---------------------------------------------------------------- softmax statistics of whole rows
+struct RowStatsArgs {
+  const float* stats;         // [tiles][2][ld_stats]
+  size_t ld_stats;
+  uint32_t tiles, M;
+  const uint32_t* count;
+  const uint32_t* rows;
+  const float* target_score;
+  float* lse;                 // [rows that take part]
+  double* part;               // [workgroups] sums of the losses
+  float *row_loss, *row_lse;  // [M] or null
+};
+// 64 rows per workgroup, four threads each.
+struct RowStats {
+  static constexpr int kThreads = 256;
+  static constexpr uint32_t kRows = 64;
+  static constexpr int kPhases = 3;
+  static constexpr size_t kLdsBytes = (2 * kThreads + 2 * kRows) * 4;
+  struct Regs {};
+  template <int PH>
+  HCNN_HD static void phase(const RowStatsArgs& a, unsigned bid, int tid, uint32_t* lds_words, Regs&) {
+    float* lds = reinterpret_cast<float*>(lds_words);
+    double* losses = reinterpret_cast<double*>(lds + 2 * kThreads);
+    const uint32_t m = bid * kRows + tid % kRows;
+    const uint32_t M = *a.count;
+    if constexpr (PH == 0) {
+      float top = -INFINITY, sum = 0.0f;
+      if (m < M)
+        for (uint32_t t = tid / kRows; t < a.tiles; t += 4) {
+          const float* s = a.stats + (size_t)t * 2 * a.ld_stats + m;
+          const float x = s[0], y = s[a.ld_stats], high = fmaxf(top, x);
+          sum = (sum != 0.0f ? sum * exp_of(top - high) : 0.0f) + y * exp_of(x - high);
+          top = high;
+        }
+      lds[tid] = top;
+      lds[kThreads + tid] = sum;
+    } else if constexpr (PH == 1) {
+      if (tid < (int)kRows) {
+        double loss = 0.0;
+        if (m < M) {
+          float top = -INFINITY, sum = 0.0f;
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, lds[i * kRows + tid]);
+          for (int i = 0; i < 4; ++i) {
+            const float s = lds[kThreads + i * kRows + tid];
+            if (s != 0.0f) sum += s * exp_of(lds[i * kRows + tid] - top);
+          }
+          const float log_sum = logf(sum), lse = top + log_sum;
+          // (the difference of the two large numbers first)
+          const float l = (top - a.target_score[m]) + log_sum;
+          a.lse[m] = lse;
+          if (a.row_loss) a.row_loss[a.rows[m]] = l;
+          if (a.row_lse) a.row_lse[a.rows[m]] = lse;
+          loss = l;
+        }
+        losses[tid] = loss;
+      }
+    } else if (tid == 0) {
+      double s = 0.0;
+      for (uint32_t i = 0; i < kRows; ++i) s += losses[i];
+      a.part[bid] = s;
+    }
+  }
+};
+struct MeanLossArgs {
+  const double* part;
+  uint32_t parts;
+  const uint32_t* count;
+  float* loss;                // mean over the rows that take part, 0 where there are none (may be null)
+  float* alpha;               // scale / count (may be null)
+  float scale;
+};
+struct MeanLoss {
+  static constexpr int kThreads = 256;
+  static constexpr int kPhases = 2;
+  static constexpr size_t kLdsBytes = kThreads * 8;
+  struct Regs {};
+  template <int PH>
+  HCNN_HD static void phase(const MeanLossArgs& a, unsigned, int tid, uint32_t* lds_words, Regs&) {
+    double* lds = reinterpret_cast<double*>(lds_words);
+    if constexpr (PH == 0) {
+      double s = 0.0;
+      for (uint32_t i = tid; i < a.parts; i += kThreads) s += a.part[i];
+      lds[tid] = s;
+    } else if (tid == 0) {
+      double s = 0.0;
+      for (int i = 0; i < kThreads; ++i) s += lds[i];
+      const uint32_t n = *a.count ? *a.count : 1;
+      if (a.loss) *a.loss = (float)(s / n);
+      if (a.alpha) *a.alpha = (float)((double)a.scale / n);
+    }
+  }
+};
+// Rows that do not take part: zeros in the gradient, and in the losses and statistics asked for.  One row per 64 threads.
+struct BlankRowsArgs {
+  KeepRowsArgs keep;
+  void* dx;                   // null: none
+  size_t ld_dx;               // bytes
+  size_t row_bytes;
+  float *row_loss, *row_lse;
+};
+struct BlankRows {
+  static constexpr int kThreads = 256;
+  static constexpr int kPhases = 1;
+  struct Regs {};
+  template <int PH>
+  HCNN_HD static void phase(const BlankRowsArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
+    const uint32_t m = bid * 4 + tid / 64, lane = tid % 64;
+    if (m >= a.keep.M || KeepRows::kept(a.keep, KeepRows::target(a.keep, m))) return;
+    if (lane == 0 && a.row_loss) a.row_loss[m] = 0.0f;
+    if (lane == 0 && a.row_lse) a.row_lse[m] = 0.0f;
+    if (!a.dx) return;
+    char* row = static_cast<char*>(a.dx) + m * a.ld_dx;
+    const size_t whole = a.row_bytes / 16 * 16;
+    const U4 zero{};
+    for (size_t b = (size_t)lane * 16; b < whole; b += 1024) st16(row + b, zero);
+    for (size_t b = whole + (size_t)lane * 2; b < a.row_bytes; b += 128) *reinterpret_cast<uint16_t*>(row + b) = 0;
+  }
+};
+
+// ---------------------------------------------------------------- norm of many gradients
+// A list of tensors travels in the launch's arguments; a workgroup takes runs of kRun numbers, `first` tells whose they are.
+constexpr uint32_t kNormTensors = 96;
+constexpr uint32_t kNormRun = 16384;
+struct NormArgs {
+  const void* in[kNormTensors];
+  void* out[kNormTensors];
+  uint64_t size[kNormTensors];
+  uint32_t first[kNormTensors + 1];        // first run of each tensor; the last entry: number of runs
+  uint8_t type[kNormTensors];              // 0: 32 bits, 1: binary16, 2: bfloat16
+  uint32_t tensors;
+  double* part;                            // sums of squares of the whole list, a number per workgroup
+  uint32_t part_first, parts;              // of this launch, of all
+  double max_norm, eps;
+  float* norm;                             // written by workgroup 0 of the first launch
+};
+struct NormRun { const char* in; char* out; uint32_t n; int type; };
+HCNN_HD NormRun norm_run(const NormArgs& a, uint32_t run) {
+  uint32_t lo = 0, hi = a.tensors;                                // first[lo] <= run < first[hi]
+  while (hi - lo > 1) {
+    const uint32_t mid = (lo + hi) / 2;
+    if (a.first[mid] <= run) lo = mid; else hi = mid;
+  }
+  NormRun r;
+  r.type = a.type[lo];
+  const uint64_t at = (uint64_t)(run - a.first[lo]) * kNormRun, left = a.size[lo] - at;
+  const uint32_t bytes = r.type == 0 ? 4 : 2;
+  r.in = static_cast<const char*>(a.in[lo]) + at * bytes;
+  r.out = a.out[lo] ? static_cast<char*>(a.out[lo]) + at * bytes : nullptr;
+  r.n = left < kNormRun ? (uint32_t)left : kNormRun;
+  return r;
+}
+// Squares are summed in 64 bits: no square of a 32-bit number leaves their range, and the sum's order does not show in a 32-bit norm.
+template <class T>
+HCNN_HD double sum_squares(const T* p, uint32_t n, int tid, int threads) {
+  constexpr uint32_t kPer16 = 16 / sizeof(T);
+  double s = 0.0;
+  const uint32_t whole = n / kPer16;
+#pragma unroll 4
+  for (uint32_t i = tid; i < whole; i += threads) {
+    const U4 w = ld16(reinterpret_cast<const char*>(p + (size_t)i * kPer16));
+    T t[kPer16];
+    __builtin_memcpy(t, &w, 16);
+#pragma unroll
+    for (uint32_t e = 0; e < kPer16; ++e) { const double x = Num<T>::widen(t[e]); s += x * x; }
+  }
+  for (uint32_t i = whole * kPer16 + tid; i < n; i += threads) { const double x = Num<T>::widen(p[i]); s += x * x; }
+  return s;
+}
+struct SumSquares {
+  static constexpr int kThreads = 256;
+  static constexpr int kPhases = 3;
+  static constexpr size_t kLdsBytes = kThreads * 8;
+  struct Regs {};
+  template <int PH>
+  HCNN_HD static void phase(const NormArgs& a, unsigned bid, int tid, uint32_t* lds_words, Regs&) {
+    double* lds = reinterpret_cast<double*>(lds_words);
+    if constexpr (PH == 0) {
+      const NormRun r = norm_run(a, bid);
+      lds[tid] = r.type == 0 ? sum_squares(reinterpret_cast<const float*>(r.in), r.n, tid, kThreads)
+               : r.type == 1 ? sum_squares(reinterpret_cast<const Half*>(r.in), r.n, tid, kThreads)
+                             : sum_squares(reinterpret_cast<const Bfloat*>(r.in), r.n, tid, kThreads);
+    } else if constexpr (PH == 1) {
+      if (tid < 16) {
+        double s = 0.0;
+        for (int i = 0; i < 16; ++i) s += lds[tid * 16 + i];
+        lds[tid * 16] = s;
+      }
+    } else if (tid == 0) {
+      double s = 0.0;
+      for (int i = 0; i < 16; ++i) s += lds[i * 16];
+      a.part[a.part_first + bid] = s;
+    }
+  }
+};
+struct NormTotalArgs {
+  const double* part;
+  uint32_t parts;
+  double max_norm, eps;
+  float* norm;
+  float* factor;
+};
+struct NormTotal {
+  static constexpr int kThreads = 1024;
+  static constexpr int kPhases = 3;
+  static constexpr size_t kLdsBytes = kThreads * 8;
+  struct Regs {};
+  template <int PH>
+  HCNN_HD static void phase(const NormTotalArgs& a, unsigned, int tid, uint32_t* lds_words, Regs&) {
+    double* lds = reinterpret_cast<double*>(lds_words);
+    if constexpr (PH == 0) {
+      double s = 0.0;
+      for (uint32_t i = tid; i < a.parts; i += kThreads) s += a.part[i];
+      lds[tid] = s;
+    } else if constexpr (PH == 1) {
+      if (tid < 32) {
+        double s = 0.0;
+        for (int i = 0; i < 32; ++i) s += lds[tid * 32 + i];
+        lds[tid * 32] = s;
+      }
+    } else if (tid == 0) {
+      double s = 0.0;
+      for (int i = 0; i < 32; ++i) s += lds[i * 32];
+      const double norm = sqrt(s), c = a.max_norm / (norm + a.eps);
+      *a.norm = (float)norm;
+      *a.factor = c < 1.0 || c != c ? (float)c : 1.0f;              // a norm that is no number makes the factor none
+    }
+  }
+};
+template <class T>
+HCNN_HD void scale_run(const T* p, T* to, uint32_t n, float c, int tid, int threads) {
+  constexpr uint32_t kPer16 = 16 / sizeof(T);
+  const uint32_t whole = n / kPer16;
+#pragma unroll 4
+  for (uint32_t i = tid; i < whole; i += threads) {
+    U4 w = ld16(reinterpret_cast<const char*>(p + (size_t)i * kPer16));
+    T t[kPer16];
+    __builtin_memcpy(t, &w, 16);
+#pragma unroll
+    for (uint32_t e = 0; e < kPer16; ++e) t[e] = Num<T>::narrow(Num<T>::widen(t[e]) * c);
+    __builtin_memcpy(&w, t, 16);
+    st16(reinterpret_cast<char*>(to + (size_t)i * kPer16), w);
+  }
+  for (uint32_t i = whole * kPer16 + tid; i < n; i += threads) to[i] = Num<T>::narrow(Num<T>::widen(p[i]) * c);
+}
+struct ScaleGrads {
+  static constexpr int kThreads = 256;
+  static constexpr int kPhases = 1;
+  struct Regs {};
+  template <int PH>
+  HCNN_HD static void phase(const NormArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
+    const float c = *a.norm;                                        // the factor
+    const NormRun r = norm_run(a, bid);
+    if (c == 1.0f && r.in == r.out) return;                         // nothing to scale, nowhere to copy
+    if (r.type == 0) scale_run(reinterpret_cast<const float*>(r.in), reinterpret_cast<float*>(r.out), r.n, c, tid, kThreads);
+    else if (r.type == 1) scale_run(reinterpret_cast<const Half*>(r.in), reinterpret_cast<Half*>(r.out), r.n, c, tid, kThreads);
+    else scale_run(reinterpret_cast<const Bfloat*>(r.in), reinterpret_cast<Bfloat*>(r.out), r.n, c, tid, kThreads);
+  }
+};
+
+}  // namespace hcnn

@@ -14,6 +14,8 @@
 // a GPU) runs the same phase bodies as plain loops over blocks and threads; it is
 // a checker for the kernel sources, not a product path, and the Python binding
 // never loads it.
+// Optional: begin(args, block, tid, lds, regs)   runs before the repeated phases, with a barrier behind it
+// Optional: skip(args, block)   true: the workgroup has nothing to do (the same answer for all of its threads)
 // Optional: wave_sync(ph)       true: up to the next barrier the phases after ph touch only LDS words that no other
 //                               wave touches in between, and no barrier stands after ph (of the last repeated phase: in front
 //                               of what follows it, the next iteration or the rest).  The checker runs the phases
@@ -183,6 +185,10 @@ template <class K, class = void> struct MinWavesPerSimd { static constexpr int v
 template <class K> struct MinWavesPerSimd<K, std::void_t<decltype(K::kMinWavesPerSimd)>> { static constexpr int value = K::kMinWavesPerSimd; };
 template <class K, class = void> struct WaveSync { static constexpr bool after(int) { return false; } };
 template <class K> struct WaveSync<K, std::void_t<decltype(K::wave_sync(0))>> { static constexpr bool after(int ph) { return K::wave_sync(ph); } };
+template <class K, class = void> struct HasBegin : std::false_type {};
+template <class K> struct HasBegin<K, std::void_t<decltype(&K::begin)>> : std::true_type {};
+template <class K, class = void> struct HasSkip : std::false_type {};
+template <class K> struct HasSkip<K, std::void_t<decltype(&K::skip)>> : std::true_type {};
 template <class K, class = void> struct LoopPhases { static constexpr int value = 0; };
 template <class K> struct LoopPhases<K, std::void_t<decltype(K::kLoopPhases)>> { static constexpr int value = K::kLoopPhases; };
 
@@ -258,6 +264,11 @@ int launch(hcnn_stream_t, size_t grid, size_t lds_bytes, const Args& a) {
   for (size_t i = steps.size(); i-- > 0;) steps[i].next = i + 1 == steps.size() || barrier[i] ? i + 1 : steps[i + 1].next;
   const int waves = (K::kThreads + 63) / 64;
   for (size_t bid = 0; bid < grid; ++bid) {
+    if constexpr (HasSkip<K>::value) { if (K::skip(a, (unsigned)bid)) continue; }
+    if constexpr (HasBegin<K>::value) {
+      regs.assign(K::kThreads, typename K::Regs{});
+      for (int tid = 0; tid < K::kThreads; ++tid) K::begin(a, (unsigned)bid, tid, lds.data(), regs[tid]);
+    }
     bool up = true;                                    // waves in ascending, then in descending order
     for (size_t s = 0; s < steps.size(); s = steps[s].next, up = !up)
       for (int w = 0; w < waves; ++w)
@@ -343,8 +354,13 @@ __device__ __forceinline__ void run_phases(const Args& a, unsigned bid, int tid,
 template <class K, class Args>
 __global__ void __launch_bounds__(K::kThreads, MinWavesPerSimd<K>::value) kernel_entry(const Args a) {
   extern __shared__ __align__(16) uint32_t hcnn_lds[];
+  if constexpr (HasSkip<K>::value) { if (K::skip(a, blockIdx.x)) return; }
   typename K::Regs regs;
   constexpr int LP = LoopPhases<K>::value;
+  if constexpr (HasBegin<K>::value) {
+    K::begin(a, blockIdx.x, (int)threadIdx.x, hcnn_lds, regs);
+    __syncthreads();
+  }
   if constexpr (LP > 0) {
     const uint32_t count = K::loop_count(a);
     for (uint32_t it = 0; it < count; ++it) {
