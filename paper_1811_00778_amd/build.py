@@ -6,8 +6,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_DIR = os.path.join(_HERE, "lib")
 LIB = os.path.join(LIB_DIR, "libhcnn.so")
-SOURCES = [os.path.join(CSRC, "hcnn.cpp"), os.path.join(CSRC, "plain.cpp")]
-HEADERS = [os.path.join(CSRC, h) for h in ("platform.h", "modarith.h", "ntt_kernels.h", "fv_kernels.h", "rate_kernels.h", "plain_kernels.h")]
+SOURCES = [os.path.join(CSRC, s) for s in ("hcnn.cpp", "plain.cpp", "plain_f32.cpp", "plain_f16.cpp", "plain_bf16.cpp")]
+HEADERS = [os.path.join(CSRC, h) for h in ("platform.h", "modarith.h", "ntt_kernels.h", "fv_kernels.h", "rate_kernels.h", "plain_kernels.h", "plain_host.h")]
 HEADERS.append(os.path.join(os.path.dirname(_HERE), "include", "hcnn.h"))
 
 HIPCC_FLAGS = [

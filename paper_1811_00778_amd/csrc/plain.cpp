@@ -1,286 +1,14 @@
-// C ABI of the plain (unencrypted) network's training: argument checks, choice of the kernels' shapes, their order.
-// A translation unit of its own in the device build; the CPU checker is built from hcnn.cpp, which includes this file there.
-#include "../../include/hcnn.h"
+// C ABI of the plain (unencrypted) network's training: argument checks and the calls behind them.  The device build has a
+// translation unit of its own for each number type; the CPU checker is built from hcnn.cpp, which includes this file there.
+#include "plain_host.h"
 
-#include <algorithm>
-#include <new>
-
-#include "plain_kernels.h"
-
-using namespace hcnn;
-
-struct hcnn_plain {
-  hcnn_stream_t stream = nullptr;
-  char* work = nullptr;                       // grows to the largest call's need
-  size_t work_bytes = 0;
-  unsigned long long* d_bad = nullptr;
-  uint32_t compute_units = 256;
-};
+#ifndef HCNN_HOSTEMU
+PLAIN_TYPE(extern, float)
+PLAIN_TYPE(extern, Half)
+PLAIN_TYPE(extern, Bfloat)
+#endif
 
 namespace plain_host {
-
-constexpr size_t kMaxSize = 0x7fffffff;
-constexpr size_t kDeltaBytes = (size_t)512 << 20;      // scores' gradients held at a time by hcnn_cross_entropy_grad
-
-size_t up(size_t x, size_t to) { return (x + to - 1) / to * to; }
-size_t blocks(size_t x, size_t each) { return (x + each - 1) / each; }
-size_t type_bytes(int dtype) { return dtype == HCNN_F32 ? 4 : 2; }
-bool bad_type(int dtype) { return dtype != HCNN_F32 && dtype != HCNN_F16 && dtype != HCNN_BF16; }
-bool misaligned(const void* p, int dtype) { return reinterpret_cast<uintptr_t>(p) % type_bytes(dtype) != 0; }
-
-// Work memory of one call, cut into arrays: sizes first, then addresses.
-struct Arena {
-  size_t bytes = 0;
-  size_t take(size_t n) {
-    const size_t at = bytes;
-    bytes += up(n, 256);
-    return at;
-  }
-};
-int reserve(hcnn_plain* h, size_t bytes) {
-  if (bytes <= h->work_bytes) return 0;
-  if (h->work) {
-    const int e = stream_sync(h->stream);
-    if (e) return e;
-    dev_free(h->work);
-    h->work = nullptr;
-    h->work_bytes = 0;
-  }
-  void* p = nullptr;
-  const int e = dev_malloc(&p, bytes);
-  if (e) return e;
-  h->work = static_cast<char*>(p);
-  h->work_bytes = bytes;
-  return 0;
-}
-template <class V> V* at(hcnn_plain* h, size_t offset) { return reinterpret_cast<V*>(h->work + offset); }
-
-// ---------------------------------------------------------------- tiles
-enum { kTile256, kTile128, kTile64, kTall, kFlat };
-struct Shape { int tile; uint32_t bm, bn, splits; };
-constexpr uint32_t kTileRows[] = {256, 128, 64, 128, 16}, kTileCols[] = {256, 128, 64, 16, 128};
-
-template <class T>
-Shape choose(const hcnn_plain* h, size_t M, size_t N, size_t K, bool may_split) {
-  const size_t units = h->compute_units;
-  auto tiles = [&](int t) { return blocks(M, kTileRows[t]) * blocks(N, kTileCols[t]); };
-  int t = kTile64;
-  if (N <= 16) t = kTall;
-  else if (M <= 16) t = kFlat;
-  else if (sizeof(T) == 2 && tiles(kTile256) * 4 >= units * 3) t = kTile256;
-  else if (tiles(kTile128) * 2 >= units) t = kTile128;
-  Shape s{t, kTileRows[t], kTileCols[t], 1};
-  if (may_split) {
-    // parts of at least four stages while there are fewer workgroups than two for each compute unit
-    const size_t stages = blocks(K, GemmNum<T>::kStage), want = blocks(2 * units, std::max<size_t>(1, tiles(t)));
-    const size_t most = std::max<size_t>(1, stages / 4);
-    s.splits = (uint32_t)std::max<size_t>(1, std::min(tiles(t) >= units ? 1 : want, most));
-  }
-  return s;
-}
-size_t sums_bytes(const Shape& s, size_t M, size_t N) { return s.splits > 1 ? s.splits * M * up(N, 4) * 4 : 0; }
-
-template <class G>
-int start(hcnn_plain* h, const GemmArgs& a, size_t grid) { return launch<G>(h->stream, grid, G::kLdsBytes, a); }
-
-template <class T, int LA, int LB, int EPI>
-int gemm(hcnn_plain* h, const GemmArgs& a, const Shape& s) {
-  const size_t grid = blocks(a.M, s.bm) * blocks(a.N, s.bn) * s.splits;
-  if (grid > kMaxSize) return HCNN_ERR_ARG;
-  switch (s.tile) {
-    case kTile256:
-      if constexpr (sizeof(T) == 2) return start<Gemm<T, LA, LB, 256, 256, 2, 4, EPI>>(h, a, grid);
-      return HCNN_ERR_ARG;
-    case kTile128: return start<Gemm<T, LA, LB, 128, 128, 2, 2, EPI>>(h, a, grid);
-    case kTile64: return start<Gemm<T, LA, LB, 64, 64, 2, 2, EPI>>(h, a, grid);
-    case kTall: return start<Gemm<T, LA, LB, 128, 16, 4, 1, EPI>>(h, a, grid);
-    default: return start<Gemm<T, LA, LB, 16, 128, 1, 4, EPI>>(h, a, grid);
-  }
-}
-// The product with the linear layer's ending, in parts of k where the shape says so (their sums at `sums`).
-template <class T, int LA, int LB>
-int product(hcnn_plain* h, GemmArgs a, const Shape& s, float* sums) {
-  if (a.M == 0 || a.N == 0) return 0;
-  a.splits = s.splits;
-  if (s.splits == 1) return gemm<T, LA, LB, kEpiOut>(h, a, s);
-  a.sums = sums;
-  a.ld_sums = up(a.N, 4);
-  const int e = gemm<T, LA, LB, kEpiSums>(h, a, s);
-  return e ? e : launch<GemmJoin<T>>(h->stream, GemmJoin<T>::grid(a), 0, a);
-}
-
-GemmArgs operands(const void* a, size_t lda, size_t a_rows, size_t a_cols, const void* b, size_t ldb, size_t b_rows, size_t b_cols) {
-  GemmArgs g{};
-  g.a = a; g.lda = lda; g.a_extent = a_rows ? (a_rows - 1) * lda + a_cols : 0;
-  g.b = b; g.ldb = ldb; g.b_extent = b_rows ? (b_rows - 1) * ldb + b_cols : 0;
-  g.splits = 1;
-  return g;
-}
-
-// ---------------------------------------------------------------- linear layer
-template <class T>
-int linear(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void* x, size_t ldx, const void* w, size_t ldw, const void* bias,
-           const void* residual, size_t ld_residual, void* y, size_t ldy, void* z, size_t ldz) {
-  const Shape s = choose<T>(h, M, N, K, true);
-  const int e = reserve(h, sums_bytes(s, M, N));
-  if (e) return e;
-  GemmArgs g = operands(x, ldx, M, K, w, ldw, N, K);
-  g.M = (uint32_t)M; g.N = (uint32_t)N; g.K = (uint32_t)K;
-  g.act = act; g.bias = bias; g.residual = residual; g.ld_residual = ld_residual;
-  g.out = y; g.ld_out = ldy; g.z = z; g.ld_z = ldz;
-  return product<T, kAlongK, kAlongK>(h, g, s, at<float>(h, 0));
-}
-
-template <class T>
-int act_grad(hcnn_plain* h, ActGradArgs a, size_t* row_blocks, bool only_size) {
-  // at least 64 rows a workgroup, and no more workgroups than eight for each compute unit
-  const int lanes = a.N <= 16 ? 4 : a.N <= 64 ? 16 : 64;
-  a.col_blocks = (uint32_t)std::max<size_t>(1, blocks(a.N, lanes * 4));
-  const size_t most = std::max<size_t>(1, (size_t)h->compute_units * 8 / a.col_blocks);
-  a.rows_each = (uint32_t)std::max<size_t>(64, up(blocks(a.M, most), 64));
-  *row_blocks = blocks(a.M, a.rows_each);
-  if (only_size) return 0;
-  const size_t grid = *row_blocks * a.col_blocks;
-  switch (lanes) {
-    case 4: return launch<ActGrad<T, 4>>(h->stream, grid, ActGrad<T, 4>::kLdsBytes, a);
-    case 16: return launch<ActGrad<T, 16>>(h->stream, grid, ActGrad<T, 16>::kLdsBytes, a);
-    default: return launch<ActGrad<T, 64>>(h->stream, grid, ActGrad<T, 64>::kLdsBytes, a);
-  }
-}
-
-template <class T>
-int linear_grad(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void* dy, size_t ld_dy, const void* x, size_t ldx, const void* w,
-                size_t ldw, const void* z, size_t ldz, void* dx, size_t ld_dx, void* dw, size_t ld_dw, void* db) {
-  const Shape sx = choose<T>(h, M, K, N, true), sw = choose<T>(h, N, K, M, true);
-  ActGradArgs ag{};
-  ag.dy = dy; ag.ld_dy = ld_dy; ag.M = (uint32_t)M; ag.N = (uint32_t)N; ag.act = act;
-  if (act != kActNone) { ag.z = z; ag.ld_z = ldz; }
-  ag.ld_dz = up(N, 16 / sizeof(T)); ag.ld_part = up(N, 4);
-  size_t row_blocks = 0;
-  act_grad<T>(h, ag, &row_blocks, true);
-  Arena w_;
-  const size_t o_dz = w_.take(act != kActNone ? M * ag.ld_dz * sizeof(T) : 0), o_part = w_.take(db ? row_blocks * ag.ld_part * 4 : 0);
-  const size_t o_sums = w_.take(std::max(dx ? sums_bytes(sx, M, K) : 0, dw ? sums_bytes(sw, N, K) : 0));
-  int e = reserve(h, w_.bytes);
-  if (e) return e;
-  const void* dz = dy;
-  size_t ld_dz = ld_dy;
-  if (M && N && (act != kActNone || db)) {
-    if (act != kActNone) { ag.dz = at<void>(h, o_dz); dz = ag.dz; ld_dz = ag.ld_dz; }
-    if (db) ag.part = at<float>(h, o_part);
-    if ((e = act_grad<T>(h, ag, &row_blocks, false))) return e;
-  }
-  if (db && N) {
-    const ColumnSumArgs cs{at<float>(h, o_part), ag.ld_part, (uint32_t)(M ? row_blocks : 0), (uint32_t)N, db};
-    if ((e = launch<ColumnSum<T>>(h->stream, blocks(N, 16), ColumnSum<T>::kLdsBytes, cs))) return e;
-  }
-  if (dx) {
-    GemmArgs g = operands(dz, ld_dz, M, N, w, ldw, N, K);
-    g.M = (uint32_t)M; g.N = (uint32_t)K; g.K = (uint32_t)N;
-    g.out = dx; g.ld_out = ld_dx;
-    if ((e = product<T, kAlongK, kAcrossK>(h, g, sx, at<float>(h, o_sums)))) return e;
-  }
-  if (dw) {
-    GemmArgs g = operands(dz, ld_dz, M, N, x, ldx, M, K);
-    g.M = (uint32_t)N; g.N = (uint32_t)K; g.K = (uint32_t)M;
-    g.out = dw; g.ld_out = ld_dw;
-    if ((e = product<T, kAcrossK, kAcrossK>(h, g, sw, at<float>(h, o_sums)))) return e;
-  }
-  return 0;
-}
-
-// ---------------------------------------------------------------- softmax cross entropy
-struct LossCall {
-  size_t M, K, V;
-  const void* x; size_t ldx;
-  const void* w; size_t ldw;
-  const void* targets; int target_bytes; int64_t ignore;
-  float *row_loss, *row_lse, *loss;
-  float scale;
-  void* dx; size_t ld_dx;
-  void* dw; size_t ld_dw;
-};
-
-// A 16-bit float with 5 bits of exponent holds nothing below 2^-24: the scores' gradients, at most 1 in magnitude, are held 2^15
-// times as large there.  The factor goes back out of the sums.
-template <class T> constexpr float delta_scale() { return std::is_same_v<T, Half> ? 32768.0f : 1.0f; }
-
-template <class T>
-int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
-  const size_t M = c.M, K = c.K, V = c.V;
-  const Shape ss = choose<T>(h, M, V, K, false);
-  // columns of a piece: whole tiles, all columns where they fit
-  const size_t fit = kDeltaBytes / (std::max<size_t>(M, 1) * sizeof(T)) / 256 * 256;
-  const size_t piece = grad ? std::min(V, std::max<size_t>(fit, 256)) : 0;
-  const size_t pieces = grad ? blocks(V, piece) : 0, ld_delta = up(piece, 16 / sizeof(T));
-  Shape sx = choose<T>(h, M, K, piece, pieces == 1), sw = choose<T>(h, piece, K, M, true);
-  const size_t tiles = blocks(V, ss.bn), ld_stats = up(M, 64), row_wgs = blocks(M, RowStats::kRows);
-  Arena a;
-  const size_t o_count = a.take(4), o_alpha = a.take(4), o_rows = a.take(M * 4), o_target = a.take(M * 4), o_score = a.take(M * 4), o_lse = a.take(M * 4);
-  const size_t o_stats = a.take(tiles * 2 * ld_stats * 4), o_part = a.take(row_wgs * 8);
-  const size_t o_delta = a.take(grad ? M * ld_delta * sizeof(T) : 0);
-  const size_t o_dx = a.take(pieces > 1 && c.dx ? M * up(K, 4) * 4 : 0);
-  const size_t o_sums = a.take(grad ? std::max(c.dx ? sums_bytes(sx, M, K) : 0, c.dw ? sums_bytes(sw, piece, K) : 0) : 0);
-  int e = reserve(h, a.bytes);
-  if (e) return e;
-  uint32_t *count = at<uint32_t>(h, o_count), *rows = at<uint32_t>(h, o_rows), *target = at<uint32_t>(h, o_target);
-  float *alpha = at<float>(h, o_alpha), *score = at<float>(h, o_score), *lse = at<float>(h, o_lse);
-
-  KeepRowsArgs kr{c.targets, c.target_bytes == 8, c.ignore, (uint32_t)M, (uint32_t)V, rows, target, count, h->d_bad};
-  if ((e = launch<KeepRows>(h->stream, 1, KeepRows::kLdsBytes, kr))) return e;
-  if (M && (c.row_loss || c.row_lse || (c.dx && K))) {
-    const BlankRowsArgs br{kr, c.dx, c.ld_dx * sizeof(T), K * sizeof(T), c.row_loss, c.row_lse};
-    if ((e = launch<BlankRows>(h->stream, blocks(M, 4), 0, br))) return e;
-  }
-  GemmArgs g = operands(c.x, c.ldx, M, K, c.w, c.ldw, V, K);
-  g.M = (uint32_t)M; g.N = (uint32_t)V; g.K = (uint32_t)K;
-  g.rows = rows; g.count = count; g.gather = kGatherA; g.count_of = kCountM;
-  g.stats = at<float>(h, o_stats); g.ld_stats = ld_stats; g.target = target; g.target_score = score; g.lse = lse;
-  g.delta_scale = delta_scale<T>();
-  if (M) {
-    if ((e = gemm<T, kAlongK, kAlongK, kEpiStats>(h, g, ss))) return e;
-    const RowStatsArgs rs{g.stats, ld_stats, (uint32_t)tiles, (uint32_t)M, count, rows, score, lse, at<double>(h, o_part), c.row_loss, c.row_lse};
-    if ((e = launch<RowStats>(h->stream, row_wgs, RowStats::kLdsBytes, rs))) return e;
-  }
-  const MeanLossArgs ml{at<double>(h, o_part), (uint32_t)row_wgs, count, c.loss, grad ? alpha : nullptr, c.scale / delta_scale<T>()};
-  if ((e = launch<MeanLoss>(h->stream, 1, MeanLoss::kLdsBytes, ml))) return e;
-
-  for (size_t p = 0; p < pieces; ++p) {
-    const size_t v0 = p * piece, n = std::min(piece, V - v0);
-    const char* wp = static_cast<const char*>(c.w) + v0 * c.ldw * sizeof(T);
-    void* delta = at<void>(h, o_delta);
-    if (M) {
-      GemmArgs d = g;
-      d.b = wp; d.b_extent = (n - 1) * c.ldw + K;
-      d.N = (uint32_t)n; d.n_offset = (uint32_t)v0;
-      d.out = delta; d.ld_out = ld_delta;
-      if ((e = gemm<T, kAlongK, kAlongK, kEpiDelta>(h, d, choose<T>(h, M, n, K, false)))) return e;
-    }
-    if (c.dx && M && K) {
-      GemmArgs d = operands(delta, ld_delta, M, n, wp, c.ldw, n, K);
-      d.M = (uint32_t)M; d.N = (uint32_t)K; d.K = (uint32_t)n;
-      d.rows = rows; d.count = count; d.count_of = kCountM;
-      if (p) { d.addend = at<float>(h, o_dx); d.ld_sums = up(K, 4); }
-      if (p + 1 < pieces) {
-        d.sums = at<float>(h, o_dx); d.ld_sums = up(K, 4);
-        if ((e = gemm<T, kAlongK, kAcrossK, kEpiSums>(h, d, sx))) return e;
-      } else {
-        d.gather = kScatterOut; d.alpha = alpha;
-        d.out = c.dx; d.ld_out = c.ld_dx;
-        if ((e = product<T, kAlongK, kAcrossK>(h, d, sx, at<float>(h, o_sums)))) return e;
-      }
-    }
-    if (c.dw && K) {
-      GemmArgs d = operands(delta, ld_delta, M, n, c.x, c.ldx, M, K);
-      d.M = (uint32_t)n; d.N = (uint32_t)K; d.K = (uint32_t)M;
-      d.rows = rows; d.count = count; d.count_of = kCountK; d.gather = kGatherB; d.alpha = alpha;
-      d.out = static_cast<char*>(c.dw) + v0 * c.ld_dw * sizeof(T); d.ld_out = c.ld_dw;
-      Shape s = sw;
-      if ((e = product<T, kAcrossK, kAcrossK>(h, d, s, at<float>(h, o_sums)))) return e;
-    }
-  }
-  return 0;
-}
 
 // The call of the operator for its number type.
 #define PLAIN_BY_TYPE(dtype, fn, ...) \

@@ -324,6 +324,62 @@ struct GemmOperand {
       *reinterpret_cast<U4*>(lds + place(c / kRowPieces, c % kRowPieces)) = r[i];
     }
   }
+  // ---- memory to LDS without registers: whole stages of operands whose stored rows all start on 16 bytes.  The LDS side of such a load
+  // is fixed (a wave writes 64 x 16 bytes in a row), so that the order of the pieces within a stored row is made on the memory side.
+  static constexpr bool kEvenWaves = kPieces % 64 == 0;
+  HCNN_HD static uint32_t numbers(uint32_t c) {                                 // of a row at LDS piece c, from the stage's first number
+    const uint32_t line = c / kRowPieces, pc = c % kRowPieces;
+    if constexpr (LAYOUT == kAlongK) return (pc ^ (line & 7)) * kPer16;
+    else if constexpr (sizeof(T) == 2) return ((pc / 2 ^ swap(line)) * 2 + pc % 2) * kPer16;
+    else return ((pc / 4 ^ swap(line)) * 4 + pc % 4) * kPer16;
+  }
+  // Byte offsets of a thread's pieces from direct_base, for the whole sum (kAcrossK with gathered rows: of the numbers within the row).
+  // Rows beyond X read a row that exists, pieces beyond X the row's first one.
+  HCNN_HD static void direct_offsets(size_t ld, uint32_t X, const uint32_t* rows, uint32_t x0, int tid, uint32_t (&off)[kEach]) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (!mine(tid, i)) continue;
+      const uint32_t c = (uint32_t)(tid + i * THREADS), line = c / kRowPieces, at = numbers(c);
+      if constexpr (LAYOUT == kAlongK) {
+        const uint32_t x = x0 + line < X ? x0 + line : X - 1;
+        off[i] = (uint32_t)(((rows ? (size_t)rows[x] : (size_t)(x - x0)) * ld + at) * sizeof(T));
+      } else {
+        const uint32_t in_row = x0 + at < X ? at : 0;
+        off[i] = (uint32_t)(((rows ? 0 : line * ld) + in_row) * sizeof(T));
+      }
+    }
+  }
+  HCNN_HD static const T* direct_base(const T* p, size_t ld, const uint32_t* rows, uint32_t x0, uint32_t k0) {
+    if constexpr (LAYOUT == kAlongK) return p + (rows ? 0 : x0 * ld) + k0;
+    else return p + (rows ? 0 : k0 * ld) + x0;
+  }
+  // May the stage at k0 be read whole?  Its k exist, and a last piece that reaches beyond the row's numbers reads memory of the operand.
+  HCNN_HD static bool direct_stage(size_t ld, size_t extent, uint32_t X, uint32_t K, const uint32_t* rows, uint32_t k0) {
+    if (k0 + kStage > K) return false;
+    if constexpr (LAYOUT == kAlongK) return true;
+    if (X % kPer16 == 0) return true;
+    const size_t last = rows ? wave_uniform(rows[k0 + kStage - 1]) : k0 + kStage - 1;      // (gathered rows ascend)
+    return last * ld + X / kPer16 * kPer16 + kPer16 <= extent;
+  }
+  HCNN_HD static void direct(const T* base, size_t ld, const uint32_t* rows, uint32_t k0, char* lds, int tid, const uint32_t (&off)[kEach]) {
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      if (!mine(tid, i)) continue;
+      uint32_t o = off[i];
+      if (LAYOUT == kAcrossK && rows) o += (uint32_t)(rows[k0 + (tid + i * THREADS) / kRowPieces] * ld * sizeof(T));
+      to_lds(base, o, lds + ((tid & ~63) + i * THREADS) * 16, tid & 63);
+    }
+  }
+  // 16 bytes of every lane of a wave to LDS, side by side
+  HCNN_HD static void to_lds(const T* base, uint32_t off, char* lds, int lane) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    const uint32_t at = wave_uniform((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds);
+    // (as an instruction of its own: of the builtin the compiler only knows that it writes LDS, and has every later LDS read wait for it)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(base) : "memory");
+#else
+    __builtin_memcpy(lds + lane * 16, reinterpret_cast<const char*>(base) + off, 16);
+#endif
+  }
   // 16 bytes of row `base + lane % 16`, step s (of two 64-byte steps) of the stage; base a multiple of 16
 #if defined(__HIP_DEVICE_COMPILE__)
   __device__ __forceinline__ static hcnn_word4 read(const char* lds, uint32_t base, uint32_t s, uint32_t lane) {
@@ -381,7 +437,14 @@ struct hcnn_float4 {
 };
 #endif
 
-template <class T, int LA, int LB, int BM, int BN, int WM, int WN, int EPI>
+// What is on its way to LDS past the registers has arrived
+HCNN_HD void direct_done() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+#endif
+}
+
+template <class T, int LA, int LB, int BM, int BN, int WM, int WN, int EPI, bool DIRECT>
 struct Gemm {
   static constexpr int kThreads = WM * WN * 64;
   static constexpr int kLoopPhases = 1;
@@ -398,7 +461,8 @@ struct Gemm {
   struct Regs {
     uint32_t iter;
     uint32_t m0, n0, k_begin, k_end, M, split;
-    U4 ra[A::kEach], rb[B::kEach];
+    U4 ra[A::kEach], rb[B::kEach];               // the next stage, unless DIRECT
+    uint32_t oa[A::kEach], ob[B::kEach];         // DIRECT: offsets of the pieces
     hcnn_float4 acc[FM][FN];
   };
 
@@ -443,16 +507,36 @@ struct Gemm {
     A::store(lds, tid, r.ra);
     B::store(lds + A::kLdsBytes, tid, r.rb);
   }
+  // The stage at k0 to LDS: past the registers where it may be read whole
+  HCNN_HD static void bring(const GemmArgs& a, uint32_t k0, char* lds, int tid, Regs& r) {
+    const uint32_t *ga = a.gather & kGatherA ? a.rows : nullptr, *gb = a.gather & kGatherB ? a.rows : nullptr;
+    if (A::direct_stage(a.lda, a.a_extent, r.M, r.k_end, ga, k0) && B::direct_stage(a.ldb, a.b_extent, a.N, r.k_end, gb, k0)) {
+      A::direct(A::direct_base(static_cast<const T*>(a.a), a.lda, ga, r.m0, k0), a.lda, ga, k0, lds, tid, r.oa);
+      B::direct(B::direct_base(static_cast<const T*>(a.b), a.ldb, gb, r.n0, k0), a.ldb, gb, k0, lds + A::kLdsBytes, tid, r.ob);
+    } else {
+      fetch(a, k0, tid, r);
+      keep(lds, tid, r);
+    }
+  }
   HCNN_HD static void begin(const GemmArgs& a, unsigned bid, int tid, uint32_t* lds, Regs& r) {
     place(a, bid, r);
+    if constexpr (DIRECT) {
+      A::direct_offsets(a.lda, r.M, a.gather & kGatherA ? a.rows : nullptr, r.m0, tid, r.oa);
+      B::direct_offsets(a.ldb, a.N, a.gather & kGatherB ? a.rows : nullptr, r.n0, tid, r.ob);
+    }
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
       for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) r.acc[i][j][e] = 0.0f;
-    fetch(a, r.k_begin, tid, r);
-    keep(reinterpret_cast<char*>(lds), tid, r);
+    if constexpr (DIRECT) {
+      bring(a, r.k_begin, reinterpret_cast<char*>(lds), tid, r);
+      direct_done();
+    } else {
+      fetch(a, r.k_begin, tid, r);
+      keep(reinterpret_cast<char*>(lds), tid, r);
+    }
   }
   HCNN_HD static void multiply(const char* lds, int tid, Regs& r) {
     const uint32_t wave = (uint32_t)tid / 64, lane = (uint32_t)tid % 64;
@@ -488,9 +572,15 @@ struct Gemm {
     if constexpr (PH == 0) {
       const uint32_t k_next = r.k_begin + (r.iter + 1) * kStage;
       const bool more = k_next < r.k_end;
-      if (more) fetch(a, k_next, tid, r);
-      if (r.k_begin + r.iter * kStage < r.k_end) multiply(lds + r.iter % 2 * kBuffer, tid, r);
-      if (more) keep(lds + (r.iter + 1) % 2 * kBuffer, tid, r);
+      if constexpr (DIRECT) {
+        if (more) bring(a, k_next, lds + (r.iter + 1) % 2 * kBuffer, tid, r);
+        if (r.k_begin + r.iter * kStage < r.k_end) multiply(lds + r.iter % 2 * kBuffer, tid, r);
+        direct_done();
+      } else {
+        if (more) fetch(a, k_next, tid, r);
+        if (r.k_begin + r.iter * kStage < r.k_end) multiply(lds + r.iter % 2 * kBuffer, tid, r);
+        if (more) keep(lds + (r.iter + 1) % 2 * kBuffer, tid, r);
+      }
     } else if constexpr (EPI == kEpiOut || EPI == kEpiSums) {
 #pragma unroll
       for (int i = 0; i < FM; ++i) {
