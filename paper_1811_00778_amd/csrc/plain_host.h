@@ -79,7 +79,7 @@ Shape choose(const hcnn_plain* h, size_t M, size_t N, size_t K, bool may_split) 
   }
   return s;
 }
-inline size_t sums_bytes(const Shape& s, size_t M, size_t N) { return s.splits > 1 ? s.splits * M * up(N, 4) * 4 : 0; }
+inline size_t sums_bytes(const Shape& s, size_t M, size_t N) { return s.splits > 1 ? s.splits * M * up(N, 8) * 4 : 0; }
 
 template <class G>
 int start(hcnn_plain* h, const GemmArgs& a, size_t grid) { return launch<G>(h->stream, grid, G::kLdsBytes, a); }
@@ -118,7 +118,7 @@ int product(hcnn_plain* h, GemmArgs a, const Shape& s, float* sums) {
   a.splits = s.splits;
   if (s.splits == 1) return gemm<T, LA, LB, kEpiOut>(h, a, s);
   a.sums = sums;
-  a.ld_sums = up(a.N, 4);
+  a.ld_sums = up(a.N, 8);
   const int e = gemm<T, LA, LB, kEpiSums>(h, a, s);
   return e ? e : launch<GemmJoin<T>>(h->stream, GemmJoin<T>::grid(a), 0, a);
 }
@@ -233,7 +233,7 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
   const size_t o_count = a.take(4), o_alpha = a.take(4), o_rows = a.take(M * 4), o_target = a.take(M * 4), o_score = a.take(M * 4), o_lse = a.take(M * 4);
   const size_t o_stats = a.take(tiles * 2 * ld_stats * 4), o_part = a.take(row_wgs * 8);
   const size_t o_delta = a.take(grad ? M * ld_delta * sizeof(T) : 0);
-  const size_t o_dx = a.take(pieces > 1 && c.dx ? M * up(K, 4) * 4 : 0);
+  const size_t o_dx = a.take(pieces > 1 && c.dx ? M * up(K, 8) * 4 : 0);
   const size_t o_sums = a.take(grad ? std::max(c.dx ? sums_bytes(sx, M, K) : 0, c.dw ? sums_bytes(sw, piece, K) : 0) : 0);
   int e = reserve(h, a.bytes);
   if (e) return e;
@@ -274,9 +274,9 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
       GemmArgs d = operands(delta, ld_delta, M, n, wp, c.ldw, n, K);
       d.M = (uint32_t)M; d.N = (uint32_t)K; d.K = (uint32_t)n;
       d.rows = rows; d.count = count; d.count_of = kCountM;
-      if (p) { d.addend = at<float>(h, o_dx); d.ld_sums = up(K, 4); }
+      if (p) { d.addend = at<float>(h, o_dx); d.ld_sums = up(K, 8); }
       if (p + 1 < pieces) {
-        d.sums = at<float>(h, o_dx); d.ld_sums = up(K, 4);
+        d.sums = at<float>(h, o_dx); d.ld_sums = up(K, 8);
         if ((e = gemm<T, kAlongK, kAcrossK, kEpiSums>(h, d, sx))) return e;
       } else {
         d.gather = kScatterOut; d.alpha = alpha;

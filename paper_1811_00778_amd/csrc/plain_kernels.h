@@ -94,47 +94,53 @@ HCNN_HD uint64_t ld8(const char* p) { uint64_t v; __builtin_memcpy(&v, p, 8); re
 HCNN_HD void st8(char* p, uint64_t v) { __builtin_memcpy(p, &v, 8); }
 #endif
 
-// Four numbers in a row, widened
-template <class T>
-HCNN_HD void load4(const T* p, float (&v)[4]) {
-  T t[4];
-  if constexpr (sizeof(T) == 4) {
-    const U4 w = ld16(reinterpret_cast<const char*>(p));
-    __builtin_memcpy(t, &w, 16);
-  } else {
+// W numbers in a row (4 or 8), widened
+template <class T, int W>
+HCNN_HD void load_row(const T* p, float (&v)[W]) {
+  T t[W];
+  if constexpr (W * sizeof(T) == 8) {
     const uint64_t w = ld8(reinterpret_cast<const char*>(p));
     __builtin_memcpy(t, &w, 8);
+  } else {
+#pragma unroll
+    for (size_t i = 0; i < W * sizeof(T); i += 16) {
+      const U4 w = ld16(reinterpret_cast<const char*>(p) + i);
+      __builtin_memcpy(reinterpret_cast<char*>(t) + i, &w, 16);
+    }
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = Num<T>::widen(t[i]);
+  for (int i = 0; i < W; ++i) v[i] = Num<T>::widen(t[i]);
 }
-template <class T>
-HCNN_HD void store4(T* p, const float (&v)[4]) {
-  T t[4];
+template <class T, int W>
+HCNN_HD void store_row(T* p, const float (&v)[W]) {
+  T t[W];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) t[i] = Num<T>::narrow(v[i]);
-  if constexpr (sizeof(T) == 4) {
-    U4 w;
-    __builtin_memcpy(&w, t, 16);
-    st16(reinterpret_cast<char*>(p), w);
-  } else {
+  for (int i = 0; i < W; ++i) t[i] = Num<T>::narrow(v[i]);
+  if constexpr (W * sizeof(T) == 8) {
     uint64_t w;
     __builtin_memcpy(&w, t, 8);
     st8(reinterpret_cast<char*>(p), w);
+  } else {
+#pragma unroll
+    for (size_t i = 0; i < W * sizeof(T); i += 16) {
+      U4 w;
+      __builtin_memcpy(&w, reinterpret_cast<char*>(t) + i, 16);
+      st16(reinterpret_cast<char*>(p) + i, w);
+    }
   }
 }
 // ... of which only the first `left` exist
-template <class T>
-HCNN_HD void load4(const T* p, uint32_t left, float (&v)[4]) {
-  if (left >= 4) return load4(p, v);
+template <class T, int W>
+HCNN_HD void load_row(const T* p, uint32_t left, float (&v)[W]) {
+  if (left >= W) return load_row(p, v);
 #pragma unroll
-  for (uint32_t i = 0; i < 4; ++i) v[i] = i < left ? Num<T>::widen(p[i]) : 0.0f;
+  for (uint32_t i = 0; i < W; ++i) v[i] = i < left ? Num<T>::widen(p[i]) : 0.0f;
 }
-template <class T>
-HCNN_HD void store4(T* p, uint32_t left, const float (&v)[4]) {
-  if (left >= 4) return store4(p, v);
+template <class T, int W>
+HCNN_HD void store_row(T* p, uint32_t left, const float (&v)[W]) {
+  if (left >= W) return store_row(p, v);
 #pragma unroll
-  for (uint32_t i = 0; i < 4; ++i)
+  for (uint32_t i = 0; i < W; ++i)
     if (i < left) p[i] = Num<T>::narrow(v[i]);
 }
 
@@ -148,6 +154,20 @@ HCNN_HD float act_of(float z, int act) {
     case kActSilu: return z / (1.0f + exp_of(-z));
   }
   return z;
+}
+template <int W>
+HCNN_HD void act_all(float (&v)[W], int act) {
+  switch (act) {
+#define PLAIN_ACT(A)                    \
+  case A:                               \
+    _Pragma("unroll") for (int i = 0; i < W; ++i) v[i] = act_of(v[i], A); \
+    break
+    PLAIN_ACT(kActSquare);
+    PLAIN_ACT(kActRelu);
+    PLAIN_ACT(kActGelu);
+    PLAIN_ACT(kActSilu);
+#undef PLAIN_ACT
+  }
 }
 HCNN_HD float slope_of(float z, int act) {
   switch (act) {
@@ -190,7 +210,7 @@ struct GemmArgs {
   uint32_t splits;             // parts of k, each summed by workgroups of its own
   // what becomes of the sums
   float* sums;                 // [splits][M][ld_sums] where kEpiSums
-  size_t ld_sums;              // a multiple of 4
+  size_t ld_sums;              // a multiple of 8
   const float* addend;         // [M][ld_sums], added to the sums of the first part (may be null; may be `sums`)
   const float* alpha;          // device factor of the sums (may be null)
   int act;
@@ -208,34 +228,23 @@ struct GemmArgs {
   uint32_t n_offset;           // class of column 0
 };
 
-// What the linear layer makes of four sums in a row of its output.
-template <class T>
-HCNN_HD void finish4(const GemmArgs& a, uint32_t m, uint32_t n, float (&v)[4]) {
-  if (n >= a.N) return;
+// What the linear layer makes of W sums in a row of its output; `bias`: of these columns, 0 where there is none.
+template <class T, int W>
+HCNN_HD void finish(const GemmArgs& a, uint32_t m, uint32_t n, const float (&bias)[W], float (&v)[W]) {
   const uint32_t left = a.N - n;
-  if (a.alpha) {
+  const float alpha = a.alpha ? *a.alpha : 1.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] *= *a.alpha;
-  }
-  if (a.bias) {
-    float b[4];
-    load4(static_cast<const T*>(a.bias) + n, left, b);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += b[i];
-  }
+  for (int i = 0; i < W; ++i) v[i] = v[i] * alpha + bias[i];
   const size_t row = a.gather & kScatterOut ? a.rows[m] : m;
-  if (a.z) store4(static_cast<T*>(a.z) + row * a.ld_z + n, left, v);
-  if (a.act != kActNone) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = act_of(v[i], a.act);
-  }
+  if (a.z) store_row(static_cast<T*>(a.z) + row * a.ld_z + n, left, v);
+  act_all(v, a.act);
   if (a.residual) {
-    float r[4];
-    load4(static_cast<const T*>(a.residual) + row * a.ld_residual + n, left, r);
+    float r[W];
+    load_row(static_cast<const T*>(a.residual) + row * a.ld_residual + n, left, r);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += r[i];
+    for (int i = 0; i < W; ++i) v[i] += r[i];
   }
-  store4(static_cast<T*>(a.out) + row * a.ld_out + n, left, v);
+  store_row(static_cast<T*>(a.out) + row * a.ld_out + n, left, v);
 }
 
 enum { kEpiOut = 0, kEpiSums = 1, kEpiStats = 2, kEpiDelta = 3 };
@@ -448,7 +457,9 @@ template <class T, int LA, int LB, int BM, int BN, int WM, int WN, int EPI, bool
 struct Gemm {
   static constexpr int kThreads = WM * WN * 64;
   static constexpr int kLoopPhases = 1;
-  static constexpr int kPhases = EPI == kEpiStats ? 3 : 2;
+  // the sums leave through LDS, as many rows at a time as the stages' memory holds
+  static constexpr int kParts = BM * BN * 4 > 2 * (BM + BN) * 128 ? 2 : 1;
+  static constexpr int kPhases = EPI == kEpiStats ? 3 : 1 + 2 * kParts;
   static constexpr int kMinWavesPerSimd = 2;
   static constexpr uint32_t kStage = GemmNum<T>::kStage;
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
@@ -457,6 +468,7 @@ struct Gemm {
   static constexpr uint32_t kBuffer = A::kLdsBytes + B::kLdsBytes;
   static constexpr size_t kLdsBytes = 2 * kBuffer;
   static_assert(EPI != kEpiStats || BM * WN * 4 * 8 <= 2 * kBuffer, "the statistics fit the stages' memory");
+  static_assert(BM / kParts * BN * 4 <= 2 * kBuffer && WM % kParts == 0, "a part's sums fit the stages' memory");
 
   struct Regs {
     uint32_t iter;
@@ -581,26 +593,54 @@ struct Gemm {
         if (r.k_begin + r.iter * kStage < r.k_end) multiply(lds + r.iter % 2 * kBuffer, tid, r);
         if (more) keep(lds + (r.iter + 1) % 2 * kBuffer, tid, r);
       }
-    } else if constexpr (EPI == kEpiOut || EPI == kEpiSums) {
+    } else if constexpr (EPI != kEpiStats) {
+      constexpr uint32_t kPart = (PH - 1) / 2, kRows = BM / kParts, kQuads = BN / 4;
+      if constexpr (PH % 2 == 1) {
+        if (wave / WN / (WM / kParts) != kPart) return;
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        const uint32_t m = r.m0 + m_lane + i * 16;
-        if (m >= r.M) continue;
+        for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          const uint32_t n = r.n0 + n_lane + j * 16;
-          if (n >= a.N) continue;
-          float v[4];
+          for (int j = 0; j < FN; ++j) {
+            const uint32_t m = m_lane + i * 16 - kPart * kRows;
+            float v[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) v[e] = r.acc[i][j][e];
-          if (a.addend && r.split == 0) {
-            float old[4];
-            load4(a.addend + (size_t)m * a.ld_sums + n, old);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] += old[e];
+            for (int e = 0; e < 4; ++e) v[e] = r.acc[i][j][e];
+            __builtin_memcpy(lds + (m * kQuads + quad_at(m, n_lane / 4 + j * 4)) * 16, v, 16);
           }
-          if constexpr (EPI == kEpiOut) finish4<T>(a, m, n, v);
-          else store4(a.sums + ((size_t)r.split * a.M + m) * a.ld_sums + n, v);
+      } else {
+        // a thread keeps its columns and goes down the rows
+        constexpr uint32_t W = sizeof(T) == 2 && kQuads % 2 == 0 ? 8 : 4, kAcross = BN / W;
+        static_assert(kThreads % kAcross == 0, "whole rows");
+        const uint32_t c = (uint32_t)tid % kAcross, n = r.n0 + c * W;
+        if (n >= a.N) return;
+        const uint32_t left = a.N - n;
+        float bias[W] = {};
+        if (EPI == kEpiOut && a.bias) load_row(static_cast<const T*>(a.bias) + n, left, bias);
+#pragma unroll 2
+        for (uint32_t line = (uint32_t)tid / kAcross; line < kRows; line += kThreads / kAcross) {
+          const uint32_t m = r.m0 + kPart * kRows + line;
+          if (m >= r.M) break;
+          float v[W];
+#pragma unroll
+          for (uint32_t q = 0; q < W / 4; ++q) __builtin_memcpy(v + q * 4, lds + (line * kQuads + quad_at(line, c * (W / 4) + q)) * 16, 16);
+          if constexpr (EPI == kEpiDelta) {
+            // the gradient of the row's loss for its scores, times delta_scale: an operand of the two products after this, so that
+            // it is rounded to their type here
+            const float lse = a.lse[m];
+            const uint32_t t = a.target[m] - a.n_offset;
+#pragma unroll
+            for (uint32_t e = 0; e < W; ++e) v[e] = (exp_of(v[e] - lse) - (n + e == t ? 1.0f : 0.0f)) * a.delta_scale;
+            store_row(static_cast<T*>(a.out) + (size_t)m * a.ld_out + n, left, v);
+          } else {
+            if (a.addend && r.split == 0) {
+              float old[W];
+              load_row(a.addend + (size_t)m * a.ld_sums + n, old);
+#pragma unroll
+              for (uint32_t e = 0; e < W; ++e) v[e] += old[e];
+            }
+            if constexpr (EPI == kEpiOut) finish<T>(a, m, n, bias, v);
+            else store_row(a.sums + ((size_t)r.split * a.M + m) * a.ld_sums + n, v);
+          }
         }
       }
     } else if constexpr (EPI == kEpiStats) {
@@ -640,26 +680,12 @@ struct Gemm {
         to[0] = top;
         to[a.ld_stats] = sum;
       }
-    } else {
-      // the gradient of the row's loss for its scores, times delta_scale: what the two products after this take as an operand,
-      // so that it is rounded to their type here
-#pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        const uint32_t m = r.m0 + m_lane + i * 16;
-        if (m >= r.M) continue;
-        const float lse = a.lse[m];
-        const uint32_t t = a.target[m] - a.n_offset;
-#pragma unroll
-        for (int j = 0; j < FN; ++j) {
-          const uint32_t n = r.n0 + n_lane + j * 16;
-          if (n >= a.N) continue;
-          float v[4];
-#pragma unroll
-          for (uint32_t e = 0; e < 4; ++e) v[e] = (exp_of(r.acc[i][j][e] - lse) - (n + e == t ? 1.0f : 0.0f)) * a.delta_scale;
-          store4(static_cast<T*>(a.out) + (size_t)m * a.ld_out + n, a.N - n, v);
-        }
-      }
     }
+  }
+  // 16 bytes of sums in LDS: the rows that a wave writes at once go to different banks
+  HCNN_HD static uint32_t quad_at(uint32_t m, uint32_t quad) {
+    constexpr uint32_t kQuads = BN / 4;
+    return kQuads >= 16 ? quad ^ (m & 15) : quad ^ (m / (16 / kQuads) & (kQuads - 1));
   }
 };
 
@@ -681,11 +707,13 @@ struct GemmJoin {
     float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     for (uint32_t s = 0; s < a.splits; ++s) {
       float x[4];
-      load4(a.sums + ((size_t)s * a.M + m) * a.ld_sums + n, x);
+      load_row(a.sums + ((size_t)s * a.M + m) * a.ld_sums + n, x);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] += x[e];
     }
-    finish4<T>(a, (uint32_t)m, n, v);
+    float bias[4] = {};
+    if (a.bias) load_row(static_cast<const T*>(a.bias) + n, a.N - n, bias);
+    finish<T>(a, (uint32_t)m, n, bias, v);
   }
 };
 
@@ -721,13 +749,13 @@ struct ActGrad {
 #pragma unroll 4
         for (uint32_t m = m0 + line; m < m1; m += kLines) {
           float v[4];
-          load4(static_cast<const T*>(a.dy) + m * a.ld_dy + n, left, v);
+          load_row(static_cast<const T*>(a.dy) + m * a.ld_dy + n, left, v);
           if (a.z) {
             float z[4];
-            load4(static_cast<const T*>(a.z) + m * a.ld_z + n, left, z);
+            load_row(static_cast<const T*>(a.z) + m * a.ld_z + n, left, z);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] *= slope_of(z[e], a.act);
-            store4(static_cast<T*>(a.dz) + m * a.ld_dz + n, left, v);
+            store_row(static_cast<T*>(a.dz) + m * a.ld_dz + n, left, v);
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum[e] += v[e];
