@@ -293,10 +293,13 @@ struct GemmOperand {
   HCNN_HD static void load(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, const uint32_t* rows, uint32_t x0, uint32_t k0,
                            int tid, U4 (&r)[kEach]) {
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      if (!mine(tid, i)) continue;
-      const uint32_t c = (uint32_t)(tid + i * THREADS), line = c / kRowPieces, at = c % kRowPieces * kPer16;
-      U4 v{};
+    for (int i = 0; i < kEach; ++i)
+      if (mine(tid, i)) r[i] = load_one(p, ld, extent, X, K, rows, x0, k0, (uint32_t)(tid + i * THREADS));
+  }
+  HCNN_HD static U4 load_one(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, const uint32_t* rows, uint32_t x0, uint32_t k0, uint32_t c) {
+    const uint32_t line = c / kRowPieces, at = c % kRowPieces * kPer16;
+    U4 v{};
+    {
       if constexpr (LAYOUT == kAlongK) {
         uint32_t x = x0 + line;
         if (x >= X) x = X - 1;
@@ -313,8 +316,14 @@ struct GemmOperand {
           v = piece(p, row * ld + x, extent);
         }
       }
-      r[i] = v;
     }
+    return v;
+  }
+  // ... straight to LDS, one piece after the other: for the one stage of a sum that is not whole, where registers are dear
+  HCNN_HD static void copy(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, const uint32_t* rows, uint32_t x0, uint32_t k0, char* lds, int tid) {
+#pragma unroll 1
+    for (uint32_t c = (uint32_t)tid; c < (uint32_t)kPieces; c += THREADS)
+      *reinterpret_cast<U4*>(lds + place(c / kRowPieces, c % kRowPieces)) = load_one(p, ld, extent, X, K, rows, x0, k0, c);
   }
   HCNN_HD static uint32_t place(uint32_t line, uint32_t pc) {                  // byte of piece pc of stored row `line`
     if constexpr (LAYOUT == kAlongK) return line * 128 + ((pc ^ (line & 7)) << 4);
@@ -446,6 +455,12 @@ struct hcnn_float4 {
 };
 #endif
 
+// All waves of the workgroup, inside a phase that the checker runs thread by thread: only in front of what it does not do
+HCNN_HD void block_barrier() {
+#if defined(__HIP_DEVICE_COMPILE__)
+  __syncthreads();
+#endif
+}
 // What is on its way to LDS past the registers has arrived
 HCNN_HD void direct_done() {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -456,10 +471,10 @@ HCNN_HD void direct_done() {
 template <class T, int LA, int LB, int BM, int BN, int WM, int WN, int EPI, bool DIRECT>
 struct Gemm {
   static constexpr int kThreads = WM * WN * 64;
-  static constexpr int kLoopPhases = 1;
+  static constexpr int kLoopPhases = 2;
   // the sums leave through LDS, as many rows at a time as the stages' memory holds
   static constexpr int kParts = BM * BN * 4 > 2 * (BM + BN) * 128 ? 2 : 1;
-  static constexpr int kPhases = EPI == kEpiStats ? 3 : 1 + 2 * kParts;
+  static constexpr int kPhases = EPI == kEpiStats ? 4 : 2 + 2 * kParts;
   static constexpr int kMinWavesPerSimd = 2;
   static constexpr uint32_t kStage = GemmNum<T>::kStage;
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
@@ -470,11 +485,18 @@ struct Gemm {
   static_assert(EPI != kEpiStats || BM * WN * 4 * 8 <= 2 * kBuffer, "the statistics fit the stages' memory");
   static_assert(BM / kParts * BN * 4 <= 2 * kBuffer && WM % kParts == 0, "a part's sums fit the stages' memory");
 
+  // Operands of the running 64-byte step; b's of the next one beside them, a's take their place as soon as a row's products are under way.
+#if defined(__HIP_DEVICE_COMPILE__)
+  struct Step { hcnn_word4 a[FM], b[2][FN]; };
+#else
+  struct Step {};
+#endif
   struct Regs {
     uint32_t iter;
     uint32_t m0, n0, k_begin, k_end, M, split;
     U4 ra[A::kEach], rb[B::kEach];               // the next stage, unless DIRECT
     uint32_t oa[A::kEach], ob[B::kEach];         // DIRECT: offsets of the pieces
+    Step step;
     hcnn_float4 acc[FM][FN];
   };
 
@@ -526,8 +548,8 @@ struct Gemm {
       A::direct(A::direct_base(static_cast<const T*>(a.a), a.lda, ga, r.m0, k0), a.lda, ga, k0, lds, tid, r.oa);
       B::direct(B::direct_base(static_cast<const T*>(a.b), a.ldb, gb, r.n0, k0), a.ldb, gb, k0, lds + A::kLdsBytes, tid, r.ob);
     } else {
-      fetch(a, k0, tid, r);
-      keep(lds, tid, r);
+      A::copy(static_cast<const T*>(a.a), a.lda, a.a_extent, r.M, r.k_end, ga, r.m0, k0, lds, tid);
+      B::copy(static_cast<const T*>(a.b), a.ldb, a.b_extent, a.N, r.k_end, gb, r.n0, k0, lds + A::kLdsBytes, tid);
     }
   }
   HCNN_HD static void begin(const GemmArgs& a, unsigned bid, int tid, uint32_t* lds, Regs& r) {
@@ -542,60 +564,79 @@ struct Gemm {
       for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int e = 0; e < 4; ++e) r.acc[i][j][e] = 0.0f;
+    char* l = reinterpret_cast<char*>(lds);
     if constexpr (DIRECT) {
-      bring(a, r.k_begin, reinterpret_cast<char*>(lds), tid, r);
+      bring(a, r.k_begin, l, tid, r);
       direct_done();
     } else {
       fetch(a, r.k_begin, tid, r);
-      keep(reinterpret_cast<char*>(lds), tid, r);
+      keep(l, tid, r);
     }
-  }
-  HCNN_HD static void multiply(const char* lds, int tid, Regs& r) {
-    const uint32_t wave = (uint32_t)tid / 64, lane = (uint32_t)tid % 64;
-    const uint32_t mw = wave / WN * (FM * 16), nw = wave % WN * (FN * 16);
-    const char* lb = lds + A::kLdsBytes;
+    block_barrier();
+    if (r.k_begin + kStage < r.k_end) {
+      if constexpr (DIRECT) bring(a, r.k_begin + kStage, l + kBuffer, tid, r);
+      else fetch(a, r.k_begin + kStage, tid, r);
+    }
 #if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
-    for (uint32_t s = 0; s < 2; ++s) {
-      hcnn_word4 fb[FN], fa[FM];
+    for (int i = 0; i < FM; ++i) r.step.a[i] = A::read(l, m_wave(tid) + i * 16, 0, tid % 64);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) fb[j] = B::read(lb, nw + j * 16, s, lane);
+    for (int j = 0; j < FN; ++j) r.step.b[0][j] = B::read(l + A::kLdsBytes, n_wave(tid) + j * 16, 0, tid % 64);
+#endif
+  }
+  HCNN_HD static uint32_t m_wave(int tid) { return (uint32_t)tid / 64 / WN * (FM * 16); }
+  HCNN_HD static uint32_t n_wave(int tid) { return (uint32_t)tid / 64 % WN * (FN * 16); }
+  // The products of step s of a stage, and the operands of the step after it from `lds`: step 1 of the same stage, or step 0 of the next
+  // one behind the barrier that tells that it has arrived.
+  HCNN_HD static void multiply(const char* lds, uint32_t s, int tid, Regs& r) {
+#if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
-      for (int i = 0; i < FM; ++i) fa[i] = A::read(lds, mw + i * 16, s, lane);
+    for (int j = 0; j < FN; ++j) r.step.b[1 - s][j] = B::read(lds + A::kLdsBytes, n_wave(tid) + j * 16, 1 - s, tid % 64);
 #pragma unroll
-      for (int i = 0; i < FM; ++i)
+    for (int i = 0; i < FM; ++i) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) mma<T>(r.acc[i][j], fb[j], fa[i]);
+      for (int j = 0; j < FN; ++j) mma<T>(r.acc[i][j], r.step.b[s][j], r.step.a[i]);
+      r.step.a[i] = A::read(lds, m_wave(tid) + i * 16, 1 - s, tid % 64);
+      sched_fence();
     }
-#else
+#endif
+  }
+  // the checker's products of the whole stage
+  HCNN_HD static void check_multiply(const char* lds, int tid, Regs& r) {
+#if !defined(__HIP_DEVICE_COMPILE__)
+    const uint32_t lane = (uint32_t)tid % 64, mw = m_wave(tid), nw = n_wave(tid);
     for (int i = 0; i < FM; ++i)
       for (int j = 0; j < FN; ++j)
         for (uint32_t e = 0; e < 4; ++e)
           for (uint32_t k = 0; k < kStage; ++k)
-            r.acc[i][j][e] += A::at(lds, mw + i * 16 + lane % 16, k) * B::at(lb, nw + j * 16 + lane / 16 * 4 + e, k);
+            r.acc[i][j][e] += A::at(lds, mw + i * 16 + lane % 16, k) * B::at(lds + A::kLdsBytes, nw + j * 16 + lane / 16 * 4 + e, k);
 #endif
   }
+  static constexpr bool wave_sync(int ph) { return ph == 1; }
 
   template <int PH>
   HCNN_HD static void phase(const GemmArgs& a, unsigned, int tid, uint32_t* lds_words, Regs& r) {
     char* lds = reinterpret_cast<char*>(lds_words);
     const uint32_t wave = (uint32_t)tid / 64, lane = (uint32_t)tid % 64;
     const uint32_t m_lane = wave / WN * (FM * 16) + lane % 16, n_lane = wave % WN * (FN * 16) + lane / 16 * 4;   // in the tile
+    char *here = lds + r.iter % 2 * kBuffer, *next = lds + (r.iter + 1) % 2 * kBuffer;
+    const uint32_t k0 = r.k_begin + r.iter * kStage;
     if constexpr (PH == 0) {
-      const uint32_t k_next = r.k_begin + (r.iter + 1) * kStage;
-      const bool more = k_next < r.k_end;
-      if constexpr (DIRECT) {
-        if (more) bring(a, k_next, lds + (r.iter + 1) % 2 * kBuffer, tid, r);
-        if (r.k_begin + r.iter * kStage < r.k_end) multiply(lds + r.iter % 2 * kBuffer, tid, r);
-        direct_done();
-      } else {
-        if (more) fetch(a, k_next, tid, r);
-        if (r.k_begin + r.iter * kStage < r.k_end) multiply(lds + r.iter % 2 * kBuffer, tid, r);
-        if (more) keep(lds + (r.iter + 1) % 2 * kBuffer, tid, r);
+      if (k0 < r.k_end) {
+        check_multiply(here, tid, r);
+        multiply(here, 0, tid, r);
       }
+      if constexpr (DIRECT) direct_done();
+      else if (k0 + kStage < r.k_end) keep(next, tid, r);
+    } else if constexpr (PH == 1) {
+      if (k0 + 2 * kStage < r.k_end) {
+        if constexpr (DIRECT) bring(a, k0 + 2 * kStage, here, tid, r);
+        else fetch(a, k0 + 2 * kStage, tid, r);
+      }
+      if (k0 < r.k_end) multiply(next, 1, tid, r);
     } else if constexpr (EPI != kEpiStats) {
-      constexpr uint32_t kPart = (PH - 1) / 2, kRows = BM / kParts, kQuads = BN / 4;
-      if constexpr (PH % 2 == 1) {
+      constexpr uint32_t kPart = (PH - 2) / 2, kRows = BM / kParts, kQuads = BN / 4;
+      if constexpr (PH % 2 == 0) {
         if (wave / WN / (WM / kParts) != kPart) return;
 #pragma unroll
         for (int i = 0; i < FM; ++i)
@@ -645,7 +686,7 @@ struct Gemm {
       }
     } else if constexpr (EPI == kEpiStats) {
       float* part = reinterpret_cast<float*>(lds);                 // [2][WN * 4][BM]
-      if constexpr (PH == 1) {
+      if constexpr (PH == 2) {
         // each lane's largest score of a row and the exponentials relative to it; the class's own score has one owner
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
