@@ -428,14 +428,11 @@ struct GemmOperand {
     const size_t last = rows ? wave_uniform(rows[k0 + kStage - 1]) : k0 + kStage - 1;      // (gathered rows ascend)
     return last * ld + X / kPer16 * kPer16 + kPer16 <= extent;
   }
-  HCNN_HD static void direct(const T* base, size_t ld, const uint32_t* rows, uint32_t k0, char* lds, int tid, const uint32_t (&off)[kEach]) {
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      if (!mine(tid, i)) continue;
-      uint32_t o = off[i];
-      if (LAYOUT == kAcrossK && rows) o += (uint32_t)(rows[k0 + (tid + i * THREADS) / kRowPieces] * ld * sizeof(T));
-      to_lds(base, o, lds + ((tid & ~63) + i * THREADS) * 16, tid & 63);
-    }
+  HCNN_HD static void direct(const T* base, size_t ld, const uint32_t* rows, uint32_t k0, char* lds, int tid, int i, const uint32_t (&off)[kEach]) {
+    if (!mine(tid, i)) return;
+    uint32_t o = off[i];
+    if (LAYOUT == kAcrossK && rows) o += (uint32_t)(rows[k0 + (tid + i * THREADS) / kRowPieces] * ld * sizeof(T));
+    to_lds(base, o, lds + ((tid & ~63) + i * THREADS) * 16, tid & 63);
   }
   // 16 bytes of every lane of a wave to LDS, side by side
   HCNN_HD static void to_lds(const T* base, uint32_t off, char* lds, int lane) {
@@ -590,17 +587,36 @@ struct Gemm {
     A::store(lds, tid, r.ra);
     B::store(lds + A::kLdsBytes, tid, r.rb);
   }
-  // The stage at k0 to LDS: past the registers where it may be read whole
-  HCNN_HD static void bring(const GemmArgs& a, uint32_t k0, char* lds, int tid, Regs& r) {
-    const uint32_t *ga = a.gather & kGatherA ? a.rows : nullptr, *gb = a.gather & kGatherB ? a.rows : nullptr;
-    if (A::direct_stage(a.lda, a.a_extent, r.M, r.k_end, ga, k0) && B::direct_stage(a.ldb, a.b_extent, a.N, r.k_end, gb, k0)) {
-      A::direct(A::direct_base(static_cast<const T*>(a.a), a.lda, ga, r.m0, k0), a.lda, ga, k0, lds, tid, r.oa);
-      B::direct(B::direct_base(static_cast<const T*>(a.b), a.ldb, gb, r.n0, k0), a.ldb, gb, k0, lds + A::kLdsBytes, tid, r.ob);
-    } else {
+  // The stage at k0 to LDS, past the registers where it may be read whole: then in kDirect pieces that the caller spreads out
+  static constexpr int kDirect = A::kEach + B::kEach;
+  struct Bring {
+    const GemmArgs& a;
+    const T *pa, *pb;
+    const uint32_t *ga, *gb;
+    char* lds;
+    uint32_t k0;
+    bool whole;
+    HCNN_HD Bring(const GemmArgs& args, uint32_t k, char* to, bool wanted, int tid, Regs& r) : a(args), lds(to), k0(k), whole(false) {
+      ga = a.gather & kGatherA ? a.rows : nullptr;
+      gb = a.gather & kGatherB ? a.rows : nullptr;
+      if (!wanted) return;
+      whole = A::direct_stage(a.lda, a.a_extent, r.M, r.k_end, ga, k0) && B::direct_stage(a.ldb, a.b_extent, a.N, r.k_end, gb, k0);
+      pa = A::direct_base(static_cast<const T*>(a.a), a.lda, ga, r.m0, k0);
+      pb = B::direct_base(static_cast<const T*>(a.b), a.ldb, gb, r.n0, k0);
+      if (whole) return;
       A::copy(static_cast<const T*>(a.a), a.lda, a.a_extent, r.M, r.k_end, ga, r.m0, k0, lds, tid);
       B::copy(static_cast<const T*>(a.b), a.ldb, a.b_extent, a.N, r.k_end, gb, r.n0, k0, lds + A::kLdsBytes, tid);
     }
-  }
+    HCNN_HD void piece(int i, int tid, Regs& r) const {
+      if (i < A::kEach) A::direct(pa, a.lda, ga, k0, lds, tid, i, r.oa);
+      else B::direct(pb, a.ldb, gb, k0, lds + A::kLdsBytes, tid, i - A::kEach, r.ob);
+    }
+    HCNN_HD void all(int tid, Regs& r) const {
+      if (!whole) return;
+#pragma unroll
+      for (int i = 0; i < kDirect; ++i) piece(i, tid, r);
+    }
+  };
   HCNN_HD static void begin(const GemmArgs& a, unsigned bid, int tid, uint32_t* lds, Regs& r) {
     place(a, bid, r);
     if constexpr (DIRECT) {
@@ -615,7 +631,7 @@ struct Gemm {
         for (int e = 0; e < 4; ++e) r.acc[i][j][e] = 0.0f;
     char* l = reinterpret_cast<char*>(lds);
     if constexpr (DIRECT) {
-      bring(a, r.k_begin, l, tid, r);
+      Bring(a, r.k_begin, l, true, tid, r).all(tid, r);
       direct_done();
     } else {
       fetch(a, r.k_begin, tid, r);
@@ -623,7 +639,7 @@ struct Gemm {
     }
     block_barrier();
     if (r.k_begin + kStage < r.k_end) {
-      if constexpr (DIRECT) bring(a, r.k_begin + kStage, l + kBuffer, tid, r);
+      if constexpr (DIRECT) Bring(a, r.k_begin + kStage, l + kBuffer, true, tid, r).all(tid, r);
       else fetch(a, r.k_begin + kStage, tid, r);
     }
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -637,7 +653,8 @@ struct Gemm {
   HCNN_HD static uint32_t n_wave(int tid) { return (uint32_t)tid / 64 % WN * (FN * 16); }
   // The products of step s of a stage, and the operands of the step after it from `lds`: step 1 of the same stage, or step 0 of the next
   // one behind the barrier that tells that it has arrived.
-  HCNN_HD static void multiply(const char* lds, uint32_t s, int tid, Regs& r) {
+  template <class Each>
+  HCNN_HD static void multiply(const char* lds, uint32_t s, int tid, Regs& r, Each&& each) {
 #if defined(__HIP_DEVICE_COMPILE__)
 #pragma unroll
     for (int j = 0; j < FN; ++j) r.step.b[1 - s][j] = B::read(lds + A::kLdsBytes, n_wave(tid) + j * 16, 1 - s, tid % 64);
@@ -646,8 +663,11 @@ struct Gemm {
 #pragma unroll
       for (int j = 0; j < FN; ++j) mma<T>(r.acc[i][j], r.step.b[s][j], r.step.a[i]);
       r.step.a[i] = A::read(lds, m_wave(tid) + i * 16, 1 - s, tid % 64);
+      each(i);
       sched_fence();
     }
+#else
+    for (int i = 0; i < FM; ++i) each(i);
 #endif
   }
   // the checker's products of the whole stage
@@ -673,16 +693,28 @@ struct Gemm {
     if constexpr (PH == 0) {
       if (k0 < r.k_end) {
         check_multiply(here, tid, r);
-        multiply(here, 0, tid, r);
+        multiply(here, 0, tid, r, [](int) {});
       }
       if constexpr (DIRECT) direct_done();
       else if (k0 + kStage < r.k_end) keep(next, tid, r);
     } else if constexpr (PH == 1) {
-      if (k0 + 2 * kStage < r.k_end) {
-        if constexpr (DIRECT) bring(a, k0 + 2 * kStage, here, tid, r);
-        else fetch(a, k0 + 2 * kStage, tid, r);
+      const bool more = k0 + 2 * kStage < r.k_end;
+      if constexpr (DIRECT) {
+        const Bring bring(a, k0 + 2 * kStage, here, more, tid, r);
+        if (k0 < r.k_end)
+          multiply(next, 1, tid, r, [&](int i) {
+            // (each behind some products: in front of them all, the matrix unit waited for their issue)
+            if (bring.whole) {
+              constexpr int kGroup = (kDirect + FM - 1) / FM;
+#pragma unroll
+              for (int d = 0; d < kGroup; ++d)
+                if (i * kGroup + d < kDirect) bring.piece(i * kGroup + d, tid, r);
+            }
+          });
+      } else {
+        if (more) fetch(a, k0 + 2 * kStage, tid, r);
+        if (k0 < r.k_end) multiply(next, 1, tid, r, [](int) {});
       }
-      if (k0 < r.k_end) multiply(next, 1, tid, r);
     } else if constexpr (EPI != kEpiStats) {
       constexpr uint32_t kPart = (PH - 2) / 2, kRows = BM / kParts, kQuads = BN / 4;
       if constexpr (PH % 2 == 0) {
