@@ -58,19 +58,19 @@ template <class V> V* at(hcnn_plain* h, size_t offset) { return reinterpret_cast
 
 // ---------------------------------------------------------------- tiles
 enum { kTile256, kTile128, kTile64, kTall, kFlat };
-struct Shape { int tile; uint32_t bm, bn, splits; };
+struct Shape { int tile; uint32_t bm, bn, splits; bool direct; };
 constexpr uint32_t kTileRows[] = {256, 128, 64, 128, 16}, kTileCols[] = {256, 128, 64, 16, 128};
 
 template <class T>
-Shape choose(const hcnn_plain* h, size_t M, size_t N, size_t K, bool may_split) {
+Shape choose(const hcnn_plain* h, size_t M, size_t N, size_t K, bool may_split, bool direct) {
   const size_t units = h->compute_units;
   auto tiles = [&](int t) { return blocks(M, kTileRows[t]) * blocks(N, kTileCols[t]); };
   int t = kTile64;
   if (N <= 16) t = kTall;
   else if (M <= 16) t = kFlat;
-  else if (sizeof(T) == 2 && tiles(kTile256) * 4 >= units * 3) t = kTile256;
+  else if (sizeof(T) == 2 && direct && tiles(kTile256) * 4 >= units * 3) t = kTile256;
   else if (tiles(kTile128) * 2 >= units) t = kTile128;
-  Shape s{t, kTileRows[t], kTileCols[t], 1};
+  Shape s{t, kTileRows[t], kTileCols[t], 1, direct};
   if (may_split) {
     // parts of at least four stages while there are fewer workgroups than two for each compute unit
     const size_t stages = blocks(K, GemmNum<T>::kStage), want = blocks(2 * units, std::max<size_t>(1, tiles(t)));
@@ -84,25 +84,49 @@ inline size_t sums_bytes(const Shape& s, size_t M, size_t N) { return s.splits >
 template <class G>
 int start(hcnn_plain* h, const GemmArgs& a, size_t grid) { return launch<G>(h->stream, grid, G::kLdsBytes, a); }
 
-// Whole stages go to LDS past the registers when every stored row of both operands starts on 16 bytes and the offsets within a
-// launch constant fit 32 bits: of a tile's rows, or of the whole operand where its rows are gathered.
-template <class T, int LAYOUT>
-bool direct_operand(const void* p, size_t ld, size_t extent, bool gathered, size_t tile) {
-  if (reinterpret_cast<uintptr_t>(p) % 16 || ld * sizeof(T) % 16) return false;
-  const size_t lines = LAYOUT == kAlongK ? tile : GemmNum<T>::kStage;
-  return (gathered ? extent : lines * ld + tile) * sizeof(T) < ((size_t)1 << 32);
+// An operand as the caller has it, or a copy of it in the work memory whose rows all start on 16 bytes, as whole stages' way to LDS
+// past the registers needs them (also: offsets within a launch constant in 32 bits, of a stage's rows or, where its rows are
+// gathered, of the whole operand).
+struct Input {
+  const void* p;
+  size_t ld, rows, cols;
+  bool packed = false;
+  size_t offset = 0;
+  size_t extent() const { return rows && cols ? (rows - 1) * ld + cols : 0; }
+};
+template <class T>
+bool direct_input(const Input& x, bool gathered) {
+  const bool aligned = x.packed || (reinterpret_cast<uintptr_t>(x.p) % 16 == 0 && x.ld * sizeof(T) % 16 == 0);
+  return aligned && (gathered ? x.extent() : 257 * x.ld) * sizeof(T) < ((size_t)1 << 32);
+}
+// Copies pay from some size of the products that take the operand on: `work` = M N K of all of them.  By measurement (bfloat16,
+// M = N = K, us with / without copies of both operands): see kPackWork.
+constexpr double kPackWork = 3e-15, kPackByte = 5e-13, kPackLaunch = 5e-6;
+template <class T>
+void plan_pack(Input& x, Arena& a, double work) {
+  if (sizeof(T) != 2 || direct_input<T>(x, false) || x.rows == 0 || x.cols == 0) return;
+  if (work * kPackWork < kPackLaunch + 4.0 * (double)x.rows * (double)x.cols * kPackByte) return;
+  x.packed = true;
+  x.ld = up(x.cols, 8);
+  x.offset = a.take(x.rows * x.ld * sizeof(T));
+}
+template <class T>
+int pack(hcnn_plain* h, Input& x, const void* from, size_t ld_from) {
+  if (!x.packed) return 0;
+  const PackArgs p{from, ld_from, at<void>(h, x.offset), x.ld, (uint32_t)x.rows, (uint32_t)x.cols, x.rows * (x.ld / 8)};
+  x.p = p.to;
+  return launch<PackRows>(h->stream, blocks(p.pieces, PackRows::kThreads), 0, p);
 }
 template <class T, int LA, int LB, int EPI>
 int gemm(hcnn_plain* h, const GemmArgs& a, const Shape& s) {
   const size_t grid = blocks(a.M, s.bm) * blocks(a.N, s.bn) * s.splits;
   if (grid > kMaxSize) return HCNN_ERR_ARG;
-  const bool direct = direct_operand<T, LA>(a.a, a.lda, a.a_extent, a.gather & kGatherA, s.bm) &&
-                      direct_operand<T, LB>(a.b, a.ldb, a.b_extent, a.gather & kGatherB, s.bn);
 #define PLAIN_TILE(BM, BN, WM, WN) \
-  return direct ? start<Gemm<T, LA, LB, BM, BN, WM, WN, EPI, true>>(h, a, grid) : start<Gemm<T, LA, LB, BM, BN, WM, WN, EPI, false>>(h, a, grid)
+  return s.direct ? start<Gemm<T, LA, LB, BM, BN, WM, WN, EPI, true>>(h, a, grid) : start<Gemm<T, LA, LB, BM, BN, WM, WN, EPI, false>>(h, a, grid)
   switch (s.tile) {
     case kTile256:
-      if constexpr (sizeof(T) == 2) PLAIN_TILE(256, 256, 2, 4);
+      if constexpr (sizeof(T) == 2)
+        if (s.direct) return start<Gemm<T, LA, LB, 256, 256, 2, 4, EPI, true>>(h, a, grid);
       return HCNN_ERR_ARG;
     case kTile128: PLAIN_TILE(128, 128, 2, 2);
     case kTile64: PLAIN_TILE(64, 64, 2, 2);
@@ -123,10 +147,10 @@ int product(hcnn_plain* h, GemmArgs a, const Shape& s, float* sums) {
   return e ? e : launch<GemmJoin<T>>(h->stream, GemmJoin<T>::grid(a), 0, a);
 }
 
-inline GemmArgs operands(const void* a, size_t lda, size_t a_rows, size_t a_cols, const void* b, size_t ldb, size_t b_rows, size_t b_cols) {
+inline GemmArgs operands(const Input& a, const Input& b) {
   GemmArgs g{};
-  g.a = a; g.lda = lda; g.a_extent = a_rows ? (a_rows - 1) * lda + a_cols : 0;
-  g.b = b; g.ldb = ldb; g.b_extent = b_rows ? (b_rows - 1) * ldb + b_cols : 0;
+  g.a = a.p; g.lda = a.ld; g.a_extent = a.extent();
+  g.b = b.p; g.ldb = b.ld; g.b_extent = b.extent();
   g.splits = 1;
   return g;
 }
@@ -135,14 +159,20 @@ inline GemmArgs operands(const void* a, size_t lda, size_t a_rows, size_t a_cols
 template <class T>
 int linear(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void* x, size_t ldx, const void* w, size_t ldw, const void* bias,
            const void* residual, size_t ld_residual, void* y, size_t ldy, void* z, size_t ldz) {
-  const Shape s = choose<T>(h, M, N, K, true);
-  const int e = reserve(h, sums_bytes(s, M, N));
-  if (e) return e;
-  GemmArgs g = operands(x, ldx, M, K, w, ldw, N, K);
+  Arena ar;
+  Input ix{x, ldx, M, K}, iw{w, ldw, N, K};
+  const double work = (double)M * (double)N * (double)K;
+  plan_pack<T>(ix, ar, work);
+  plan_pack<T>(iw, ar, work);
+  const Shape s = choose<T>(h, M, N, K, true, direct_input<T>(ix, false) && direct_input<T>(iw, false));
+  const size_t o_sums = ar.take(sums_bytes(s, M, N));
+  int e = reserve(h, ar.bytes);
+  if (e || (e = pack<T>(h, ix, x, ldx)) || (e = pack<T>(h, iw, w, ldw))) return e;
+  GemmArgs g = operands(ix, iw);
   g.M = (uint32_t)M; g.N = (uint32_t)N; g.K = (uint32_t)K;
   g.act = act; g.bias = bias; g.residual = residual; g.ld_residual = ld_residual;
   g.out = y; g.ld_out = ldy; g.z = z; g.ld_z = ldz;
-  return product<T, kAlongK, kAlongK>(h, g, s, at<float>(h, 0));
+  return product<T, kAlongK, kAlongK>(h, g, s, at<float>(h, o_sums));
 }
 
 template <class T>
@@ -165,22 +195,38 @@ int act_grad(hcnn_plain* h, ActGradArgs a, size_t* row_blocks, bool only_size) {
 template <class T>
 int linear_grad(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void* dy, size_t ld_dy, const void* x, size_t ldx, const void* w,
                 size_t ldw, const void* z, size_t ldz, void* dx, size_t ld_dx, void* dw, size_t ld_dw, void* db) {
-  const Shape sx = choose<T>(h, M, K, N, true), sw = choose<T>(h, N, K, M, true);
+  const double work = (double)M * (double)N * (double)K;
   ActGradArgs ag{};
   ag.dy = dy; ag.ld_dy = ld_dy; ag.M = (uint32_t)M; ag.N = (uint32_t)N; ag.act = act;
   if (act != kActNone) { ag.z = z; ag.ld_z = ldz; }
-  ag.ld_dz = up(N, 16 / sizeof(T)); ag.ld_part = up(N, 4);
+  ag.ld_part = up(N, 4);
   size_t row_blocks = 0;
   act_grad<T>(h, ag, &row_blocks, true);
-  Arena w_;
-  const size_t o_dz = w_.take(act != kActNone ? M * ag.ld_dz * sizeof(T) : 0), o_part = w_.take(db ? row_blocks * ag.ld_part * 4 : 0);
-  const size_t o_sums = w_.take(std::max(dx ? sums_bytes(sx, M, K) : 0, dw ? sums_bytes(sw, N, K) : 0));
-  int e = reserve(h, w_.bytes);
-  if (e) return e;
-  const void* dz = dy;
-  size_t ld_dz = ld_dy;
+  Arena ar;
+  Input ix{x, ldx, M, K}, iw{w, ldw, N, K}, idz{dy, ld_dy, M, N};
+  if (act != kActNone) {                                   // dz: aligned rows in the work memory
+    idz.packed = true;
+    idz.ld = up(N, 16 / sizeof(T));
+    idz.offset = ar.take(M * idz.ld * sizeof(T));
+  } else {
+    plan_pack<T>(idz, ar, work * ((dx != nullptr) + (dw != nullptr)));
+  }
+  if (dw) plan_pack<T>(ix, ar, work);
+  if (dx) plan_pack<T>(iw, ar, work);
+  const bool direct = direct_input<T>(idz, false);
+  const Shape sx = choose<T>(h, M, K, N, true, direct && direct_input<T>(iw, false)), sw = choose<T>(h, N, K, M, true, direct && direct_input<T>(ix, false));
+  const size_t o_part = ar.take(db ? row_blocks * ag.ld_part * 4 : 0);
+  const size_t o_sums = ar.take(std::max(dx ? sums_bytes(sx, M, K) : 0, dw ? sums_bytes(sw, N, K) : 0));
+  int e = reserve(h, ar.bytes);
+  if (e || (e = pack<T>(h, ix, x, ldx)) || (e = pack<T>(h, iw, w, ldw))) return e;
+  if (act == kActNone) {
+    if ((e = pack<T>(h, idz, dy, ld_dy))) return e;
+  } else {
+    idz.p = at<void>(h, idz.offset);
+    ag.dz = at<void>(h, idz.offset);
+    ag.ld_dz = idz.ld;
+  }
   if (M && N && (act != kActNone || db)) {
-    if (act != kActNone) { ag.dz = at<void>(h, o_dz); dz = ag.dz; ld_dz = ag.ld_dz; }
     if (db) ag.part = at<float>(h, o_part);
     if ((e = act_grad<T>(h, ag, &row_blocks, false))) return e;
   }
@@ -189,13 +235,13 @@ int linear_grad(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void
     if ((e = launch<ColumnSum<T>>(h->stream, blocks(N, 16), ColumnSum<T>::kLdsBytes, cs))) return e;
   }
   if (dx) {
-    GemmArgs g = operands(dz, ld_dz, M, N, w, ldw, N, K);
+    GemmArgs g = operands(idz, iw);
     g.M = (uint32_t)M; g.N = (uint32_t)K; g.K = (uint32_t)N;
     g.out = dx; g.ld_out = ld_dx;
     if ((e = product<T, kAlongK, kAcrossK>(h, g, sx, at<float>(h, o_sums)))) return e;
   }
   if (dw) {
-    GemmArgs g = operands(dz, ld_dz, M, N, x, ldx, M, K);
+    GemmArgs g = operands(idz, ix);
     g.M = (uint32_t)N; g.N = (uint32_t)K; g.K = (uint32_t)M;
     g.out = dw; g.ld_out = ld_dw;
     if ((e = product<T, kAcrossK, kAcrossK>(h, g, sw, at<float>(h, o_sums)))) return e;
@@ -222,21 +268,28 @@ template <class T> constexpr float delta_scale() { return std::is_same_v<T, Half
 template <class T>
 int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
   const size_t M = c.M, K = c.K, V = c.V;
-  const Shape ss = choose<T>(h, M, V, K, false);
+  Arena a;
+  Input ix{c.x, c.ldx, M, K}, iw{c.w, c.ldw, V, K};
+  const double work = (double)M * (double)V * (double)K * (grad ? 3 : 1);
+  plan_pack<T>(ix, a, work);
+  plan_pack<T>(iw, a, work);
   // columns of a piece: whole tiles, all columns where they fit
   const size_t fit = kDeltaBytes / (std::max<size_t>(M, 1) * sizeof(T)) / 256 * 256;
   const size_t piece = grad ? std::min(V, std::max<size_t>(fit, 256)) : 0;
   const size_t pieces = grad ? blocks(V, piece) : 0, ld_delta = up(piece, 16 / sizeof(T));
-  Shape sx = choose<T>(h, M, K, piece, pieces == 1), sw = choose<T>(h, piece, K, M, true);
+  const bool direct_x = direct_input<T>(ix, true), direct_w = direct_input<T>(iw, false);
+  const Shape ss = choose<T>(h, M, V, K, false, direct_x && direct_w);
+  Input idelta{nullptr, ld_delta, M, piece, true, a.take(grad ? M * ld_delta * sizeof(T) : 0)};
+  const bool direct_d = direct_input<T>(idelta, false);
+  const Shape sx = choose<T>(h, M, K, piece, pieces == 1, direct_d && direct_w), sw = choose<T>(h, piece, K, M, true, direct_d && direct_x);
   const size_t tiles = blocks(V, ss.bn), ld_stats = up(M, 64), row_wgs = blocks(M, RowStats::kRows);
-  Arena a;
   const size_t o_count = a.take(4), o_alpha = a.take(4), o_rows = a.take(M * 4), o_target = a.take(M * 4), o_score = a.take(M * 4), o_lse = a.take(M * 4);
   const size_t o_stats = a.take(tiles * 2 * ld_stats * 4), o_part = a.take(row_wgs * 8);
-  const size_t o_delta = a.take(grad ? M * ld_delta * sizeof(T) : 0);
   const size_t o_dx = a.take(pieces > 1 && c.dx ? M * up(K, 8) * 4 : 0);
   const size_t o_sums = a.take(grad ? std::max(c.dx ? sums_bytes(sx, M, K) : 0, c.dw ? sums_bytes(sw, piece, K) : 0) : 0);
   int e = reserve(h, a.bytes);
-  if (e) return e;
+  if (e || (e = pack<T>(h, ix, c.x, c.ldx)) || (e = pack<T>(h, iw, c.w, c.ldw))) return e;
+  idelta.p = at<void>(h, idelta.offset);
   uint32_t *count = at<uint32_t>(h, o_count), *rows = at<uint32_t>(h, o_rows), *target = at<uint32_t>(h, o_target);
   float *alpha = at<float>(h, o_alpha), *score = at<float>(h, o_score), *lse = at<float>(h, o_lse);
 
@@ -246,7 +299,7 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
     const BlankRowsArgs br{kr, c.dx, c.ld_dx * sizeof(T), K * sizeof(T), c.row_loss, c.row_lse};
     if ((e = launch<BlankRows>(h->stream, blocks(M, 4), 0, br))) return e;
   }
-  GemmArgs g = operands(c.x, c.ldx, M, K, c.w, c.ldw, V, K);
+  GemmArgs g = operands(ix, iw);
   g.M = (uint32_t)M; g.N = (uint32_t)V; g.K = (uint32_t)K;
   g.rows = rows; g.count = count; g.gather = kGatherA; g.count_of = kCountM;
   g.stats = at<float>(h, o_stats); g.ld_stats = ld_stats; g.target = target; g.target_score = score; g.lse = lse;
@@ -261,17 +314,17 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
 
   for (size_t p = 0; p < pieces; ++p) {
     const size_t v0 = p * piece, n = std::min(piece, V - v0);
-    const char* wp = static_cast<const char*>(c.w) + v0 * c.ldw * sizeof(T);
-    void* delta = at<void>(h, o_delta);
+    Input wp{static_cast<const char*>(iw.p) + v0 * iw.ld * sizeof(T), iw.ld, n, K};
+    idelta.cols = n;
     if (M) {
       GemmArgs d = g;
-      d.b = wp; d.b_extent = (n - 1) * c.ldw + K;
+      d.b = wp.p; d.b_extent = wp.extent();
       d.N = (uint32_t)n; d.n_offset = (uint32_t)v0;
-      d.out = delta; d.ld_out = ld_delta;
-      if ((e = gemm<T, kAlongK, kAlongK, kEpiDelta>(h, d, choose<T>(h, M, n, K, false)))) return e;
+      d.out = at<void>(h, idelta.offset); d.ld_out = ld_delta;
+      if ((e = gemm<T, kAlongK, kAlongK, kEpiDelta>(h, d, choose<T>(h, M, n, K, false, direct_x && direct_w)))) return e;
     }
     if (c.dx && M && K) {
-      GemmArgs d = operands(delta, ld_delta, M, n, wp, c.ldw, n, K);
+      GemmArgs d = operands(idelta, wp);
       d.M = (uint32_t)M; d.N = (uint32_t)K; d.K = (uint32_t)n;
       d.rows = rows; d.count = count; d.count_of = kCountM;
       if (p) { d.addend = at<float>(h, o_dx); d.ld_sums = up(K, 8); }
@@ -285,12 +338,11 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
       }
     }
     if (c.dw && K) {
-      GemmArgs d = operands(delta, ld_delta, M, n, c.x, c.ldx, M, K);
+      GemmArgs d = operands(idelta, ix);
       d.M = (uint32_t)n; d.N = (uint32_t)K; d.K = (uint32_t)M;
       d.rows = rows; d.count = count; d.count_of = kCountK; d.gather = kGatherB; d.alpha = alpha;
       d.out = static_cast<char*>(c.dw) + v0 * c.ld_dw * sizeof(T); d.ld_out = c.ld_dw;
-      Shape s = sw;
-      if ((e = product<T, kAcrossK, kAcrossK>(h, d, s, at<float>(h, o_sums)))) return e;
+      if ((e = product<T, kAcrossK, kAcrossK>(h, d, sw, at<float>(h, o_sums)))) return e;
     }
   }
   return 0;

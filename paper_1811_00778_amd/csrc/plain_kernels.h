@@ -214,10 +214,12 @@ HCNN_HD float slope_of(float z, int act) {
 // ---------------------------------------------------------------- matrix products
 // out[m][n] = sum_k a(m, k) b(n, k).  An operand is stored with its contraction index k contiguous (kAlongK: a[m][k]) or with
 // its output index contiguous (kAcrossK: a[k][m]).  A workgroup computes a tile of BM x BN outputs in WM x WN waves; a stage is 128
-// bytes of k (64 numbers of 16 bits, 32 of 32).  A stage's tiles go from memory to registers one stage ahead and from there to one
-// of two LDS buffers, so that a stage costs one barrier.
+// bytes of k (64 numbers of 16 bits, 32 of 32) in two steps, and LDS holds two stages.  While a step's products run, the next step's operands go
+// from LDS to registers.  One barrier a stage, between its steps: behind it the stage's operands are all in registers, the stage after
+// next comes from memory to its place, and the next one, which was asked for a stage earlier, has arrived.  (Four stages of half the size in the same
+// memory and a load's time of two: a barrier for half as many products cost 8 %.)
 //   kAlongK  in LDS [row][8 pieces of 16 bytes], piece p of a row at p ^ (row mod 8): the 16 rows x 4 pieces that a wave reads at once
-//            and the rows that it writes spread evenly over the banks
+//            spread evenly over the banks
 //   kAcrossK in LDS [k][rows] as it lies in memory, in granules of 16 rows; 16-bit numbers are read with the transposing LDS read
 //            (16 lanes: 4 k x 16 rows in, 4 k of one row out), 32-bit ones word by word; granules are swapped by the bits of k in which the lanes
 //            of one read differ
@@ -431,8 +433,22 @@ struct GemmOperand {
   HCNN_HD static void direct(const T* base, size_t ld, const uint32_t* rows, uint32_t k0, char* lds, int tid, int i, const uint32_t (&off)[kEach]) {
     if (!mine(tid, i)) return;
     uint32_t o = off[i];
-    if (LAYOUT == kAcrossK && rows) o += (uint32_t)(rows[k0 + (tid + i * THREADS) / kRowPieces] * ld * sizeof(T));
+    if (LAYOUT == kAcrossK && rows) o += (uint32_t)(row_at(rows, k0, tid, i) * ld * sizeof(T));
     to_lds(base, o, lds + ((tid & ~63) + i * THREADS) * 16, tid & 63);
+  }
+  // The gathered row of a thread's piece.  A wave's pieces lie in few rows: their indices come by scalar loads, since a vector load in the
+  // middle of the stages would be waited for together with all stages on their way.
+  HCNN_HD static uint32_t row_at(const uint32_t* rows, uint32_t k0, int tid, int i) {
+    constexpr uint32_t kLines = 64 / kRowPieces;                                // stored rows of a wave's pieces
+    if constexpr (LAYOUT == kAcrossK && kRowPieces <= 64 && kLines <= 4) {
+      const uint32_t first = k0 + wave_uniform((uint32_t)(tid & ~63) + i * THREADS) / kRowPieces, mine = (uint32_t)(tid & 63) / kRowPieces;
+      uint32_t row = ldc(rows, first);
+#pragma unroll
+      for (uint32_t l = 1; l < kLines; ++l) row = mine == l ? ldc(rows, first + l) : row;
+      return row;
+    } else {
+      return rows[k0 + (tid + i * THREADS) / kRowPieces];
+    }
   }
   // 16 bytes of every lane of a wave to LDS, side by side
   HCNN_HD static void to_lds(const T* base, uint32_t off, char* lds, int lane) {
@@ -444,7 +460,7 @@ struct GemmOperand {
     __builtin_memcpy(lds + lane * 16, reinterpret_cast<const char*>(base) + off, 16);
 #endif
   }
-  // 16 bytes of row `base + lane % 16`, step s (of two 64-byte steps) of the stage; base a multiple of 16
+  // 16 bytes of row `base + lane % 16` of step s of a stage; base a multiple of 16
 #if defined(__HIP_DEVICE_COMPILE__)
   __device__ __forceinline__ static hcnn_word4 read(const char* lds, uint32_t base, uint32_t s, uint32_t lane) {
     const uint32_t g = lane / 16, i = lane % 16;
@@ -479,7 +495,7 @@ struct GemmOperand {
 
 #if defined(__HIP_DEVICE_COMPILE__)
 typedef float hcnn_float4 __attribute__((ext_vector_type(4)));
-// acc += b (16 n) x a (16 m) over a 64-byte step
+// acc += b (16 n) x a (16 m) over a step
 template <class T>
 __device__ __forceinline__ void mma(hcnn_float4& acc, hcnn_word4 b, hcnn_word4 a) {
   if constexpr (sizeof(T) == 4) {
@@ -501,12 +517,6 @@ struct hcnn_float4 {
 };
 #endif
 
-// All waves of the workgroup, inside a phase that the checker runs thread by thread: only in front of what it does not do
-HCNN_HD void block_barrier() {
-#if defined(__HIP_DEVICE_COMPILE__)
-  __syncthreads();
-#endif
-}
 // What is on its way to LDS past the registers has arrived
 HCNN_HD void direct_done() {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -528,18 +538,22 @@ struct Gemm {
   typedef GemmOperand<T, LB, BN, kThreads> B;
   static constexpr uint32_t kBuffer = A::kLdsBytes + B::kLdsBytes;
   static constexpr size_t kLdsBytes = 2 * kBuffer;
-  static_assert(EPI != kEpiStats || BM * WN * 4 * 8 <= 2 * kBuffer, "the statistics fit the stages' memory");
-  static_assert(BM / kParts * BN * 4 <= 2 * kBuffer && WM % kParts == 0, "a part's sums fit the stages' memory");
+  static_assert(EPI != kEpiStats || BM * WN * 4 * 8 <= kLdsBytes, "the statistics fit the stages' memory");
+  static_assert(BM / kParts * BN * 4 <= kLdsBytes && WM % kParts == 0, "a part's sums fit the stages' memory");
 
-  // Operands of the running 64-byte step; b's of the next one beside them, a's take their place as soon as a row's products are under way.
+  // Operands of the running step.  The next one's take the place of an a as soon as its products are under way; b and the last kAhead
+  // of a have two places, so that their reads come first and the step's end does not wait for one that was just asked for.
+  static constexpr int kAhead = LA == kAlongK && FM >= 8 ? 2 : 0;
+  static constexpr uint32_t kStep = kStage / 2;
 #if defined(__HIP_DEVICE_COMPILE__)
-  struct Step { hcnn_word4 a[FM], b[2][FN]; };
+  struct Step { hcnn_word4 a[FM + kAhead], b[2][FN]; };
 #else
-  struct Step {};
+  struct Step { float a[FM + kAhead][kStep], b[2][FN * 4][kStep]; };
 #endif
   struct Regs {
     uint32_t iter;
     uint32_t m0, n0, k_begin, k_end, M, split;
+    const uint32_t *ga, *gb;                     // indices of gathered rows; null where all rows take part: they are in order
     U4 ra[A::kEach], rb[B::kEach];               // the next stage, unless DIRECT
     uint32_t oa[A::kEach], ob[B::kEach];         // DIRECT: offsets of the pieces
     Step step;
@@ -556,7 +570,8 @@ struct Gemm {
     const uint32_t stages = (counted(a, kCountK, a.K) + kStage - 1) / kStage;
     return (stages + a.splits - 1) / a.splits;
   }
-  // Workgroups go round the eight dies; each die takes a run of consecutive tiles, which walk through bands of eight tiles of m, so
+  static constexpr bool wave_sync(int ph) { return ph == 1; }
+  // Workgroups go round the eight dies; each die takes a run of consecutive tiles, which walk through bands of four tiles of m, so
   // that the operands' rows that its workgroups read at a time are few.  Tiles beyond the counted rows are not in the order.
   HCNN_HD static bool skip(const GemmArgs& a, unsigned bid) {
     if (a.count_of != kCountM) return false;
@@ -570,18 +585,21 @@ struct Gemm {
     uint32_t at = die * each + (die < rest ? die : rest) + bid / 8;
     r.split = at / (tm * tn);
     at -= r.split * (tm * tn);
-    constexpr uint32_t kBand = 8;
+    constexpr uint32_t kBand = 4;
     const uint32_t band = at / (kBand * tn), high = tm - band * kBand < kBand ? tm - band * kBand : kBand;
     at -= band * kBand * tn;
     r.m0 = (band * kBand + at % high) * BM;
     r.n0 = at / high * BN;
+    const bool some = a.count_of != kCountNone && wave_uniform(*a.count) < (a.count_of == kCountM ? a.M : a.K);
+    r.ga = some && (a.gather & kGatherA) ? a.rows : nullptr;
+    r.gb = some && (a.gather & kGatherB) ? a.rows : nullptr;
     const uint32_t K = counted(a, kCountK, a.K), run = loop_count(a) * kStage;
     r.k_begin = r.split * run;
     r.k_end = K < r.k_begin + run ? K : r.k_begin + run;
   }
   HCNN_HD static void fetch(const GemmArgs& a, uint32_t k0, int tid, Regs& r) {
-    A::load(static_cast<const T*>(a.a), a.lda, a.a_extent, r.M, r.k_end, a.gather & kGatherA ? a.rows : nullptr, r.m0, k0, tid, r.ra);
-    B::load(static_cast<const T*>(a.b), a.ldb, a.b_extent, a.N, r.k_end, a.gather & kGatherB ? a.rows : nullptr, r.n0, k0, tid, r.rb);
+    A::load(static_cast<const T*>(a.a), a.lda, a.a_extent, r.M, r.k_end, r.ga, r.m0, k0, tid, r.ra);
+    B::load(static_cast<const T*>(a.b), a.ldb, a.b_extent, a.N, r.k_end, r.gb, r.n0, k0, tid, r.rb);
   }
   HCNN_HD static void keep(char* lds, int tid, const Regs& r) {
     A::store(lds, tid, r.ra);
@@ -592,24 +610,21 @@ struct Gemm {
   struct Bring {
     const GemmArgs& a;
     const T *pa, *pb;
-    const uint32_t *ga, *gb;
     char* lds;
     uint32_t k0;
     bool whole;
     HCNN_HD Bring(const GemmArgs& args, uint32_t k, char* to, bool wanted, int tid, Regs& r) : a(args), lds(to), k0(k), whole(false) {
-      ga = a.gather & kGatherA ? a.rows : nullptr;
-      gb = a.gather & kGatherB ? a.rows : nullptr;
       if (!wanted) return;
-      whole = A::direct_stage(a.lda, a.a_extent, r.M, r.k_end, ga, k0) && B::direct_stage(a.ldb, a.b_extent, a.N, r.k_end, gb, k0);
-      pa = A::direct_base(static_cast<const T*>(a.a), a.lda, ga, r.m0, k0);
-      pb = B::direct_base(static_cast<const T*>(a.b), a.ldb, gb, r.n0, k0);
+      whole = A::direct_stage(a.lda, a.a_extent, r.M, r.k_end, r.ga, k0) && B::direct_stage(a.ldb, a.b_extent, a.N, r.k_end, r.gb, k0);
+      pa = A::direct_base(static_cast<const T*>(a.a), a.lda, r.ga, r.m0, k0);
+      pb = B::direct_base(static_cast<const T*>(a.b), a.ldb, r.gb, r.n0, k0);
       if (whole) return;
-      A::copy(static_cast<const T*>(a.a), a.lda, a.a_extent, r.M, r.k_end, ga, r.m0, k0, lds, tid);
-      B::copy(static_cast<const T*>(a.b), a.ldb, a.b_extent, a.N, r.k_end, gb, r.n0, k0, lds + A::kLdsBytes, tid);
+      A::copy(static_cast<const T*>(a.a), a.lda, a.a_extent, r.M, r.k_end, r.ga, r.m0, k0, lds, tid);
+      B::copy(static_cast<const T*>(a.b), a.ldb, a.b_extent, a.N, r.k_end, r.gb, r.n0, k0, lds + A::kLdsBytes, tid);
     }
     HCNN_HD void piece(int i, int tid, Regs& r) const {
-      if (i < A::kEach) A::direct(pa, a.lda, ga, k0, lds, tid, i, r.oa);
-      else B::direct(pb, a.ldb, gb, k0, lds + A::kLdsBytes, tid, i - A::kEach, r.ob);
+      if (i < A::kEach) A::direct(pa, a.lda, r.ga, k0, lds, tid, i, r.oa);
+      else B::direct(pb, a.ldb, r.gb, k0, lds + A::kLdsBytes, tid, i - A::kEach, r.ob);
     }
     HCNN_HD void all(int tid, Regs& r) const {
       if (!whole) return;
@@ -620,8 +635,8 @@ struct Gemm {
   HCNN_HD static void begin(const GemmArgs& a, unsigned bid, int tid, uint32_t* lds, Regs& r) {
     place(a, bid, r);
     if constexpr (DIRECT) {
-      A::direct_offsets(a.lda, r.M, a.gather & kGatherA ? a.rows : nullptr, r.m0, tid, r.oa);
-      B::direct_offsets(a.ldb, a.N, a.gather & kGatherB ? a.rows : nullptr, r.n0, tid, r.ob);
+      A::direct_offsets(a.lda, r.M, r.ga, r.m0, tid, r.oa);
+      B::direct_offsets(a.ldb, a.N, r.gb, r.n0, tid, r.ob);
     }
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -632,75 +647,80 @@ struct Gemm {
     char* l = reinterpret_cast<char*>(lds);
     if constexpr (DIRECT) {
       Bring(a, r.k_begin, l, true, tid, r).all(tid, r);
+      Bring(a, r.k_begin + kStage, l + kBuffer, r.k_begin + kStage < r.k_end, tid, r).all(tid, r);
       direct_done();
     } else {
       fetch(a, r.k_begin, tid, r);
       keep(l, tid, r);
+      fetch(a, r.k_begin + kStage, tid, r);
     }
-    block_barrier();
-    if (r.k_begin + kStage < r.k_end) {
-      if constexpr (DIRECT) Bring(a, r.k_begin + kStage, l + kBuffer, true, tid, r).all(tid, r);
-      else fetch(a, r.k_begin + kStage, tid, r);
-    }
-#if defined(__HIP_DEVICE_COMPILE__)
+  }
+  HCNN_HD static void begin_next(const GemmArgs&, unsigned, int tid, uint32_t* lds, Regs& r) {
 #pragma unroll
-    for (int i = 0; i < FM; ++i) r.step.a[i] = A::read(l, m_wave(tid) + i * 16, 0, tid % 64);
+    for (int i = 0; i < FM; ++i) read_a(reinterpret_cast<char*>(lds), 0, i, tid, r);
 #pragma unroll
-    for (int j = 0; j < FN; ++j) r.step.b[0][j] = B::read(l + A::kLdsBytes, n_wave(tid) + j * 16, 0, tid % 64);
-#endif
+    for (int j = 0; j < FN; ++j) read_b(reinterpret_cast<char*>(lds), 0, j, tid, r);
   }
   HCNN_HD static uint32_t m_wave(int tid) { return (uint32_t)tid / 64 / WN * (FM * 16); }
   HCNN_HD static uint32_t n_wave(int tid) { return (uint32_t)tid / 64 % WN * (FN * 16); }
-  // The products of step s of a stage, and the operands of the step after it from `lds`: step 1 of the same stage, or step 0 of the next
-  // one behind the barrier that tells that it has arrived.
-  template <class Each>
-  HCNN_HD static void multiply(const char* lds, uint32_t s, int tid, Regs& r, Each&& each) {
+  // place of a's i-th operand of step s
+  static constexpr int a_place(int s, int i) { return s && i >= FM - kAhead ? i + kAhead : i; }
 #if defined(__HIP_DEVICE_COMPILE__)
+  __device__ __forceinline__ static void read_a(const char* lds, int s, int i, int tid, Regs& r) {
+    r.step.a[a_place(s, i)] = A::read(lds, m_wave(tid) + i * 16, s, tid % 64);
+  }
+  __device__ __forceinline__ static void read_b(const char* lds, int s, int j, int tid, Regs& r) {
+    r.step.b[s][j] = B::read(lds + A::kLdsBytes, n_wave(tid) + j * 16, s, tid % 64);
+  }
+  __device__ __forceinline__ static void products(int s, int i, Regs& r) {
 #pragma unroll
-    for (int j = 0; j < FN; ++j) r.step.b[1 - s][j] = B::read(lds + A::kLdsBytes, n_wave(tid) + j * 16, 1 - s, tid % 64);
+    for (int j = 0; j < FN; ++j) mma<T>(r.acc[i][j], r.step.b[s][j], r.step.a[a_place(s, i)]);
+  }
+#else
+  // (the checker keeps the numbers that a lane's four sums of each 16 x 16 take)
+  HCNN_HD static void read_a(const char* lds, int s, int i, int tid, Regs& r) {
+    for (uint32_t k = 0; k < kStep; ++k) r.step.a[a_place(s, i)][k] = A::at(lds, m_wave(tid) + i * 16 + tid % 16, s * kStep + k);
+  }
+  HCNN_HD static void read_b(const char* lds, int s, int j, int tid, Regs& r) {
+    for (uint32_t e = 0; e < 4; ++e)
+      for (uint32_t k = 0; k < kStep; ++k) r.step.b[s][j * 4 + e][k] = B::at(lds + A::kLdsBytes, n_wave(tid) + j * 16 + tid % 64 / 16 * 4 + e, s * kStep + k);
+  }
+  HCNN_HD static void products(int s, int i, Regs& r) {
+    for (int j = 0; j < FN; ++j)
+      for (uint32_t e = 0; e < 4; ++e)
+        for (uint32_t k = 0; k < kStep; ++k) r.acc[i][j][e] += r.step.a[a_place(s, i)][k] * r.step.b[s][j * 4 + e][k];
+  }
+#endif
+  // The products of step s, and the operands of the step after it from `next`
+  template <class Each>
+  HCNN_HD static void multiply(const char* next, int s, int tid, Regs& r, Each&& each) {
+#pragma unroll
+    for (int j = 0; j < FN; ++j) read_b(next, 1 - s, j, tid, r);
+#pragma unroll
+    for (int i = FM - kAhead; i < FM; ++i) read_a(next, 1 - s, i, tid, r);
 #pragma unroll
     for (int i = 0; i < FM; ++i) {
-#pragma unroll
-      for (int j = 0; j < FN; ++j) mma<T>(r.acc[i][j], r.step.b[s][j], r.step.a[i]);
-      r.step.a[i] = A::read(lds, m_wave(tid) + i * 16, 1 - s, tid % 64);
+      products(s, i, r);
+      if (i < FM - kAhead) read_a(next, 1 - s, i, tid, r);
       each(i);
       sched_fence();
     }
-#else
-    for (int i = 0; i < FM; ++i) each(i);
-#endif
   }
-  // the checker's products of the whole stage
-  HCNN_HD static void check_multiply(const char* lds, int tid, Regs& r) {
-#if !defined(__HIP_DEVICE_COMPILE__)
-    const uint32_t lane = (uint32_t)tid % 64, mw = m_wave(tid), nw = n_wave(tid);
-    for (int i = 0; i < FM; ++i)
-      for (int j = 0; j < FN; ++j)
-        for (uint32_t e = 0; e < 4; ++e)
-          for (uint32_t k = 0; k < kStage; ++k)
-            r.acc[i][j][e] += A::at(lds, mw + i * 16 + lane % 16, k) * B::at(lds + A::kLdsBytes, nw + j * 16 + lane / 16 * 4 + e, k);
-#endif
-  }
-  static constexpr bool wave_sync(int ph) { return ph == 1; }
 
   template <int PH>
   HCNN_HD static void phase(const GemmArgs& a, unsigned, int tid, uint32_t* lds_words, Regs& r) {
     char* lds = reinterpret_cast<char*>(lds_words);
     const uint32_t wave = (uint32_t)tid / 64, lane = (uint32_t)tid % 64;
     const uint32_t m_lane = wave / WN * (FM * 16) + lane % 16, n_lane = wave % WN * (FN * 16) + lane / 16 * 4;   // in the tile
-    char *here = lds + r.iter % 2 * kBuffer, *next = lds + (r.iter + 1) % 2 * kBuffer;
-    const uint32_t k0 = r.k_begin + r.iter * kStage;
-    if constexpr (PH == 0) {
-      if (k0 < r.k_end) {
-        check_multiply(here, tid, r);
-        multiply(here, 0, tid, r, [](int) {});
-      }
-      if constexpr (DIRECT) direct_done();
-      else if (k0 + kStage < r.k_end) keep(next, tid, r);
-    } else if constexpr (PH == 1) {
-      const bool more = k0 + 2 * kStage < r.k_end;
-      if constexpr (DIRECT) {
-        const Bring bring(a, k0 + 2 * kStage, here, more, tid, r);
+    if constexpr (PH < 2) {
+      char *here = lds + r.iter % 2 * kBuffer, *next = lds + (r.iter + 1) % 2 * kBuffer;
+      const uint32_t k0 = r.k_begin + r.iter * kStage;
+      if constexpr (PH == 0) {
+        if (k0 < r.k_end) multiply(here, 0, tid, r, [](int) {});
+        if constexpr (DIRECT) direct_done();
+        else if (k0 + kStage < r.k_end) keep(next, tid, r);
+      } else if constexpr (DIRECT) {
+        const Bring bring(a, k0 + 2 * kStage, here, k0 + 2 * kStage < r.k_end, tid, r);
         if (k0 < r.k_end)
           multiply(next, 1, tid, r, [&](int i) {
             // (each behind some products: in front of them all, the matrix unit waited for their issue)
@@ -712,7 +732,7 @@ struct Gemm {
             }
           });
       } else {
-        if (more) fetch(a, k0 + 2 * kStage, tid, r);
+        if (k0 + 2 * kStage < r.k_end) fetch(a, k0 + 2 * kStage, tid, r);
         if (k0 < r.k_end) multiply(next, 1, tid, r, [](int) {});
       }
     } else if constexpr (EPI != kEpiStats) {
@@ -858,6 +878,31 @@ struct GemmJoin {
     if (a.bias) load_row(static_cast<const T*>(a.bias) + n, a.N - n, bias);
     const uint32_t at_m[1] = {(uint32_t)m};
     finish<T>(a, at_m, n, bias, v);
+  }
+};
+
+// A matrix of 16-bit numbers with rows that start on 16 bytes: eight numbers per thread.
+struct PackArgs {
+  const void* from;
+  size_t ld_from;
+  void* to;
+  size_t ld_to;               // a multiple of 8
+  uint32_t rows, cols;
+  size_t pieces;              // rows * ld_to / 8
+};
+struct PackRows {
+  static constexpr int kThreads = 256;
+  static constexpr int kPhases = 1;
+  struct Regs {};
+  template <int PH>
+  HCNN_HD static void phase(const PackArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
+    typedef GemmOperand<Half, kAlongK, 16, 64> Op;
+    const size_t at = (size_t)bid * kThreads + tid;
+    if (at >= a.pieces) return;
+    const size_t each = a.ld_to / 8, row = at / each;
+    const uint32_t c = (uint32_t)(at - row * each) * 8;
+    const U4 v = Op::piece(static_cast<const Half*>(a.from), row * a.ld_from + c, (a.rows - 1) * a.ld_from + a.cols);
+    *reinterpret_cast<U4*>(static_cast<Half*>(a.to) + row * a.ld_to + c) = Op::first(v, a.cols - c < 8 ? a.cols - c : 8);
   }
 };
 

@@ -14,7 +14,8 @@
 // a GPU) runs the same phase bodies as plain loops over blocks and threads; it is
 // a checker for the kernel sources, not a product path, and the Python binding
 // never loads it.
-// Optional: begin(args, block, tid, lds, regs)   runs before the repeated phases, with a barrier behind it
+// Optional: begin(args, block, tid, lds, regs)   runs before the repeated phases, with a barrier behind it; then begin_next, where
+//                               there is one, with another
 // Optional: skip(args, block)   true: the workgroup has nothing to do (the same answer for all of its threads)
 // Optional: wave_sync(ph)       true: up to the next barrier the phases after ph touch only LDS words that no other
 //                               wave touches in between, and no barrier stands after ph (of the last repeated phase: in front
@@ -187,6 +188,8 @@ template <class K, class = void> struct WaveSync { static constexpr bool after(i
 template <class K> struct WaveSync<K, std::void_t<decltype(K::wave_sync(0))>> { static constexpr bool after(int ph) { return K::wave_sync(ph); } };
 template <class K, class = void> struct HasBegin : std::false_type {};
 template <class K> struct HasBegin<K, std::void_t<decltype(&K::begin)>> : std::true_type {};
+template <class K, class = void> struct HasBeginNext : std::false_type {};
+template <class K> struct HasBeginNext<K, std::void_t<decltype(&K::begin_next)>> : std::true_type {};
 template <class K, class = void> struct HasSkip : std::false_type {};
 template <class K> struct HasSkip<K, std::void_t<decltype(&K::skip)>> : std::true_type {};
 template <class K, class = void> struct LoopPhases { static constexpr int value = 0; };
@@ -269,6 +272,8 @@ int launch(hcnn_stream_t, size_t grid, size_t lds_bytes, const Args& a) {
       regs.assign(K::kThreads, typename K::Regs{});
       for (int tid = 0; tid < K::kThreads; ++tid) K::begin(a, (unsigned)bid, tid, lds.data(), regs[tid]);
     }
+    if constexpr (HasBeginNext<K>::value)
+      for (int tid = 0; tid < K::kThreads; ++tid) K::begin_next(a, (unsigned)bid, tid, lds.data(), regs[tid]);
     bool up = true;                                    // waves in ascending, then in descending order
     for (size_t s = 0; s < steps.size(); s = steps[s].next, up = !up)
       for (int w = 0; w < waves; ++w)
@@ -359,6 +364,10 @@ __global__ void __launch_bounds__(K::kThreads, MinWavesPerSimd<K>::value) kernel
   constexpr int LP = LoopPhases<K>::value;
   if constexpr (HasBegin<K>::value) {
     K::begin(a, blockIdx.x, (int)threadIdx.x, hcnn_lds, regs);
+    __syncthreads();
+  }
+  if constexpr (HasBeginNext<K>::value) {
+    K::begin_next(a, blockIdx.x, (int)threadIdx.x, hcnn_lds, regs);
     __syncthreads();
   }
   if constexpr (LP > 0) {
