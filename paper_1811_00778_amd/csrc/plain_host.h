@@ -4,6 +4,7 @@
 #include "../../include/hcnn.h"
 
 #include <algorithm>
+#include <cmath>
 #include <new>
 
 #include "plain_kernels.h"
@@ -61,23 +62,33 @@ enum { kTile256, kTile128, kTile64, kTall, kFlat };
 struct Shape { int tile; uint32_t bm, bn, splits; bool direct; };
 constexpr uint32_t kTileRows[] = {256, 128, 64, 128, 16}, kTileCols[] = {256, 128, 64, 16, 128};
 
+// Tile and parts of k by an estimate of the time in us: `load` workgroups for each compute unit, `held` of them at a time; a stage takes
+// what the unit's matrix instructions and LDS need for it (kFull, per workgroup) or a load's way (kAlone), whichever is more; a
+// workgroup's beginning and ending kEnds; parts of k are written and joined.
 template <class T>
 Shape choose(const hcnn_plain* h, size_t M, size_t N, size_t K, bool may_split, bool direct) {
-  const size_t units = h->compute_units;
-  auto tiles = [&](int t) { return blocks(M, kTileRows[t]) * blocks(N, kTileCols[t]); };
-  int t = kTile64;
-  if (N <= 16) t = kTall;
-  else if (M <= 16) t = kFlat;
-  else if (sizeof(T) == 2 && direct && tiles(kTile256) * 4 >= units * 3) t = kTile256;
-  else if (tiles(kTile128) * 2 >= units) t = kTile128;
-  Shape s{t, kTileRows[t], kTileCols[t], 1, direct};
-  if (may_split) {
-    // parts of at least four stages while there are fewer workgroups than two for each compute unit
-    const size_t stages = blocks(K, GemmNum<T>::kStage), want = blocks(2 * units, std::max<size_t>(1, tiles(t)));
-    const size_t most = std::max<size_t>(1, stages / 4);
-    s.splits = (uint32_t)std::max<size_t>(1, std::min(tiles(t) >= units ? 1 : want, most));
+  constexpr bool wide = sizeof(T) == 4;
+  constexpr double kFull[] = {1.5, wide ? 1.9 : 0.55, wide ? 0.5 : 0.2, wide ? 0.3 : 0.12, wide ? 0.3 : 0.12};
+  constexpr double kHeld[] = {1, 2, 4, 4, 4}, kEnds[] = {10, 6, 4, 4, 4}, kAlone = 0.7;
+  const double units = h->compute_units;
+  const size_t stages = std::max<size_t>(1, blocks(K, GemmNum<T>::kStage));
+  Shape best{kTile64, 64, 64, 1, direct};
+  double least = 1e300;
+  for (int t = kTile256; t <= kFlat; ++t) {
+    if (t == kTile256 && (wide || !direct)) continue;
+    const size_t tiles = std::max<size_t>(1, blocks(M, kTileRows[t]) * blocks(N, kTileCols[t]));
+    for (size_t s = 1; s == 1 || (may_split && s * 2 <= stages && s <= 64); s += s < 4 ? 1 : s / 2) {
+      const double load = std::ceil((double)(tiles * s) / units), turns = std::ceil(load / kHeld[t]);
+      const double stage = std::max(kAlone * turns, load * kFull[t]) * (direct ? 1.0 : 1.6);
+      double us = (double)blocks(stages, s) * stage + turns * kEnds[t];
+      if (s > 1) us += 5.0 + (double)(2 * s * M * N * 4) / 3e6;
+      if (us < least) {
+        least = us;
+        best = Shape{t, kTileRows[t], kTileCols[t], (uint32_t)s, direct};
+      }
+    }
   }
-  return s;
+  return best;
 }
 inline size_t sums_bytes(const Shape& s, size_t M, size_t N) { return s.splits > 1 ? s.splits * M * up(N, 8) * 4 : 0; }
 
@@ -85,8 +96,7 @@ template <class G>
 int start(hcnn_plain* h, const GemmArgs& a, size_t grid) { return launch<G>(h->stream, grid, G::kLdsBytes, a); }
 
 // An operand as the caller has it, or a copy of it in the work memory whose rows all start on 16 bytes, as whole stages' way to LDS
-// past the registers needs them (also: offsets within a launch constant in 32 bits, of a stage's rows or, where its rows are
-// gathered, of the whole operand).
+// past the registers needs them (also: offsets within a stage in 32 bits).
 struct Input {
   const void* p;
   size_t ld, rows, cols;
@@ -95,16 +105,16 @@ struct Input {
   size_t extent() const { return rows && cols ? (rows - 1) * ld + cols : 0; }
 };
 template <class T>
-bool direct_input(const Input& x, bool gathered) {
+bool direct_input(const Input& x) {
   const bool aligned = x.packed || (reinterpret_cast<uintptr_t>(x.p) % 16 == 0 && x.ld * sizeof(T) % 16 == 0);
-  return aligned && (gathered ? x.extent() : 257 * x.ld) * sizeof(T) < ((size_t)1 << 32);
+  return aligned && 257 * x.ld * sizeof(T) < ((size_t)1 << 32);
 }
 // Copies pay from some size of the products that take the operand on: `work` = M N K of all of them.  By measurement (bfloat16,
 // M = N = K, us with / without copies of both operands): see kPackWork.
 constexpr double kPackWork = 3e-15, kPackByte = 5e-13, kPackLaunch = 5e-6;
 template <class T>
 void plan_pack(Input& x, Arena& a, double work) {
-  if (sizeof(T) != 2 || direct_input<T>(x, false) || x.rows == 0 || x.cols == 0) return;
+  if (sizeof(T) != 2 || direct_input<T>(x) || x.rows == 0 || x.cols == 0) return;
   if (work * kPackWork < kPackLaunch + 4.0 * (double)x.rows * (double)x.cols * kPackByte) return;
   x.packed = true;
   x.ld = up(x.cols, 8);
@@ -164,7 +174,7 @@ int linear(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void* x, 
   const double work = (double)M * (double)N * (double)K;
   plan_pack<T>(ix, ar, work);
   plan_pack<T>(iw, ar, work);
-  const Shape s = choose<T>(h, M, N, K, true, direct_input<T>(ix, false) && direct_input<T>(iw, false));
+  const Shape s = choose<T>(h, M, N, K, true, direct_input<T>(ix) && direct_input<T>(iw));
   const size_t o_sums = ar.take(sums_bytes(s, M, N));
   int e = reserve(h, ar.bytes);
   if (e || (e = pack<T>(h, ix, x, ldx)) || (e = pack<T>(h, iw, w, ldw))) return e;
@@ -213,8 +223,8 @@ int linear_grad(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void
   }
   if (dw) plan_pack<T>(ix, ar, work);
   if (dx) plan_pack<T>(iw, ar, work);
-  const bool direct = direct_input<T>(idz, false);
-  const Shape sx = choose<T>(h, M, K, N, true, direct && direct_input<T>(iw, false)), sw = choose<T>(h, N, K, M, true, direct && direct_input<T>(ix, false));
+  const bool direct = direct_input<T>(idz);
+  const Shape sx = choose<T>(h, M, K, N, true, direct && direct_input<T>(iw)), sw = choose<T>(h, N, K, M, true, direct && direct_input<T>(ix));
   const size_t o_part = ar.take(db ? row_blocks * ag.ld_part * 4 : 0);
   const size_t o_sums = ar.take(std::max(dx ? sums_bytes(sx, M, K) : 0, dw ? sums_bytes(sw, N, K) : 0));
   int e = reserve(h, ar.bytes);
@@ -273,14 +283,17 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
   const double work = (double)M * (double)V * (double)K * (grad ? 3 : 1);
   plan_pack<T>(ix, a, work);
   plan_pack<T>(iw, a, work);
+  // the rows that take part, one behind the other: used where they are not all rows, or where x is copied anyway
+  Input ikept{c.x, up(K, 16 / sizeof(T)), M, K, true, ix.offset};
+  if (!ix.packed) ikept.offset = a.take(M * ikept.ld * sizeof(T));
   // columns of a piece: whole tiles, all columns where they fit
   const size_t fit = kDeltaBytes / (std::max<size_t>(M, 1) * sizeof(T)) / 256 * 256;
   const size_t piece = grad ? std::min(V, std::max<size_t>(fit, 256)) : 0;
   const size_t pieces = grad ? blocks(V, piece) : 0, ld_delta = up(piece, 16 / sizeof(T));
-  const bool direct_x = direct_input<T>(ix, true), direct_w = direct_input<T>(iw, false);
+  const bool direct_x = direct_input<T>(ix), direct_w = direct_input<T>(iw);
   const Shape ss = choose<T>(h, M, V, K, false, direct_x && direct_w);
   Input idelta{nullptr, ld_delta, M, piece, true, a.take(grad ? M * ld_delta * sizeof(T) : 0)};
-  const bool direct_d = direct_input<T>(idelta, false);
+  const bool direct_d = direct_input<T>(idelta);
   const Shape sx = choose<T>(h, M, K, piece, pieces == 1, direct_d && direct_w), sw = choose<T>(h, piece, K, M, true, direct_d && direct_x);
   const size_t tiles = blocks(V, ss.bn), ld_stats = up(M, 64), row_wgs = blocks(M, RowStats::kRows);
   const size_t o_count = a.take(4), o_alpha = a.take(4), o_rows = a.take(M * 4), o_target = a.take(M * 4), o_score = a.take(M * 4), o_lse = a.take(M * 4);
@@ -288,20 +301,22 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
   const size_t o_dx = a.take(pieces > 1 && c.dx ? M * up(K, 8) * 4 : 0);
   const size_t o_sums = a.take(grad ? std::max(c.dx ? sums_bytes(sx, M, K) : 0, c.dw ? sums_bytes(sw, piece, K) : 0) : 0);
   int e = reserve(h, a.bytes);
-  if (e || (e = pack<T>(h, ix, c.x, c.ldx)) || (e = pack<T>(h, iw, c.w, c.ldw))) return e;
+  if (e || (e = pack<T>(h, iw, c.w, c.ldw))) return e;
   idelta.p = at<void>(h, idelta.offset);
   uint32_t *count = at<uint32_t>(h, o_count), *rows = at<uint32_t>(h, o_rows), *target = at<uint32_t>(h, o_target);
   float *alpha = at<float>(h, o_alpha), *score = at<float>(h, o_score), *lse = at<float>(h, o_lse);
 
   KeepRowsArgs kr{c.targets, c.target_bytes == 8, c.ignore, (uint32_t)M, (uint32_t)V, rows, target, count, h->d_bad};
   if ((e = launch<KeepRows>(h->stream, 1, KeepRows::kLdsBytes, kr))) return e;
-  if (M && (c.row_loss || c.row_lse || (c.dx && K))) {
-    const BlankRowsArgs br{kr, c.dx, c.ld_dx * sizeof(T), K * sizeof(T), c.row_loss, c.row_lse};
-    if ((e = launch<BlankRows>(h->stream, blocks(M, 4), 0, br))) return e;
+  if (M) {
+    const SortRowsArgs sr{kr, K ? c.dx : nullptr, c.ld_dx * sizeof(T), K * sizeof(T), c.row_loss, c.row_lse,
+                          c.x, c.ldx * sizeof(T), at<void>(h, ikept.offset), ikept.ld * sizeof(T), ix.packed};
+    if ((e = launch<SortRows>(h->stream, blocks(M, 4), 0, sr))) return e;
   }
+  if (ix.packed) ix.p = at<void>(h, ikept.offset);
   GemmArgs g = operands(ix, iw);
   g.M = (uint32_t)M; g.N = (uint32_t)V; g.K = (uint32_t)K;
-  g.rows = rows; g.count = count; g.gather = kGatherA; g.count_of = kCountM;
+  g.count = count; g.count_of = kCountM; g.kept = at<void>(h, ikept.offset); g.ld_kept = ikept.ld; g.kept_always = ix.packed;
   g.stats = at<float>(h, o_stats); g.ld_stats = ld_stats; g.target = target; g.target_score = score; g.lse = lse;
   g.delta_scale = delta_scale<T>();
   if (M) {
@@ -326,13 +341,13 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
     if (c.dx && M && K) {
       GemmArgs d = operands(idelta, wp);
       d.M = (uint32_t)M; d.N = (uint32_t)K; d.K = (uint32_t)n;
-      d.rows = rows; d.count = count; d.count_of = kCountM;
+      d.count = count; d.count_of = kCountM;
       if (p) { d.addend = at<float>(h, o_dx); d.ld_sums = up(K, 8); }
       if (p + 1 < pieces) {
         d.sums = at<float>(h, o_dx); d.ld_sums = up(K, 8);
         if ((e = gemm<T, kAlongK, kAcrossK, kEpiSums>(h, d, sx))) return e;
       } else {
-        d.gather = kScatterOut; d.alpha = alpha;
+        d.rows = rows; d.alpha = alpha;
         d.out = c.dx; d.ld_out = c.ld_dx;
         if ((e = product<T, kAlongK, kAcrossK>(h, d, sx, at<float>(h, o_sums)))) return e;
       }
@@ -340,7 +355,7 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
     if (c.dw && K) {
       GemmArgs d = operands(idelta, ix);
       d.M = (uint32_t)n; d.N = (uint32_t)K; d.K = (uint32_t)M;
-      d.rows = rows; d.count = count; d.count_of = kCountK; d.gather = kGatherB; d.alpha = alpha;
+      d.count = count; d.count_of = kCountK; d.kept = at<void>(h, ikept.offset); d.ld_kept = ikept.ld; d.kept_always = ix.packed; d.alpha = alpha;
       d.out = static_cast<char*>(c.dw) + v0 * c.ld_dw * sizeof(T); d.ld_out = c.ld_dw;
       if ((e = product<T, kAcrossK, kAcrossK>(h, d, sw, at<float>(h, o_sums)))) return e;
     }

@@ -227,7 +227,6 @@ HCNN_HD float slope_of(float z, int act) {
 // 4 g .. 4 g + 3 (32 bits) of a row, g = lane / 16; both operands use the same order, so that the sum is the same whatever the instruction
 // calls these k.  b is the first operand: a lane then holds four consecutive n of a row m = lane mod 16.
 enum { kAlongK = 0, kAcrossK = 1 };
-enum { kGatherA = 1, kGatherB = 2, kScatterOut = 4 };      // which index goes through GemmArgs::rows: a's m, b's k, the output's m
 enum { kCountNone = 0, kCountM = 1, kCountK = 2 };         // what GemmArgs::count limits
 
 struct GemmArgs {
@@ -235,9 +234,12 @@ struct GemmArgs {
   size_t lda, ldb;             // numbers from one stored row to the next
   size_t a_extent, b_extent;   // numbers from the first to the last one that exists, inclusive
   uint32_t M, N, K;
-  const uint32_t* rows;        // indices for `gather`
   const uint32_t* count;       // device count of the rows that take part, see count_of
-  uint32_t gather, count_of;
+  uint32_t count_of;
+  const void* kept;            // the operand with those rows only (a with kCountM, b with kCountK), read where they are not all rows
+  size_t ld_kept;
+  uint32_t kept_always;        // ... or in any case
+  const uint32_t* rows;        // row of the output that m goes to (null: m)
   uint32_t splits;             // parts of k, each summed by workgroups of its own
   // what becomes of the sums
   float* sums;                 // [splits][M][ld_sums] where kEpiSums
@@ -267,7 +269,7 @@ HCNN_HD void finish(const GemmArgs& a, const uint32_t (&m)[B], uint32_t n, const
   float r[B][W];
 #pragma unroll
   for (int i = 0; i < B; ++i) {
-    row[i] = a.gather & kScatterOut && m[i] != ~0u ? a.rows[m[i]] : m[i];
+    row[i] = a.rows && m[i] != ~0u ? a.rows[m[i]] : m[i];
     if (a.residual && m[i] != ~0u) load_row(static_cast<const T*>(a.residual) + row[i] * a.ld_residual + n, left, r[i]);
   }
   if (a.alpha) {
@@ -341,13 +343,12 @@ struct GemmOperand {
   }
   // Pieces of the stage that begins at k0, of the rows from x0 on.  Rows beyond X and what lies beyond them may hold anything (their sums
   // are dropped), k beyond K are 0 in both operands.
-  HCNN_HD static void load(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, const uint32_t* rows, uint32_t x0, uint32_t k0,
-                           int tid, U4 (&r)[kEach]) {
+  HCNN_HD static void load(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, uint32_t x0, uint32_t k0, int tid, U4 (&r)[kEach]) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i)
-      if (mine(tid, i)) r[i] = load_one(p, ld, extent, X, K, rows, x0, k0, (uint32_t)(tid + i * THREADS));
+      if (mine(tid, i)) r[i] = load_one(p, ld, extent, X, K, x0, k0, (uint32_t)(tid + i * THREADS));
   }
-  HCNN_HD static U4 load_one(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, const uint32_t* rows, uint32_t x0, uint32_t k0, uint32_t c) {
+  HCNN_HD static U4 load_one(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, uint32_t x0, uint32_t k0, uint32_t c) {
     const uint32_t line = c / kRowPieces, at = c % kRowPieces * kPer16;
     U4 v{};
     {
@@ -356,25 +357,23 @@ struct GemmOperand {
         if (x >= X) x = X - 1;
         const uint32_t k = k0 + at;
         if (k < K) {
-          const size_t row = rows ? rows[x] : x;
-          v = piece(p, row * ld + k, extent);
+          v = piece(p, x * ld + k, extent);
           if (K - k < kPer16) v = first(v, K - k);
         }
       } else {
         const uint32_t k = k0 + line, x = x0 + at;
         if (k < K && x < X) {
-          const size_t row = rows ? rows[k] : k;
-          v = piece(p, row * ld + x, extent);
+          v = piece(p, k * ld + x, extent);
         }
       }
     }
     return v;
   }
   // ... straight to LDS, one piece after the other: for the one stage of a sum that is not whole, where registers are dear
-  HCNN_HD static void copy(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, const uint32_t* rows, uint32_t x0, uint32_t k0, char* lds, int tid) {
+  HCNN_HD static void copy(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, uint32_t x0, uint32_t k0, char* lds, int tid) {
 #pragma unroll 1
     for (uint32_t c = (uint32_t)tid; c < (uint32_t)kPieces; c += THREADS)
-      *reinterpret_cast<U4*>(lds + place(c / kRowPieces, c % kRowPieces)) = load_one(p, ld, extent, X, K, rows, x0, k0, c);
+      *reinterpret_cast<U4*>(lds + place(c / kRowPieces, c % kRowPieces)) = load_one(p, ld, extent, X, K, x0, k0, c);
   }
   HCNN_HD static uint32_t place(uint32_t line, uint32_t pc) {                  // byte of piece pc of stored row `line`
     if constexpr (LAYOUT == kAlongK) return line * 128 + ((pc ^ (line & 7)) << 4);
@@ -402,53 +401,33 @@ struct GemmOperand {
     else if constexpr (sizeof(T) == 2) return ((pc / 2 ^ swap(line)) * 2 + pc % 2) * kPer16;
     else return ((pc / 4 ^ swap(line)) * 4 + pc % 4) * kPer16;
   }
-  // Byte offsets of a thread's pieces from direct_base, for the whole sum (kAcrossK with gathered rows: of the numbers within the row).
-  // Rows beyond X read a row that exists, pieces beyond X the row's first one.
-  HCNN_HD static void direct_offsets(size_t ld, uint32_t X, const uint32_t* rows, uint32_t x0, int tid, uint32_t (&off)[kEach]) {
+  // Byte offsets of a thread's pieces from direct_base, for the whole sum.  Rows beyond X read a row that exists, pieces beyond X the
+  // row's first one.
+  HCNN_HD static void direct_offsets(size_t ld, uint32_t X, uint32_t x0, int tid, uint32_t (&off)[kEach]) {
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       if (!mine(tid, i)) continue;
       const uint32_t c = (uint32_t)(tid + i * THREADS), line = c / kRowPieces, at = numbers(c);
       if constexpr (LAYOUT == kAlongK) {
-        const uint32_t x = x0 + line < X ? x0 + line : X - 1;
-        off[i] = (uint32_t)(((rows ? (size_t)rows[x] : (size_t)(x - x0)) * ld + at) * sizeof(T));
+        const uint32_t x = x0 + line < X ? line : X - 1 - x0;
+        off[i] = (uint32_t)((x * ld + at) * sizeof(T));
       } else {
-        const uint32_t in_row = x0 + at < X ? at : 0;
-        off[i] = (uint32_t)(((rows ? 0 : line * ld) + in_row) * sizeof(T));
+        off[i] = (uint32_t)((line * ld + (x0 + at < X ? at : 0)) * sizeof(T));
       }
     }
   }
-  HCNN_HD static const T* direct_base(const T* p, size_t ld, const uint32_t* rows, uint32_t x0, uint32_t k0) {
-    if constexpr (LAYOUT == kAlongK) return p + (rows ? 0 : x0 * ld) + k0;
-    else return p + (rows ? 0 : k0 * ld) + x0;
+  HCNN_HD static const T* direct_base(const T* p, size_t ld, uint32_t x0, uint32_t k0) {
+    if constexpr (LAYOUT == kAlongK) return p + x0 * ld + k0;
+    else return p + k0 * ld + x0;
   }
   // May the stage at k0 be read whole?  Its k exist, and a last piece that reaches beyond the row's numbers reads memory of the operand.
-  HCNN_HD static bool direct_stage(size_t ld, size_t extent, uint32_t X, uint32_t K, const uint32_t* rows, uint32_t k0) {
+  HCNN_HD static bool direct_stage(size_t ld, size_t extent, uint32_t X, uint32_t K, uint32_t k0) {
     if (k0 + kStage > K) return false;
     if constexpr (LAYOUT == kAlongK) return true;
-    if (X % kPer16 == 0) return true;
-    const size_t last = rows ? wave_uniform(rows[k0 + kStage - 1]) : k0 + kStage - 1;      // (gathered rows ascend)
-    return last * ld + X / kPer16 * kPer16 + kPer16 <= extent;
+    return X % kPer16 == 0 || (size_t)(k0 + kStage - 1) * ld + X / kPer16 * kPer16 + kPer16 <= extent;
   }
-  HCNN_HD static void direct(const T* base, size_t ld, const uint32_t* rows, uint32_t k0, char* lds, int tid, int i, const uint32_t (&off)[kEach]) {
-    if (!mine(tid, i)) return;
-    uint32_t o = off[i];
-    if (LAYOUT == kAcrossK && rows) o += (uint32_t)(row_at(rows, k0, tid, i) * ld * sizeof(T));
-    to_lds(base, o, lds + ((tid & ~63) + i * THREADS) * 16, tid & 63);
-  }
-  // The gathered row of a thread's piece.  A wave's pieces lie in few rows: their indices come by scalar loads, since a vector load in the
-  // middle of the stages would be waited for together with all stages on their way.
-  HCNN_HD static uint32_t row_at(const uint32_t* rows, uint32_t k0, int tid, int i) {
-    constexpr uint32_t kLines = 64 / kRowPieces;                                // stored rows of a wave's pieces
-    if constexpr (LAYOUT == kAcrossK && kRowPieces <= 64 && kLines <= 4) {
-      const uint32_t first = k0 + wave_uniform((uint32_t)(tid & ~63) + i * THREADS) / kRowPieces, mine = (uint32_t)(tid & 63) / kRowPieces;
-      uint32_t row = ldc(rows, first);
-#pragma unroll
-      for (uint32_t l = 1; l < kLines; ++l) row = mine == l ? ldc(rows, first + l) : row;
-      return row;
-    } else {
-      return rows[k0 + (tid + i * THREADS) / kRowPieces];
-    }
+  HCNN_HD static void direct(const T* base, char* lds, int tid, int i, const uint32_t (&off)[kEach]) {
+    if (mine(tid, i)) to_lds(base, off[i], lds + ((tid & ~63) + i * THREADS) * 16, tid & 63);
   }
   // 16 bytes of every lane of a wave to LDS, side by side
   HCNN_HD static void to_lds(const T* base, uint32_t off, char* lds, int lane) {
@@ -553,7 +532,8 @@ struct Gemm {
   struct Regs {
     uint32_t iter;
     uint32_t m0, n0, k_begin, k_end, M, split;
-    const uint32_t *ga, *gb;                     // indices of gathered rows; null where all rows take part: they are in order
+    const T *a, *b;
+    size_t lda, ldb, a_extent, b_extent;
     U4 ra[A::kEach], rb[B::kEach];               // the next stage, unless DIRECT
     uint32_t oa[A::kEach], ob[B::kEach];         // DIRECT: offsets of the pieces
     Step step;
@@ -590,16 +570,20 @@ struct Gemm {
     at -= band * kBand * tn;
     r.m0 = (band * kBand + at % high) * BM;
     r.n0 = at / high * BN;
-    const bool some = a.count_of != kCountNone && wave_uniform(*a.count) < (a.count_of == kCountM ? a.M : a.K);
-    r.ga = some && (a.gather & kGatherA) ? a.rows : nullptr;
-    r.gb = some && (a.gather & kGatherB) ? a.rows : nullptr;
+    const bool kept = a.kept && (a.kept_always || wave_uniform(*a.count) < (a.count_of == kCountM ? a.M : a.K));
+    r.a = static_cast<const T*>(kept && a.count_of == kCountM ? a.kept : a.a);
+    r.b = static_cast<const T*>(kept && a.count_of == kCountK ? a.kept : a.b);
+    r.lda = kept && a.count_of == kCountM ? a.ld_kept : a.lda;
+    r.ldb = kept && a.count_of == kCountK ? a.ld_kept : a.ldb;
+    r.a_extent = kept && a.count_of == kCountM ? (a.M - 1) * a.ld_kept + a.K : a.a_extent;
+    r.b_extent = kept && a.count_of == kCountK ? (a.K - 1) * a.ld_kept + a.N : a.b_extent;
     const uint32_t K = counted(a, kCountK, a.K), run = loop_count(a) * kStage;
     r.k_begin = r.split * run;
     r.k_end = K < r.k_begin + run ? K : r.k_begin + run;
   }
   HCNN_HD static void fetch(const GemmArgs& a, uint32_t k0, int tid, Regs& r) {
-    A::load(static_cast<const T*>(a.a), a.lda, a.a_extent, r.M, r.k_end, r.ga, r.m0, k0, tid, r.ra);
-    B::load(static_cast<const T*>(a.b), a.ldb, a.b_extent, a.N, r.k_end, r.gb, r.n0, k0, tid, r.rb);
+    A::load(r.a, r.lda, r.a_extent, r.M, r.k_end, r.m0, k0, tid, r.ra);
+    B::load(r.b, r.ldb, r.b_extent, a.N, r.k_end, r.n0, k0, tid, r.rb);
   }
   HCNN_HD static void keep(char* lds, int tid, const Regs& r) {
     A::store(lds, tid, r.ra);
@@ -608,25 +592,23 @@ struct Gemm {
   // The stage at k0 to LDS, past the registers where it may be read whole: then in kDirect pieces that the caller spreads out
   static constexpr int kDirect = A::kEach + B::kEach;
   struct Bring {
-    const GemmArgs& a;
     const T *pa, *pb;
     char* lds;
-    uint32_t k0;
     bool whole;
-    HCNN_HD Bring(const GemmArgs& args, uint32_t k, char* to, bool wanted, int tid, Regs& r) : a(args), lds(to), k0(k), whole(false) {
+    HCNN_HD Bring(const GemmArgs& a, uint32_t k0, char* to, bool wanted, int tid, const Regs& r) : lds(to), whole(false) {
       if (!wanted) return;
-      whole = A::direct_stage(a.lda, a.a_extent, r.M, r.k_end, r.ga, k0) && B::direct_stage(a.ldb, a.b_extent, a.N, r.k_end, r.gb, k0);
-      pa = A::direct_base(static_cast<const T*>(a.a), a.lda, r.ga, r.m0, k0);
-      pb = B::direct_base(static_cast<const T*>(a.b), a.ldb, r.gb, r.n0, k0);
+      whole = A::direct_stage(r.lda, r.a_extent, r.M, r.k_end, k0) && B::direct_stage(r.ldb, r.b_extent, a.N, r.k_end, k0);
+      pa = A::direct_base(r.a, r.lda, r.m0, k0);
+      pb = B::direct_base(r.b, r.ldb, r.n0, k0);
       if (whole) return;
-      A::copy(static_cast<const T*>(a.a), a.lda, a.a_extent, r.M, r.k_end, r.ga, r.m0, k0, lds, tid);
-      B::copy(static_cast<const T*>(a.b), a.ldb, a.b_extent, a.N, r.k_end, r.gb, r.n0, k0, lds + A::kLdsBytes, tid);
+      A::copy(r.a, r.lda, r.a_extent, r.M, r.k_end, r.m0, k0, lds, tid);
+      B::copy(r.b, r.ldb, r.b_extent, a.N, r.k_end, r.n0, k0, lds + A::kLdsBytes, tid);
     }
-    HCNN_HD void piece(int i, int tid, Regs& r) const {
-      if (i < A::kEach) A::direct(pa, a.lda, r.ga, k0, lds, tid, i, r.oa);
-      else B::direct(pb, a.ldb, r.gb, k0, lds + A::kLdsBytes, tid, i - A::kEach, r.ob);
+    HCNN_HD void piece(int i, int tid, const Regs& r) const {
+      if (i < A::kEach) A::direct(pa, lds, tid, i, r.oa);
+      else B::direct(pb, lds + A::kLdsBytes, tid, i - A::kEach, r.ob);
     }
-    HCNN_HD void all(int tid, Regs& r) const {
+    HCNN_HD void all(int tid, const Regs& r) const {
       if (!whole) return;
 #pragma unroll
       for (int i = 0; i < kDirect; ++i) piece(i, tid, r);
@@ -635,8 +617,8 @@ struct Gemm {
   HCNN_HD static void begin(const GemmArgs& a, unsigned bid, int tid, uint32_t* lds, Regs& r) {
     place(a, bid, r);
     if constexpr (DIRECT) {
-      A::direct_offsets(a.lda, r.M, r.ga, r.m0, tid, r.oa);
-      B::direct_offsets(a.ldb, a.N, r.gb, r.n0, tid, r.ob);
+      A::direct_offsets(r.lda, r.M, r.m0, tid, r.oa);
+      B::direct_offsets(r.ldb, a.N, r.n0, tid, r.ob);
     }
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -1018,6 +1000,7 @@ struct KeepRows {
     const uint32_t m0 = (uint32_t)tid * each < a.M ? tid * each : a.M, m1 = a.M - m0 < each ? a.M : m0 + each;
     if constexpr (PH == 0) {
       uint32_t n = 0;
+#pragma unroll 8
       for (uint32_t m = m0; m < m1; ++m) {
         const int64_t t = target(a, m);
         if (kept(a, t)) ++n;
@@ -1036,6 +1019,7 @@ struct KeepRows {
       for (int i = 0; i < tid / 32; ++i) at += lds[kThreads + i];
       for (int i = tid / 32 * 32; i < tid; ++i) at += lds[i];
       if (tid == kThreads - 1) *a.count = at + r.mine;
+#pragma unroll 8
       for (uint32_t m = m0; m < m1; ++m) {
         const int64_t t = target(a, m);
         if (!kept(a, t)) continue;
@@ -1139,30 +1123,46 @@ struct MeanLoss {
     }
   }
 };
-// Rows that do not take part: zeros in the gradient, and in the losses and statistics asked for.  One row per 64 threads.
-struct BlankRowsArgs {
+// Rows that do not take part: zeros in the gradient, and in the losses and statistics asked for.  Rows that do: a copy of theirs in x one
+// behind the other, where they are not all rows or the copy is wanted in any case.  64 threads per row.
+struct SortRowsArgs {
   KeepRowsArgs keep;
   void* dx;                   // null: none
   size_t ld_dx;               // bytes
   size_t row_bytes;
   float *row_loss, *row_lse;
+  const void* x;
+  size_t ld_x;                // bytes
+  void* kept;
+  size_t ld_kept;             // bytes, a multiple of 16
+  uint32_t always;
 };
-struct BlankRows {
+struct SortRows {
   static constexpr int kThreads = 256;
   static constexpr int kPhases = 1;
   struct Regs {};
   template <int PH>
-  HCNN_HD static void phase(const BlankRowsArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
+  HCNN_HD static void phase(const SortRowsArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
     const uint32_t m = bid * 4 + tid / 64, lane = tid % 64;
-    if (m >= a.keep.M || KeepRows::kept(a.keep, KeepRows::target(a.keep, m))) return;
-    if (lane == 0 && a.row_loss) a.row_loss[m] = 0.0f;
-    if (lane == 0 && a.row_lse) a.row_lse[m] = 0.0f;
-    if (!a.dx) return;
-    char* row = static_cast<char*>(a.dx) + m * a.ld_dx;
+    const uint32_t n = *a.keep.count;
+    if (m >= a.keep.M || (n == a.keep.M && !a.always)) return;
     const size_t whole = a.row_bytes / 16 * 16;
-    const U4 zero{};
-    for (size_t b = (size_t)lane * 16; b < whole; b += 1024) st16(row + b, zero);
-    for (size_t b = whole + (size_t)lane * 2; b < a.row_bytes; b += 128) *reinterpret_cast<uint16_t*>(row + b) = 0;
+    if (!KeepRows::kept(a.keep, KeepRows::target(a.keep, m))) {
+      if (lane == 0 && a.row_loss) a.row_loss[m] = 0.0f;
+      if (lane == 0 && a.row_lse) a.row_lse[m] = 0.0f;
+      if (a.dx) {
+        char* row = static_cast<char*>(a.dx) + m * a.ld_dx;
+        const U4 zero{};
+        for (size_t b = (size_t)lane * 16; b < whole; b += 1024) st16(row + b, zero);
+        for (size_t b = whole + (size_t)lane * 2; b < a.row_bytes; b += 128) *reinterpret_cast<uint16_t*>(row + b) = 0;
+      }
+    }
+    if (m >= n) return;
+    const char* from = static_cast<const char*>(a.x) + a.keep.rows[m] * a.ld_x;
+    char* to = static_cast<char*>(a.kept) + m * a.ld_kept;
+#pragma unroll 4
+    for (size_t b = (size_t)lane * 16; b < whole; b += 1024) st16(to + b, ld16(from + b));
+    for (size_t b = whole + (size_t)lane * 2; b < a.row_bytes; b += 128) *reinterpret_cast<uint16_t*>(to + b) = *reinterpret_cast<const uint16_t*>(from + b);
   }
 };
 
