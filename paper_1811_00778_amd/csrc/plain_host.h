@@ -154,7 +154,11 @@ int product(hcnn_plain* h, GemmArgs a, const Shape& s, float* sums) {
   a.sums = sums;
   a.ld_sums = up(a.N, 8);
   const int e = gemm<T, LA, LB, kEpiSums>(h, a, s);
-  return e ? e : launch<GemmJoin<T>>(h->stream, GemmJoin<T>::grid(a), 0, a);
+  if (e) return e;
+  // the parts side by side where there are fewer outputs than a workgroup of quads for each compute unit
+  const bool few = (size_t)a.M * blocks(a.N, 4) < (size_t)h->compute_units * 256 && s.splits >= 8;
+  if (few) return launch<GemmJoin<T, 8>>(h->stream, GemmJoin<T, 8>::grid(a), GemmJoin<T, 8>::kLdsBytes, a);
+  return launch<GemmJoin<T, 1>>(h->stream, GemmJoin<T, 1>::grid(a), 0, a);
 }
 
 inline GemmArgs operands(const Input& a, const Input& b) {
@@ -169,6 +173,13 @@ inline GemmArgs operands(const Input& a, const Input& b) {
 template <class T>
 int linear(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void* x, size_t ldx, const void* w, size_t ldw, const void* bias,
            const void* residual, size_t ld_residual, void* y, size_t ldy, void* z, size_t ldz) {
+  if (M <= 16 && blocks(N, 16) <= kMaxSize) {
+    GemmArgs g = operands(Input{x, ldx, M, K}, Input{w, ldw, N, K});
+    g.M = (uint32_t)M; g.N = (uint32_t)N; g.K = (uint32_t)K;
+    g.act = act; g.bias = bias; g.residual = residual; g.ld_residual = ld_residual;
+    g.out = y; g.ld_out = ldy; g.z = z; g.ld_z = ldz;
+    return launch<FewRows<T>>(h->stream, blocks(N, 16), FewRows<T>::kLdsBytes, g);
+  }
   Arena ar;
   Input ix{x, ldx, M, K}, iw{w, ldw, N, K};
   const double work = (double)M * (double)N * (double)K;

@@ -833,33 +833,118 @@ struct Gemm {
   }
 };
 
-// Joins the parts of k: four outputs of a row per thread.
-template <class T>
+// Joins the parts of k: four outputs of a row for SIDE threads, which share the parts.  (50 x 125 outputs of 63 parts: 9.1 us with one
+// thread each, in 7 workgroups; few outputs need the parts side by side.)
+template <class T, int SIDE>
 struct GemmJoin {
-  static constexpr int kThreads = 256;
-  static constexpr int kPhases = 1;
-  struct Regs {};
-  static size_t grid(const GemmArgs& a) { return ((size_t)a.M * ((a.N + 3) / 4) + kThreads - 1) / kThreads; }
+  static constexpr int kThreads = 256, kQuads = kThreads / SIDE;
+  static constexpr int kPhases = 2;
+  static constexpr size_t kLdsBytes = SIDE > 1 ? kThreads * 16 : 0;
+  struct Regs { float v[1][4]; };
+  static size_t grid(const GemmArgs& a) { return ((size_t)a.M * ((a.N + 3) / 4) + kQuads - 1) / kQuads; }
   template <int PH>
-  HCNN_HD static void phase(const GemmArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
-    const uint32_t quads = (a.N + 3) / 4;
-    const size_t at = (size_t)bid * kThreads + tid;
+  HCNN_HD static void phase(const GemmArgs& a, unsigned bid, int tid, uint32_t* lds_words, Regs& r) {
+    float* lds = reinterpret_cast<float*>(lds_words);              // [4][SIDE][kQuads]
+    const uint32_t quads = (a.N + 3) / 4, side = (uint32_t)tid / kQuads;
+    const size_t at = (size_t)bid * kQuads + tid % kQuads;
     const size_t m = at / quads;
     const uint32_t n = (uint32_t)(at - m * quads) * 4;
     const uint32_t M = a.count_of == kCountM && *a.count < a.M ? *a.count : a.M;
-    if (m >= M) return;
-    float v[1][4] = {};
-#pragma unroll 4
-    for (uint32_t s = 0; s < a.splits; ++s) {
-      float x[4];
-      load_row(a.sums + ((size_t)s * a.M + m) * a.ld_sums + n, x);
+    if constexpr (PH == 0) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[0][e] += x[e];
+      for (int e = 0; e < 4; ++e) r.v[0][e] = 0.0f;
+      if (m < M) {
+#pragma unroll 4
+        for (uint32_t s = side; s < a.splits; s += SIDE) {
+          float x[4];
+          load_row(a.sums + ((size_t)s * a.M + m) * a.ld_sums + n, x);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) r.v[0][e] += x[e];
+        }
+      }
+      if (SIDE > 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) lds[e * kThreads + tid] = r.v[0][e];
+    } else if (m < M && side == 0) {
+      if (SIDE > 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int l = 1; l < SIDE; ++l) r.v[0][e] += lds[e * kThreads + l * kQuads + tid];
+      float bias[4] = {};
+      if (a.bias) load_row(static_cast<const T*>(a.bias) + n, a.N - n, bias);
+      const uint32_t at_m[1] = {(uint32_t)m};
+      finish<T>(a, at_m, n, bias, r.v);
     }
-    float bias[4] = {};
-    if (a.bias) load_row(static_cast<const T*>(a.bias) + n, a.N - n, bias);
-    const uint32_t at_m[1] = {(uint32_t)m};
-    finish<T>(a, at_m, n, bias, v);
+  }
+};
+
+// out = a b^T for at most 16 rows of a, both along k: bound by reading b, once.  A workgroup takes 16 rows of b and all of k; its
+// waves take every eighth 64-byte step of k and load it straight to the registers that the products read (lane: row lane % 16, piece
+// lane / 16), kDeep steps ahead: eight waves hold 8 x kDeep KiB of b on its way, nothing waits for another wave, and the sums join in LDS.
+// One row of 4096 x 4096 bfloat16 weights, us of GPU time: tiles of 16 x 128 in 16 parts of k and their join 5.4 + 4.5, this 7.6.
+template <class T>
+struct FewRows {
+  static constexpr int kThreads = 512, kWaves = 8, kDeep = 4;
+  static constexpr int kPhases = 2;
+  static constexpr uint32_t kStep = GemmNum<T>::kStage / 2, kPer16 = GemmNum<T>::kPer16;
+  static constexpr size_t kLdsBytes = kWaves * 256 * 4;
+  typedef GemmOperand<T, kAlongK, 16, 64> Op;
+  struct Regs {};
+  // piece `lane / 16` of the step at k of row x
+  HCNN_HD static U4 piece(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, uint32_t x, uint32_t k) {
+    U4 v{};
+    if (k >= K) return v;
+    v = Op::piece(p, (x < X ? x : X - 1) * ld + k, extent);
+    return K - k < kPer16 ? Op::first(v, K - k) : v;
+  }
+  template <int PH>
+  HCNN_HD static void phase(const GemmArgs& a, unsigned bid, int tid, uint32_t* lds_words, Regs&) {
+    float* lds = reinterpret_cast<float*>(lds_words);              // [wave][m][n]
+    const uint32_t wave = (uint32_t)tid / 64, lane = (uint32_t)tid % 64, i = lane % 16, g = lane / 16;
+    const uint32_t n0 = bid * 16;
+    if constexpr (PH == 0) {
+      const T *pa = static_cast<const T*>(a.a), *pb = static_cast<const T*>(a.b);
+#if defined(__HIP_DEVICE_COMPILE__)
+      hcnn_float4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+      for (uint32_t k0 = wave * kStep; k0 < a.K; k0 += kWaves * kStep * kDeep) {
+        U4 fa[kDeep], fb[kDeep];
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d) {
+          const uint32_t k = k0 + d * (kWaves * kStep) + g * kPer16;
+          fb[d] = piece(pb, a.ldb, a.b_extent, a.N, a.K, n0 + i, k);
+          fa[d] = piece(pa, a.lda, a.a_extent, a.M, a.K, i, k);
+        }
+#pragma unroll
+        for (int d = 0; d < kDeep; ++d)
+          mma<T>(acc, hcnn_word4{fb[d].x, fb[d].y, fb[d].z, fb[d].w}, hcnn_word4{fa[d].x, fa[d].y, fa[d].z, fa[d].w});
+      }
+#else
+      hcnn_float4 acc = {};
+      for (uint32_t k0 = wave * kStep; k0 < a.K; k0 += kWaves * kStep)
+        for (uint32_t gg = 0; gg < 4; ++gg)
+          for (uint32_t e = 0; e < 4; ++e) {
+            T x[kPer16], y[kPer16];
+            const U4 fa = piece(pa, a.lda, a.a_extent, a.M, a.K, i, k0 + gg * kPer16);
+            const U4 fb = piece(pb, a.ldb, a.b_extent, a.N, a.K, n0 + g * 4 + e, k0 + gg * kPer16);
+            __builtin_memcpy(x, &fa, 16);
+            __builtin_memcpy(y, &fb, 16);
+            for (uint32_t l = 0; l < kPer16; ++l) acc[e] += Num<T>::widen(x[l]) * Num<T>::widen(y[l]);
+          }
+#endif
+#pragma unroll
+      for (int e = 0; e < 4; ++e) lds[wave * 256 + i * 16 + g * 4 + e] = acc[e];
+    } else if (tid < 64) {
+      const uint32_t m[1] = {(uint32_t)tid / 4}, n = n0 + tid % 4 * 4;
+      if (m[0] >= a.M || n >= a.N) return;
+      float v[1][4] = {}, bias[4] = {};
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[0][e] += lds[w * 256 + tid * 4 + e];
+      if (a.bias) load_row(static_cast<const T*>(a.bias) + n, a.N - n, bias);
+      finish<T>(a, m, n, bias, v);
+    }
   }
 };
 
@@ -994,17 +1079,26 @@ struct KeepRows {
     return a.wide ? static_cast<const int64_t*>(a.targets)[m] : static_cast<const int32_t*>(a.targets)[m];
   }
   HCNN_HD static bool kept(const KeepRowsArgs& a, int64_t t) { return t != a.ignore && t >= 0 && t < (int64_t)a.classes; }
+  // targets m .. m + kBatch - 1, asked for together; those from m1 on as if ignored
+  static constexpr uint32_t kBatch = 8;
+  HCNN_HD static void batch(const KeepRowsArgs& a, uint32_t m, uint32_t m1, int64_t (&t)[kBatch]) {
+#pragma unroll
+    for (uint32_t i = 0; i < kBatch; ++i) t[i] = m + i < m1 ? target(a, m + i) : a.ignore;
+  }
   template <int PH>
   HCNN_HD static void phase(const KeepRowsArgs& a, unsigned, int tid, uint32_t* lds, Regs& r) {
     const uint32_t each = (a.M + kThreads - 1) / kThreads;
     const uint32_t m0 = (uint32_t)tid * each < a.M ? tid * each : a.M, m1 = a.M - m0 < each ? a.M : m0 + each;
     if constexpr (PH == 0) {
       uint32_t n = 0;
-#pragma unroll 8
-      for (uint32_t m = m0; m < m1; ++m) {
-        const int64_t t = target(a, m);
-        if (kept(a, t)) ++n;
-        else if (t != a.ignore) atomic_inc64(a.bad);
+      for (uint32_t m = m0; m < m1; m += kBatch) {
+        int64_t t[kBatch];
+        batch(a, m, m1, t);
+#pragma unroll
+        for (uint32_t i = 0; i < kBatch; ++i) {
+          if (kept(a, t[i])) ++n;
+          else if (t[i] != a.ignore) atomic_inc64(a.bad);
+        }
       }
       r.mine = n;
       lds[tid] = n;
@@ -1019,13 +1113,16 @@ struct KeepRows {
       for (int i = 0; i < tid / 32; ++i) at += lds[kThreads + i];
       for (int i = tid / 32 * 32; i < tid; ++i) at += lds[i];
       if (tid == kThreads - 1) *a.count = at + r.mine;
-#pragma unroll 8
-      for (uint32_t m = m0; m < m1; ++m) {
-        const int64_t t = target(a, m);
-        if (!kept(a, t)) continue;
-        a.rows[at] = m;
-        a.target[at] = (uint32_t)t;
-        ++at;
+      for (uint32_t m = m0; m < m1; m += kBatch) {
+        int64_t t[kBatch];
+        batch(a, m, m1, t);
+#pragma unroll
+        for (uint32_t i = 0; i < kBatch; ++i) {
+          if (!kept(a, t[i])) continue;
+          a.rows[at] = m + i;
+          a.target[at] = (uint32_t)t[i];
+          ++at;
+        }
       }
     }
   }
@@ -1178,9 +1275,10 @@ struct NormArgs {
   uint8_t type[kNormTensors];              // 0: 32 bits, 1: binary16, 2: bfloat16
   uint32_t tensors;
   double* part;                            // sums of squares of the whole list, a number per workgroup
-  uint32_t part_first, parts;              // of this launch, of all
-  double max_norm, eps;
-  float* norm;                             // written by workgroup 0 of the first launch
+  uint32_t part_first;                     // of this launch
+  const float* factor;
+  double max_norm, eps;                    // ClipSmall
+  float* norm;
 };
 struct NormRun { const char* in; char* out; uint32_t n; int type; };
 HCNN_HD NormRun norm_run(const NormArgs& a, uint32_t run) {
@@ -1215,6 +1313,17 @@ HCNN_HD double sum_squares(const T* p, uint32_t n, int tid, int threads) {
   for (uint32_t i = whole * kPer16 + tid; i < n; i += threads) { const double x = Num<T>::widen(p[i]); s += x * x; }
   return s;
 }
+HCNN_HD double sum_any(const NormRun& r, int tid, int threads) {
+  return r.type == 0 ? sum_squares(reinterpret_cast<const float*>(r.in), r.n, tid, threads)
+       : r.type == 1 ? sum_squares(reinterpret_cast<const Half*>(r.in), r.n, tid, threads)
+                     : sum_squares(reinterpret_cast<const Bfloat*>(r.in), r.n, tid, threads);
+}
+// The norm, and the factor that goes with it: a norm that is no number makes it none
+HCNN_HD float norm_factor(double squares, double max_norm, double eps, float* norm_out) {
+  const double norm = sqrt(squares), c = max_norm / (norm + eps);
+  *norm_out = (float)norm;
+  return c < 1.0 || c != c ? (float)c : 1.0f;
+}
 struct SumSquares {
   static constexpr int kThreads = 256;
   static constexpr int kPhases = 3;
@@ -1225,9 +1334,7 @@ struct SumSquares {
     double* lds = reinterpret_cast<double*>(lds_words);
     if constexpr (PH == 0) {
       const NormRun r = norm_run(a, bid);
-      lds[tid] = r.type == 0 ? sum_squares(reinterpret_cast<const float*>(r.in), r.n, tid, kThreads)
-               : r.type == 1 ? sum_squares(reinterpret_cast<const Half*>(r.in), r.n, tid, kThreads)
-                             : sum_squares(reinterpret_cast<const Bfloat*>(r.in), r.n, tid, kThreads);
+      lds[tid] = sum_any(r, tid, kThreads);
     } else if constexpr (PH == 1) {
       if (tid < 16) {
         double s = 0.0;
@@ -1269,9 +1376,7 @@ struct NormTotal {
     } else if (tid == 0) {
       double s = 0.0;
       for (int i = 0; i < 32; ++i) s += lds[i * 32];
-      const double norm = sqrt(s), c = a.max_norm / (norm + a.eps);
-      *a.norm = (float)norm;
-      *a.factor = c < 1.0 || c != c ? (float)c : 1.0f;              // a norm that is no number makes the factor none
+      *a.factor = norm_factor(s, a.max_norm, a.eps, a.norm);
     }
   }
 };
@@ -1291,18 +1396,57 @@ HCNN_HD void scale_run(const T* p, T* to, uint32_t n, float c, int tid, int thre
   }
   for (uint32_t i = whole * kPer16 + tid; i < n; i += threads) to[i] = Num<T>::narrow(Num<T>::widen(p[i]) * c);
 }
+HCNN_HD void scale_any(const NormRun& r, float c, int tid, int threads) {
+  if (r.type == 0) scale_run(reinterpret_cast<const float*>(r.in), reinterpret_cast<float*>(r.out), r.n, c, tid, threads);
+  else if (r.type == 1) scale_run(reinterpret_cast<const Half*>(r.in), reinterpret_cast<Half*>(r.out), r.n, c, tid, threads);
+  else scale_run(reinterpret_cast<const Bfloat*>(r.in), reinterpret_cast<Bfloat*>(r.out), r.n, c, tid, threads);
+}
 struct ScaleGrads {
   static constexpr int kThreads = 256;
   static constexpr int kPhases = 1;
   struct Regs {};
   template <int PH>
   HCNN_HD static void phase(const NormArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
-    const float c = *a.norm;                                        // the factor
-    const NormRun r = norm_run(a, bid);
+    const float c = *a.factor;
+    const NormRun r = norm_run(a, a.first[a.tensors] - 1 - bid);      // the last ones first: the sum has just read them
     if (c == 1.0f && r.in == r.out) return;                         // nothing to scale, nowhere to copy
-    if (r.type == 0) scale_run(reinterpret_cast<const float*>(r.in), reinterpret_cast<float*>(r.out), r.n, c, tid, kThreads);
-    else if (r.type == 1) scale_run(reinterpret_cast<const Half*>(r.in), reinterpret_cast<Half*>(r.out), r.n, c, tid, kThreads);
-    else scale_run(reinterpret_cast<const Bfloat*>(r.in), reinterpret_cast<Bfloat*>(r.out), r.n, c, tid, kThreads);
+    scale_any(r, c, tid, kThreads);
+  }
+};
+// The whole of it for a list of few numbers: one workgroup, one launch.
+struct ClipSmall {
+  static constexpr int kThreads = 1024;
+  static constexpr int kPhases = 4;
+  static constexpr size_t kLdsBytes = kThreads * 8 + 16;
+  struct Regs {};
+  template <int PH>
+  HCNN_HD static void phase(const NormArgs& a, unsigned, int tid, uint32_t* lds_words, Regs&) {
+    double* lds = reinterpret_cast<double*>(lds_words);
+    float* factor = reinterpret_cast<float*>(lds + kThreads);
+    if constexpr (PH == 0) {
+      double s = 0.0;
+      for (uint32_t i = 0; i < a.first[a.tensors]; ++i) s += sum_any(norm_run(a, i), tid, kThreads);
+      lds[tid] = s;
+    } else if constexpr (PH == 1) {
+      if (tid < 32) {
+        double s = 0.0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s += lds[tid * 32 + i];
+        lds[tid * 32] = s;
+      }
+    } else if constexpr (PH == 2) {
+      if (tid == 0) {
+        double s = 0.0;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s += lds[i * 32];
+        *factor = norm_factor(s, a.max_norm, a.eps, a.norm);
+      }
+    } else {
+      for (uint32_t i = 0; i < a.first[a.tensors]; ++i) {
+        const NormRun r = norm_run(a, i);
+        if (*factor != 1.0f || r.in != r.out) scale_any(r, *factor, tid, kThreads);
+      }
+    }
   }
 };
 
