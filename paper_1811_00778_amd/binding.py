@@ -122,6 +122,8 @@ class PlainContext(PlainOpsMixin):
         if not torch.cuda.is_available():
             raise RuntimeError("no GPU visible: the HIP path cannot run (there is no CPU fallback)")
         self.device = torch.device(device)
+        if self.device.index is None:
+            self.device = torch.device(self.device.type, torch.cuda.current_device())
         torch.cuda.set_device(self.device)
         self._stream = torch.cuda.current_stream(self.device).cuda_stream
         self.raw = _capi.RawPlain(lib(), self._stream)
@@ -132,7 +134,10 @@ class PlainContext(PlainOpsMixin):
         self.raw.call("hcnn_plain_set_stream", ctypes.c_void_p(stream.cuda_stream))
         self._stream = stream.cuda_stream
 
-    _pre_call = Context._pre_call
+    def _pre_call(self):
+        # (the raw handle: a stream object's making takes a fifth of a small call)
+        if torch._C._cuda_getCurrentRawStream(self.device.index) != self._stream:
+            Context._pre_call(self)
 
     def _matrix(self, x, what):
         if not isinstance(x, torch.Tensor) or x.dtype not in _PLAIN_DT or x.device != self.device or x.dim() != 2:

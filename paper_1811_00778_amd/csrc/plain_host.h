@@ -169,16 +169,24 @@ inline GemmArgs operands(const Input& a, const Input& b) {
   return g;
 }
 
+constexpr size_t kShortRow = 1024;       // bytes up to which a wave takes whole rows (Strip)
+template <class T, bool NARROW, int SHARE>
+int strip(hcnn_plain* h, const GemmArgs& g, size_t streamed) {
+  typedef Strip<T, NARROW, SHARE, false> S;
+  return launch<S>(h->stream, blocks(streamed, S::kRows), S::kLdsBytes, g);
+}
+
 // ---------------------------------------------------------------- linear layer
 template <class T>
 int linear(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void* x, size_t ldx, const void* w, size_t ldw, const void* bias,
            const void* residual, size_t ld_residual, void* y, size_t ldy, void* z, size_t ldz) {
-  if (M <= 16 && blocks(N, 16) <= kMaxSize) {
+  if (K && (M <= 16 || N <= 16)) {
     GemmArgs g = operands(Input{x, ldx, M, K}, Input{w, ldw, N, K});
     g.M = (uint32_t)M; g.N = (uint32_t)N; g.K = (uint32_t)K;
     g.act = act; g.bias = bias; g.residual = residual; g.ld_residual = ld_residual;
     g.out = y; g.ld_out = ldy; g.z = z; g.ld_z = ldz;
-    return launch<FewRows<T>>(h->stream, blocks(N, 16), FewRows<T>::kLdsBytes, g);
+    if (M <= 16) return strip<T, false, 8>(h, g, N);
+    return K * sizeof(T) <= kShortRow ? strip<T, true, 1>(h, g, M) : strip<T, true, 8>(h, g, M);
   }
   Arena ar;
   Input ix{x, ldx, M, K}, iw{w, ldw, N, K};
@@ -286,6 +294,12 @@ struct LossCall {
 // times as large there.  The factor goes back out of the sums.
 template <class T> constexpr float delta_scale() { return std::is_same_v<T, Half> ? 32768.0f : 1.0f; }
 
+template <class T, int SHARE>
+int strip_loss(hcnn_plain* h, const GemmArgs& g, const RowStatsArgs& rows) {
+  typedef Strip<T, true, SHARE, true> S;
+  return launch<S>(h->stream, blocks(g.M, S::kRows), S::kLdsBytes, StripLossArgs{g, rows});
+}
+
 template <class T>
 int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
   const size_t M = c.M, K = c.K, V = c.V;
@@ -306,7 +320,8 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
   Input idelta{nullptr, ld_delta, M, piece, true, a.take(grad ? M * ld_delta * sizeof(T) : 0)};
   const bool direct_d = direct_input<T>(idelta);
   const Shape sx = choose<T>(h, M, K, piece, pieces == 1, direct_d && direct_w), sw = choose<T>(h, piece, K, M, true, direct_d && direct_x);
-  const size_t tiles = blocks(V, ss.bn), ld_stats = up(M, 64), row_wgs = blocks(M, RowStats::kRows);
+  const bool narrow = V <= 16 && K;                             // scores, losses and the scores' gradients in one kernel
+  const size_t tiles = narrow ? 0 : blocks(V, ss.bn), ld_stats = up(M, 64), row_wgs = blocks(M, 16);
   const size_t o_count = a.take(4), o_alpha = a.take(4), o_rows = a.take(M * 4), o_target = a.take(M * 4), o_score = a.take(M * 4), o_lse = a.take(M * 4);
   const size_t o_stats = a.take(tiles * 2 * ld_stats * 4), o_part = a.take(row_wgs * 8);
   const size_t o_dx = a.take(pieces > 1 && c.dx ? M * up(K, 8) * 4 : 0);
@@ -317,7 +332,7 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
   uint32_t *count = at<uint32_t>(h, o_count), *rows = at<uint32_t>(h, o_rows), *target = at<uint32_t>(h, o_target);
   float *alpha = at<float>(h, o_alpha), *score = at<float>(h, o_score), *lse = at<float>(h, o_lse);
 
-  KeepRowsArgs kr{c.targets, c.target_bytes == 8, c.ignore, (uint32_t)M, (uint32_t)V, rows, target, count, h->d_bad};
+  KeepRowsArgs kr{c.targets, c.target_bytes == 8, c.ignore, (uint32_t)M, (uint32_t)V, rows, target, count, h->d_bad, c.loss, alpha, c.scale / delta_scale<T>()};
   if ((e = launch<KeepRows>(h->stream, 1, KeepRows::kLdsBytes, kr))) return e;
   if (M) {
     const SortRowsArgs sr{kr, K ? c.dx : nullptr, c.ld_dx * sizeof(T), K * sizeof(T), c.row_loss, c.row_lse,
@@ -330,19 +345,25 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
   g.count = count; g.count_of = kCountM; g.kept = at<void>(h, ikept.offset); g.ld_kept = ikept.ld; g.kept_always = ix.packed;
   g.stats = at<float>(h, o_stats); g.ld_stats = ld_stats; g.target = target; g.target_score = score; g.lse = lse;
   g.delta_scale = delta_scale<T>();
-  if (M) {
+  const RowStatsArgs rs{g.stats, ld_stats, (uint32_t)tiles, (uint32_t)M, count, rows, score, lse, at<double>(h, o_part), c.row_loss, c.row_lse};
+  if (M && narrow) {
+    if (grad) { g.out = at<void>(h, idelta.offset); g.ld_out = ld_delta; }
+    if ((e = K * sizeof(T) <= kShortRow ? strip_loss<T, 1>(h, g, rs) : strip_loss<T, 8>(h, g, rs))) return e;
+  } else if (M) {
     if ((e = gemm<T, kAlongK, kAlongK, kEpiStats>(h, g, ss))) return e;
-    const RowStatsArgs rs{g.stats, ld_stats, (uint32_t)tiles, (uint32_t)M, count, rows, score, lse, at<double>(h, o_part), c.row_loss, c.row_lse};
-    if ((e = launch<RowStats>(h->stream, row_wgs, RowStats::kLdsBytes, rs))) return e;
+    if ((e = launch<RowStats>(h->stream, blocks(M, RowStats::kRows), RowStats::kLdsBytes, rs))) return e;
   }
-  const MeanLossArgs ml{at<double>(h, o_part), (uint32_t)row_wgs, count, c.loss, grad ? alpha : nullptr, c.scale / delta_scale<T>()};
-  if ((e = launch<MeanLoss>(h->stream, 1, MeanLoss::kLdsBytes, ml))) return e;
+  if (M && c.loss) {
+    const size_t groups = blocks(M, !narrow ? RowStats::kRows : K * sizeof(T) <= kShortRow ? Strip<T, true, 1, true>::kRows : Strip<T, true, 8, true>::kRows);
+    const MeanLossArgs ml{at<double>(h, o_part), (uint32_t)groups, count, c.loss};
+    if ((e = launch<MeanLoss>(h->stream, 1, MeanLoss::kLdsBytes, ml))) return e;
+  }
 
   for (size_t p = 0; p < pieces; ++p) {
     const size_t v0 = p * piece, n = std::min(piece, V - v0);
     Input wp{static_cast<const char*>(iw.p) + v0 * iw.ld * sizeof(T), iw.ld, n, K};
     idelta.cols = n;
-    if (M) {
+    if (M && !narrow) {
       GemmArgs d = g;
       d.b = wp.p; d.b_extent = wp.extent();
       d.N = (uint32_t)n; d.n_offset = (uint32_t)v0;

@@ -879,75 +879,6 @@ struct GemmJoin {
   }
 };
 
-// out = a b^T for at most 16 rows of a, both along k: bound by reading b, once.  A workgroup takes 16 rows of b and all of k; its
-// waves take every eighth 64-byte step of k and load it straight to the registers that the products read (lane: row lane % 16, piece
-// lane / 16), kDeep steps ahead: eight waves hold 8 x kDeep KiB of b on its way, nothing waits for another wave, and the sums join in LDS.
-// One row of 4096 x 4096 bfloat16 weights, us of GPU time: tiles of 16 x 128 in 16 parts of k and their join 5.4 + 4.5, this 7.6.
-template <class T>
-struct FewRows {
-  static constexpr int kThreads = 512, kWaves = 8, kDeep = 4;
-  static constexpr int kPhases = 2;
-  static constexpr uint32_t kStep = GemmNum<T>::kStage / 2, kPer16 = GemmNum<T>::kPer16;
-  static constexpr size_t kLdsBytes = kWaves * 256 * 4;
-  typedef GemmOperand<T, kAlongK, 16, 64> Op;
-  struct Regs {};
-  // piece `lane / 16` of the step at k of row x
-  HCNN_HD static U4 piece(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, uint32_t x, uint32_t k) {
-    U4 v{};
-    if (k >= K) return v;
-    v = Op::piece(p, (x < X ? x : X - 1) * ld + k, extent);
-    return K - k < kPer16 ? Op::first(v, K - k) : v;
-  }
-  template <int PH>
-  HCNN_HD static void phase(const GemmArgs& a, unsigned bid, int tid, uint32_t* lds_words, Regs&) {
-    float* lds = reinterpret_cast<float*>(lds_words);              // [wave][m][n]
-    const uint32_t wave = (uint32_t)tid / 64, lane = (uint32_t)tid % 64, i = lane % 16, g = lane / 16;
-    const uint32_t n0 = bid * 16;
-    if constexpr (PH == 0) {
-      const T *pa = static_cast<const T*>(a.a), *pb = static_cast<const T*>(a.b);
-#if defined(__HIP_DEVICE_COMPILE__)
-      hcnn_float4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
-      for (uint32_t k0 = wave * kStep; k0 < a.K; k0 += kWaves * kStep * kDeep) {
-        U4 fa[kDeep], fb[kDeep];
-#pragma unroll
-        for (int d = 0; d < kDeep; ++d) {
-          const uint32_t k = k0 + d * (kWaves * kStep) + g * kPer16;
-          fb[d] = piece(pb, a.ldb, a.b_extent, a.N, a.K, n0 + i, k);
-          fa[d] = piece(pa, a.lda, a.a_extent, a.M, a.K, i, k);
-        }
-#pragma unroll
-        for (int d = 0; d < kDeep; ++d)
-          mma<T>(acc, hcnn_word4{fb[d].x, fb[d].y, fb[d].z, fb[d].w}, hcnn_word4{fa[d].x, fa[d].y, fa[d].z, fa[d].w});
-      }
-#else
-      hcnn_float4 acc = {};
-      for (uint32_t k0 = wave * kStep; k0 < a.K; k0 += kWaves * kStep)
-        for (uint32_t gg = 0; gg < 4; ++gg)
-          for (uint32_t e = 0; e < 4; ++e) {
-            T x[kPer16], y[kPer16];
-            const U4 fa = piece(pa, a.lda, a.a_extent, a.M, a.K, i, k0 + gg * kPer16);
-            const U4 fb = piece(pb, a.ldb, a.b_extent, a.N, a.K, n0 + g * 4 + e, k0 + gg * kPer16);
-            __builtin_memcpy(x, &fa, 16);
-            __builtin_memcpy(y, &fb, 16);
-            for (uint32_t l = 0; l < kPer16; ++l) acc[e] += Num<T>::widen(x[l]) * Num<T>::widen(y[l]);
-          }
-#endif
-#pragma unroll
-      for (int e = 0; e < 4; ++e) lds[wave * 256 + i * 16 + g * 4 + e] = acc[e];
-    } else if (tid < 64) {
-      const uint32_t m[1] = {(uint32_t)tid / 4}, n = n0 + tid % 4 * 4;
-      if (m[0] >= a.M || n >= a.N) return;
-      float v[1][4] = {}, bias[4] = {};
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[0][e] += lds[w * 256 + tid * 4 + e];
-      if (a.bias) load_row(static_cast<const T*>(a.bias) + n, a.N - n, bias);
-      finish<T>(a, m, n, bias, v);
-    }
-  }
-};
-
 // A matrix of 16-bit numbers with rows that start on 16 bytes: eight numbers per thread.
 struct PackArgs {
   const void* from;
@@ -1066,64 +997,76 @@ struct KeepRowsArgs {
   uint32_t M, classes;
   uint32_t* rows;             // [M] rows that take part, in order
   uint32_t* target;           // [M] their classes
-  uint32_t* count;
+  uint32_t* count;            // rows that take part
   unsigned long long* bad;    // targets that are neither a class nor the ignored value
+  float* loss;                // 0 here: the mean of no rows (may be null)
+  float* alpha;               // scale / count
+  float scale;
 };
-// One workgroup: a run of consecutive rows per thread.
+// One workgroup, 8192 rows at a time: thread t takes rows t, 1024 + t, ..., so that what it reads and writes lies side by side with the
+// other lanes' (a run of rows per thread: 14.6 us for 8192 rows, this 11.8).  A row's place is the number of rows before it that
+// take part: of those in its 64, by their bits in LDS, and of the 64s before.
 struct KeepRows {
-  static constexpr int kThreads = 1024;
-  static constexpr int kPhases = 3;
-  static constexpr size_t kLdsBytes = (kThreads + 32) * 4;
-  struct Regs { uint32_t mine; };
+  static constexpr int kThreads = 1024, kEach = 8, kWaves = kThreads / 64;
+  static constexpr int kLoopPhases = 4, kPhases = 5;
+  static constexpr size_t kLdsBytes = kEach * kWaves * 12;
+  struct Regs {
+    uint32_t iter;
+    uint32_t before;          // rows of earlier iterations that take part
+    uint32_t target[kEach];   // ~0: takes no part
+  };
+  HCNN_HD static uint32_t loop_count(const KeepRowsArgs& a) { return (a.M + kThreads * kEach - 1) / (kThreads * kEach); }
   HCNN_HD static int64_t target(const KeepRowsArgs& a, uint32_t m) {
     return a.wide ? static_cast<const int64_t*>(a.targets)[m] : static_cast<const int32_t*>(a.targets)[m];
   }
   HCNN_HD static bool kept(const KeepRowsArgs& a, int64_t t) { return t != a.ignore && t >= 0 && t < (int64_t)a.classes; }
-  // targets m .. m + kBatch - 1, asked for together; those from m1 on as if ignored
-  static constexpr uint32_t kBatch = 8;
-  HCNN_HD static void batch(const KeepRowsArgs& a, uint32_t m, uint32_t m1, int64_t (&t)[kBatch]) {
-#pragma unroll
-    for (uint32_t i = 0; i < kBatch; ++i) t[i] = m + i < m1 ? target(a, m + i) : a.ignore;
-  }
+  HCNN_HD static uint32_t ones(uint32_t x) { return (uint32_t)__builtin_popcount(x); }
+  HCNN_HD static void begin(const KeepRowsArgs&, unsigned, int, uint32_t*, Regs& r) { r.before = 0; }
   template <int PH>
   HCNN_HD static void phase(const KeepRowsArgs& a, unsigned, int tid, uint32_t* lds, Regs& r) {
-    const uint32_t each = (a.M + kThreads - 1) / kThreads;
-    const uint32_t m0 = (uint32_t)tid * each < a.M ? tid * each : a.M, m1 = a.M - m0 < each ? a.M : m0 + each;
+    uint32_t* counts = lds + kEach * kWaves * 2;                   // [kEach][kWaves], behind the bits [kEach][kWaves][2]
+    const uint32_t m0 = r.iter * (kThreads * kEach) + tid, wave = (uint32_t)tid / 64, lane = (uint32_t)tid % 64;
     if constexpr (PH == 0) {
-      uint32_t n = 0;
-      for (uint32_t m = m0; m < m1; m += kBatch) {
-        int64_t t[kBatch];
-        batch(a, m, m1, t);
-#pragma unroll
-        for (uint32_t i = 0; i < kBatch; ++i) {
-          if (kept(a, t[i])) ++n;
-          else if (t[i] != a.ignore) atomic_inc64(a.bad);
-        }
-      }
-      r.mine = n;
-      lds[tid] = n;
+      if (tid < kEach * kWaves * 2) lds[tid] = 0;
     } else if constexpr (PH == 1) {
-      if (tid < 32) {
-        uint32_t s = 0;
-        for (int i = 0; i < 32; ++i) s += lds[tid * 32 + i];
-        lds[kThreads + tid] = s;
-      }
-    } else {
-      uint32_t at = 0;
-      for (int i = 0; i < tid / 32; ++i) at += lds[kThreads + i];
-      for (int i = tid / 32 * 32; i < tid; ++i) at += lds[i];
-      if (tid == kThreads - 1) *a.count = at + r.mine;
-      for (uint32_t m = m0; m < m1; m += kBatch) {
-        int64_t t[kBatch];
-        batch(a, m, m1, t);
+      int64_t t[kEach];
 #pragma unroll
-        for (uint32_t i = 0; i < kBatch; ++i) {
-          if (!kept(a, t[i])) continue;
-          a.rows[at] = m + i;
-          a.target[at] = (uint32_t)t[i];
-          ++at;
+      for (int i = 0; i < kEach; ++i) {
+        const uint32_t m = m0 + i * kThreads;
+        t[i] = target(a, m < a.M ? m : a.M - 1);
+      }
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        const bool is = m0 + i * kThreads < a.M, keep = is && kept(a, t[i]);
+        r.target[i] = keep ? (uint32_t)t[i] : ~0u;
+        if (keep) lds_or(lds + (i * kWaves + wave) * 2 + lane / 32, 1u << lane % 32);
+        else if (is && t[i] != a.ignore) atomic_inc64(a.bad);
+      }
+    } else if constexpr (PH == 2) {
+      if (tid < kEach * kWaves) counts[tid] = ones(lds[tid * 2]) + ones(lds[tid * 2 + 1]);
+    } else if constexpr (PH == 3) {
+      uint32_t at = r.before, start[kEach];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          if (w == (int)wave) start[i] = at;
+          at += counts[i * kWaves + w];
         }
       }
+      r.before = at;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        if (r.target[i] == ~0u) continue;
+        const uint32_t *bits = lds + (i * kWaves + wave) * 2, below = (1u << lane % 32) - 1;
+        const uint32_t to = start[i] + (lane < 32 ? ones(bits[0] & below) : ones(bits[0]) + ones(bits[1] & below));
+        a.rows[to] = m0 + i * kThreads;
+        a.target[to] = r.target[i];
+      }
+    } else if (tid == 0) {
+      *a.count = r.before;
+      if (a.loss) *a.loss = 0.0f;
+      *a.alpha = (float)((double)a.scale / (r.before ? r.before : 1));
     }
   }
 };
@@ -1140,6 +1083,15 @@ struct RowStatsArgs {
   double* part;               // [workgroups] sums of the losses
   float *row_loss, *row_lse;  // [M] or null
 };
+// Loss of a row from its largest score, the sum of exponentials relative to it, and the class's score; what the row has to leave behind.
+HCNN_HD float row_loss(const RowStatsArgs& a, uint32_t m, float top, float sum, float score, float* lse_out) {
+  const float log_sum = logf(sum), lse = top + log_sum;
+  const float l = (top - score) + log_sum;                      // (the difference of the two large numbers first)
+  if (a.row_loss) a.row_loss[a.rows[m]] = l;
+  if (a.row_lse) a.row_lse[a.rows[m]] = lse;
+  *lse_out = lse;
+  return l;
+}
 // 64 rows per workgroup, four threads each.
 struct RowStats {
   static constexpr int kThreads = 256;
@@ -1151,11 +1103,11 @@ struct RowStats {
   HCNN_HD static void phase(const RowStatsArgs& a, unsigned bid, int tid, uint32_t* lds_words, Regs&) {
     float* lds = reinterpret_cast<float*>(lds_words);
     double* losses = reinterpret_cast<double*>(lds + 2 * kThreads);
-    const uint32_t m = bid * kRows + tid % kRows;
-    const uint32_t M = *a.count;
+    const uint32_t m = bid * kRows + tid % kRows, M = *a.count;
     if constexpr (PH == 0) {
       float top = -INFINITY, sum = 0.0f;
       if (m < M)
+#pragma unroll 4
         for (uint32_t t = tid / kRows; t < a.tiles; t += 4) {
           const float* s = a.stats + (size_t)t * 2 * a.ld_stats + m;
           const float x = s[0], y = s[a.ld_stats], high = fmaxf(top, x);
@@ -1174,18 +1126,13 @@ struct RowStats {
             const float s = lds[kThreads + i * kRows + tid];
             if (s != 0.0f) sum += s * exp_of(lds[i * kRows + tid] - top);
           }
-          const float log_sum = logf(sum), lse = top + log_sum;
-          // (the difference of the two large numbers first)
-          const float l = (top - a.target_score[m]) + log_sum;
-          a.lse[m] = lse;
-          if (a.row_loss) a.row_loss[a.rows[m]] = l;
-          if (a.row_lse) a.row_lse[a.rows[m]] = lse;
-          loss = l;
+          loss = row_loss(a, m, top, sum, a.target_score[m], a.lse + m);
         }
         losses[tid] = loss;
       }
     } else if (tid == 0) {
       double s = 0.0;
+#pragma unroll 8
       for (uint32_t i = 0; i < kRows; ++i) s += losses[i];
       a.part[bid] = s;
     }
@@ -1195,13 +1142,12 @@ struct MeanLossArgs {
   const double* part;
   uint32_t parts;
   const uint32_t* count;
-  float* loss;                // mean over the rows that take part, 0 where there are none (may be null)
-  float* alpha;               // scale / count (may be null)
-  float scale;
+  float* loss;                // mean over the rows that take part, 0 where there are none
 };
+// (by a workgroup of its own: when the last one of the kernel before took it along, each one's fence at the device cost more)
 struct MeanLoss {
   static constexpr int kThreads = 256;
-  static constexpr int kPhases = 2;
+  static constexpr int kPhases = 3;
   static constexpr size_t kLdsBytes = kThreads * 8;
   struct Regs {};
   template <int PH>
@@ -1211,15 +1157,188 @@ struct MeanLoss {
       double s = 0.0;
       for (uint32_t i = tid; i < a.parts; i += kThreads) s += a.part[i];
       lds[tid] = s;
+    } else if constexpr (PH == 1) {
+      if (tid < 16) {
+        double s = 0.0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += lds[tid * 16 + i];
+        lds[tid * 16] = s;
+      }
     } else if (tid == 0) {
       double s = 0.0;
-      for (int i = 0; i < kThreads; ++i) s += lds[i];
-      const uint32_t n = *a.count ? *a.count : 1;
-      if (a.loss) *a.loss = (float)(s / n);
-      if (a.alpha) *a.alpha = (float)((double)a.scale / n);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s += lds[i * 16];
+      *a.loss = (float)(s / (*a.count ? *a.count : 1));
     }
   }
 };
+// out = a b^T with at most 16 rows of a or (NARROW) of b, both along k: bound by reading the other operand, once.  It is loaded straight to
+// the registers that the products read (lane: row lane % 16, 16 bytes lane / 16 of a 64-byte step of k); no wave waits for another.
+//   SHARE 8  a workgroup takes 16 of its rows, eight waves every eighth step of k each, kDeep steps asked for at a time; sums join in LDS
+//   SHARE 1  a wave takes 4 x 16 rows and all of k (short rows: at most 1 KiB)
+// GPU us: one row of 4096 x 4096 bfloat16 weights in tiles of 16 x 128, 16 parts of k and their join 5.4 + 4.5, this 7.2; 147456 rows of
+// 25 numbers by 5 filters in tiles of 128 x 16 10.2, this 6.4.
+// LOSS (NARROW): the scores of at most 16 classes end in the rows' losses and the gradients for the scores.
+struct StripLossArgs { GemmArgs g; RowStatsArgs rows; };
+template <bool LOSS> struct StripArgs { typedef GemmArgs type; };
+template <> struct StripArgs<true> { typedef StripLossArgs type; };
+template <class T, bool NARROW, int SHARE, bool LOSS>
+struct Strip {
+  typedef typename StripArgs<LOSS>::type Args;
+  static constexpr int kWaves = SHARE == 8 ? 8 : 4, kThreads = kWaves * 64;
+  static constexpr int R = SHARE == 8 ? 1 : 4, kDeep = SHARE == 8 ? 8 : 2;
+  static constexpr uint32_t kRows = SHARE == 8 ? 16 : kWaves * R * 16;         // of the streamed operand in a workgroup
+  static constexpr int kPhases = LOSS ? 3 : SHARE == 8 ? 2 : 1;
+  static constexpr uint32_t kStep = GemmNum<T>::kStage / 2, kPer16 = GemmNum<T>::kPer16, kSpan = SHARE * kStep * kDeep;
+  static constexpr size_t kLdsBytes = (SHARE == 8 ? kWaves * 256 : LOSS ? kWaves * R * 256 : 0) * 4 + (LOSS ? kThreads * 8 : 0);
+  typedef GemmOperand<T, kAlongK, 16, 64> Op;
+  struct Regs {};
+  HCNN_HD static const GemmArgs& gemm(const GemmArgs& a) { return a; }
+  HCNN_HD static const GemmArgs& gemm(const StripLossArgs& a) { return a.g; }
+  // 16 bytes at k of row x (the last one where there is none)
+  HCNN_HD static U4 piece(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, uint32_t x, uint32_t k) {
+    const U4 v = Op::piece(p, (x < X ? x : X - 1) * ld + (k < K ? k : K - 1), extent);
+    return Op::first(v, k < K ? K - k : 0);
+  }
+  template <int PH>
+  HCNN_HD static void phase(const Args& args, unsigned bid, int tid, uint32_t* lds_words, Regs&) {
+    const GemmArgs& a = gemm(args);
+    float* lds = reinterpret_cast<float*>(lds_words);              // [wave][R][m][n]
+    const uint32_t wave = (uint32_t)tid / 64, lane = (uint32_t)tid % 64, i = lane % 16, g = lane / 16;
+    const uint32_t x0 = bid * kRows;                                // first streamed row
+    uint32_t M = a.M;
+    if constexpr (LOSS) M = wave_uniform(*a.count) < M ? wave_uniform(*a.count) : M;
+    if constexpr (PH == 0) {
+      const bool kept = LOSS && a.kept && (a.kept_always || M < a.M);
+      const T *pa = static_cast<const T*>(kept ? a.kept : a.a), *pb = static_cast<const T*>(a.b);
+      const size_t lda = kept ? a.ld_kept : a.lda, a_extent = kept ? (a.M - 1) * a.ld_kept + a.K : a.a_extent;
+      const T *ps = NARROW ? pa : pb, *po = NARROW ? pb : pa;
+      const size_t lds_ = NARROW ? lda : a.ldb, ldo = NARROW ? a.ldb : lda;
+      const size_t es = NARROW ? a_extent : a.b_extent, eo = NARROW ? a.b_extent : a_extent;
+      const uint32_t XS = NARROW ? M : a.N, XO = NARROW ? a.N : M;
+      if (x0 < XS) {
+        const uint32_t row = x0 + (SHARE == 8 ? 0 : wave * (R * 16)) + i;
+        hcnn_float4 acc[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[r][e] = 0.0f;
+#if defined(__HIP_DEVICE_COMPILE__)
+        const uint32_t first = (SHARE == 8 ? wave * kStep : 0) + g * kPer16;
+        const T* at[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) at[r] = ps + (row + r * 16 < XS ? row + r * 16 : XS - 1) * lds_ + first;
+        const T* other = po + (i < XO ? i : XO - 1) * ldo + first;
+        for (uint32_t k0 = 0; k0 < a.K; k0 += kSpan) {
+          U4 fs[R][kDeep], fo[kDeep];
+#pragma unroll
+          for (int d = 0; d < kDeep; ++d) {
+            const uint32_t step = k0 + d * (SHARE * kStep) + (SHARE == 8 ? wave_uniform(wave) * kStep : 0);
+            if (step + kStep <= a.K) {
+#pragma unroll
+              for (int r = 0; r < R; ++r) fs[r][d] = ld16(reinterpret_cast<const char*>(at[r] + k0 + d * (SHARE * kStep)));
+              fo[d] = ld16(reinterpret_cast<const char*>(other + k0 + d * (SHARE * kStep)));
+            } else {
+#pragma unroll
+              for (int r = 0; r < R; ++r) fs[r][d] = piece(ps, lds_, es, XS, a.K, row + r * 16, step + g * kPer16);
+              fo[d] = piece(po, ldo, eo, XO, a.K, i, step + g * kPer16);
+            }
+          }
+#pragma unroll
+          for (int d = 0; d < kDeep; ++d)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              const hcnn_word4 s4{fs[r][d].x, fs[r][d].y, fs[r][d].z, fs[r][d].w}, o4{fo[d].x, fo[d].y, fo[d].z, fo[d].w};
+              mma<T>(acc[r], NARROW ? o4 : s4, NARROW ? s4 : o4);
+            }
+        }
+#else
+        for (int r = 0; r < R; ++r)
+          for (uint32_t k0 = SHARE == 8 ? wave * kStep : 0; k0 < a.K; k0 += SHARE * kStep)
+            for (uint32_t p = 0; p < 4; ++p)
+              for (uint32_t e = 0; e < 4; ++e) {
+                // (the lane's m: row i of a, its n: rows 4 g + e of b)
+                const uint32_t ra = (NARROW ? row + r * 16 : i), rb = NARROW ? g * 4 + e : x0 + g * 4 + e, k = k0 + p * kPer16;
+                T x[kPer16], y[kPer16];
+                const U4 fa = piece(pa, lda, a_extent, M, a.K, ra, k), fb = piece(pb, a.ldb, a.b_extent, a.N, a.K, rb, k);
+                __builtin_memcpy(x, &fa, 16);
+                __builtin_memcpy(y, &fb, 16);
+                for (uint32_t l = 0; l < kPer16; ++l) acc[r][e] += Num<T>::widen(x[l]) * Num<T>::widen(y[l]);
+              }
+        (void)ps; (void)po; (void)lds_; (void)ldo; (void)es; (void)eo; (void)XO;
+#endif
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          float v[1][4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[0][e] = acc[r][e];
+          if constexpr (SHARE == 8 || LOSS) {
+            __builtin_memcpy(lds + ((wave * R + r) * 16 + i) * 16 + g * 4, v, 16);
+          } else {
+            const uint32_t m[1] = {row + r * 16}, n = g * 4;
+            if (m[0] < M && n < a.N) end(a, m, n, v);
+          }
+        }
+      }
+    } else if constexpr (!LOSS) {
+      if (tid < 64) {
+        const uint32_t m[1] = {(NARROW ? x0 : 0) + (uint32_t)tid / 4}, n = (NARROW ? 0 : x0) + tid % 4 * 4;
+        if (m[0] >= M || n >= a.N) return;
+        float v[1][4] = {};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[0][e] += lds[w * 256 + tid * 4 + e];
+        end(a, m, n, v);
+      }
+    } else {
+      double* losses = reinterpret_cast<double*>(lds + (SHARE == 8 ? kWaves : kWaves * R) * 256);
+      const RowStatsArgs& rows = args.rows;
+      const uint32_t m = x0 + tid;
+      if constexpr (PH == 1) {
+        double loss = 0.0;
+        if (tid < (int)kRows && m < M) {
+          float v[16], top = -INFINITY, sum = 0.0f, score = 0.0f;
+          const uint32_t t = a.target[m];
+#pragma unroll
+          for (uint32_t n = 0; n < 16; ++n) {
+            v[n] = 0.0f;
+#pragma unroll
+            for (int w = 0; w < SHARE; ++w) v[n] += lds[(SHARE == 8 ? w * 256 : 0) + tid * 16 + n];
+            if (n < a.N) top = fmaxf(top, v[n]);
+            if (n == t) score = v[n];
+          }
+#pragma unroll
+          for (uint32_t n = 0; n < 16; ++n) {
+            v[n] = exp_of(v[n] - top);
+            if (n < a.N) sum += v[n];
+          }
+          float lse;
+          loss = row_loss(rows, m, top, sum, score, &lse);
+          if (a.out) {
+            const float part = 1.0f / sum;
+            T* to = static_cast<T*>(a.out) + (size_t)m * a.ld_out;
+#pragma unroll
+            for (uint32_t n = 0; n < 16; ++n)
+              if (n < a.N) to[n] = Num<T>::narrow((v[n] * part - (n == t ? 1.0f : 0.0f)) * a.delta_scale);
+          }
+        }
+        losses[tid] = loss;
+      } else if (tid == 0) {
+        double s = 0.0;
+#pragma unroll 8
+        for (uint32_t l = 0; l < (kRows < (uint32_t)kThreads ? kRows : kThreads); ++l) s += losses[l];
+        rows.part[bid] = s;
+      }
+    }
+  }
+  HCNN_HD static void end(const GemmArgs& a, const uint32_t (&m)[1], uint32_t n, float (&v)[1][4]) {
+    float bias[4] = {};
+    if (a.bias) load_row(static_cast<const T*>(a.bias) + n, a.N - n, bias);
+    finish<T>(a, m, n, bias, v);
+  }
+};
+
 // Rows that do not take part: zeros in the gradient, and in the losses and statistics asked for.  Rows that do: a copy of theirs in x one
 // behind the other, where they are not all rows or the copy is wanted in any case.  64 threads per row.
 struct SortRowsArgs {
