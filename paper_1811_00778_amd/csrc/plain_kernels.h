@@ -94,7 +94,7 @@ HCNN_HD uint64_t ld8(const char* p) { uint64_t v; __builtin_memcpy(&v, p, 8); re
 HCNN_HD void st8(char* p, uint64_t v) { __builtin_memcpy(p, &v, 8); }
 #endif
 
-// W numbers in a row (4 or 8), widened
+// W numbers in a row (4, 8 or 16), widened
 template <class T, int W>
 HCNN_HD void load_row(const T* p, float (&v)[W]) {
   T t[W];
@@ -134,14 +134,29 @@ template <class T, int W>
 HCNN_HD void load_row(const T* p, uint32_t left, float (&v)[W]) {
   if (left >= W) return load_row(p, v);
 #pragma unroll
-  for (uint32_t i = 0; i < W; ++i) v[i] = i < left ? Num<T>::widen(p[i]) : 0.0f;
+  for (uint32_t q = 0; q < W; q += 4) {
+    float t[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (left >= q + 4) load_row(p + q, t);
+    else
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+        if (q + i < left) t[i] = Num<T>::widen(p[q + i]);
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) v[q + i] = t[i];
+  }
 }
 template <class T, int W>
 HCNN_HD void store_row(T* p, uint32_t left, const float (&v)[W]) {
   if (left >= W) return store_row(p, v);
 #pragma unroll
-  for (uint32_t i = 0; i < W; ++i)
-    if (i < left) p[i] = Num<T>::narrow(v[i]);
+  for (uint32_t q = 0; q < W; q += 4) {
+    const float t[4] = {v[q], v[q + 1], v[q + 2], v[q + 3]};
+    if (left >= q + 4) store_row(p + q, t);
+    else
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+        if (q + i < left) p[q + i] = Num<T>::narrow(t[i]);
+  }
 }
 
 // ---------------------------------------------------------------- activations
@@ -221,11 +236,12 @@ HCNN_HD float slope_of(float z, int act) {
 //   kAlongK  in LDS [row][8 pieces of 16 bytes], piece p of a row at p ^ (row mod 8): the 16 rows x 4 pieces that a wave reads at once
 //            spread evenly over the banks
 //   kAcrossK in LDS [k][rows] as it lies in memory, in granules of 16 rows; 16-bit numbers are read with the transposing LDS read
-//            (16 lanes: 4 k x 16 rows in, 4 k of one row out), 32-bit ones word by word; granules are swapped by the bits of k in which the lanes
-//            of one read differ
+//            (16 lanes: 4 k x 16 rows in, 4 k of one row out), 32-bit ones word by word
 // Products: v_mfma_f32_16x16x32 (16 bits) and v_mfma_f32_16x16x4_f32.  A lane's 16 bytes of an operand are k 8 g .. 8 g + 7 (16 bits) or
 // 4 g .. 4 g + 3 (32 bits) of a row, g = lane / 16; both operands use the same order, so that the sum is the same whatever the instruction
-// calls these k.  b is the first operand: a lane then holds four consecutive n of a row m = lane mod 16.
+// calls these k.  b is the first operand: a lane then holds four consecutive n of a row m = lane mod 16, and, by the choice of b's rows for
+// each product (GemmOperand), 4 FN consecutive n in all: whole 128-byte lines of 16-bit numbers for each row leave without a way through LDS
+// (that way, in two halves of the tile with a barrier before and behind each, took 7 of 110 us of a tile with 4096 k).
 enum { kAlongK = 0, kAcrossK = 1 };
 enum { kCountNone = 0, kCountM = 1, kCountK = 2 };         // what GemmArgs::count limits
 
@@ -307,8 +323,10 @@ template <class T> struct GemmNum {
   static constexpr uint32_t kStage = 128 / sizeof(T);      // k of a stage
 };
 
-// One operand's way through a workgroup: BX rows of the output index, THREADS threads.
-template <class T, int LAYOUT, int BX, int THREADS>
+// One operand's way through a workgroup: BX rows of the output index, THREADS threads.  The 16 rows that a wave takes for one product are four
+// runs of four, GROUP rows apart: with GROUP = 4 sixteen rows in a row; b takes 4 x its products of a wave, so that the sums of a lane
+// in all of them lie side by side.
+template <class T, int LAYOUT, int BX, int THREADS, int GROUP = 4>
 struct GemmOperand {
   static constexpr uint32_t kPer16 = GemmNum<T>::kPer16, kStage = GemmNum<T>::kStage;
   static constexpr int kPieces = BX * 8;                                       // of 16 bytes in a stage
@@ -376,13 +394,24 @@ struct GemmOperand {
       *reinterpret_cast<U4*>(lds + place(c / kRowPieces, c % kRowPieces)) = load_one(p, ld, extent, X, K, x0, k0, c);
   }
   HCNN_HD static uint32_t place(uint32_t line, uint32_t pc) {                  // byte of piece pc of stored row `line`
-    if constexpr (LAYOUT == kAlongK) return line * 128 + ((pc ^ (line & 7)) << 4);
-    else if constexpr (sizeof(T) == 2) return line * (BX * 2) + ((pc / 2 ^ swap(line)) << 5) + (pc % 2 << 4);
-    else return line * (BX * 4) + ((pc / 4 ^ swap(line)) << 6) + (pc % 4 << 4);
+    if constexpr (LAYOUT == kAlongK) return line * 128 + ((pc ^ turn(line)) << 4);
+    else return line * (BX * sizeof(T)) + (moved(line, pc) << 4);
   }
-  // kAcrossK: granule g of stored row k lies at g ^ swap(k)
-  HCNN_HD static uint32_t swap(uint32_t k) {
-    return (sizeof(T) == 2 ? (k & 3) + (k >> 3 & 1) * 4 : k >> 2 & 3) & (kGranules & (kGranules - 1) ? 0 : kGranules - 1);
+  // kAlongK: piece p of row x lies at p ^ turn(x), which takes eight values in the 16 rows that are read at once
+  HCNN_HD static uint32_t turn(uint32_t x) { return (x & 3) + (x / GROUP & 1) * 4; }
+  // kAcrossK: piece pc of stored row k lies at moved(k, pc), its own inverse: within its granule of 16 numbers and the granules by the bits
+  // of k in which the lanes of one read differ, as far as those do not differ in the granule or the piece themselves.
+  HCNN_HD static uint32_t moved(uint32_t k, uint32_t pc) {
+    constexpr uint32_t kIn = sizeof(T) == 2 ? 2 : 4, kMask = kGranules & (kGranules - 1) ? 0 : kGranules - 1;   // pieces of a granule
+    uint32_t granule, piece = 0;
+    if constexpr (sizeof(T) == 2) {
+      granule = GROUP == 4 ? (k & 3) + (k >> 3 & 1) * 4 : GROUP == 8 ? (k & 3) * 2 : (k & 1) * 4;
+      if (GROUP == 16) piece = k >> 1 & 1;
+    } else {
+      granule = GROUP == 4 ? k >> 2 & 3 : GROUP == 8 ? (k >> 3 & 1) * 2 : 0;
+      piece = GROUP == 4 ? 0 : GROUP == 8 ? k >> 2 & 1 : k >> 2 & 3;
+    }
+    return (pc / kIn ^ (granule & kMask)) * kIn + (pc % kIn ^ piece);
   }
   HCNN_HD static void store(char* lds, int tid, const U4 (&r)[kEach]) {
 #pragma unroll
@@ -397,9 +426,8 @@ struct GemmOperand {
   static constexpr bool kEvenWaves = kPieces % 64 == 0;
   HCNN_HD static uint32_t numbers(uint32_t c) {                                 // of a row at LDS piece c, from the stage's first number
     const uint32_t line = c / kRowPieces, pc = c % kRowPieces;
-    if constexpr (LAYOUT == kAlongK) return (pc ^ (line & 7)) * kPer16;
-    else if constexpr (sizeof(T) == 2) return ((pc / 2 ^ swap(line)) * 2 + pc % 2) * kPer16;
-    else return ((pc / 4 ^ swap(line)) * 4 + pc % 4) * kPer16;
+    if constexpr (LAYOUT == kAlongK) return (pc ^ turn(line)) * kPer16;
+    else return moved(line, pc) * kPer16;
   }
   // Byte offsets of a thread's pieces from direct_base, for the whole sum.  Rows beyond X read a row that exists, pieces beyond X the
   // row's first one.
@@ -439,26 +467,30 @@ struct GemmOperand {
     __builtin_memcpy(lds + lane * 16, reinterpret_cast<const char*>(base) + off, 16);
 #endif
   }
-  // 16 bytes of row `base + lane % 16` of step s of a stage; base a multiple of 16
+  // row of lane i (of 16) for product j
+  HCNN_HD static uint32_t row_of(uint32_t j, uint32_t i) { return GROUP == 4 ? j * 16 + i : i / 4 * GROUP + j * 4 + i % 4; }
+  // 16 bytes of the lane's row of step s of a stage, for product j of the wave whose first row is `base` (a multiple of 16)
 #if defined(__HIP_DEVICE_COMPILE__)
-  __device__ __forceinline__ static hcnn_word4 read(const char* lds, uint32_t base, uint32_t s, uint32_t lane) {
+  __device__ __forceinline__ static hcnn_word4 read(const char* lds, uint32_t base, uint32_t j, uint32_t s, uint32_t lane) {
     const uint32_t g = lane / 16, i = lane % 16;
     if constexpr (LAYOUT == kAlongK) {
-      return *reinterpret_cast<const hcnn_word4*>(lds + place(base + i, s * 4 + g));
+      return *reinterpret_cast<const hcnn_word4*>(lds + place(base + row_of(j, i), s * 4 + g));
     } else if constexpr (sizeof(T) == 2) {
+      // (lanes 4 l .. 4 l + 3 of 16 point at the four runs of rows at k = l)
       typedef short four __attribute__((ext_vector_type(4)));
       typedef four __attribute__((address_space(3)))* lptr;
-      const uint32_t k = s * 32 + g * 8 + i / 4;
-      const four lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(lds + place(k, base / 8) + (i % 4) * 8));
-      const four hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(lds + place(k + 4, base / 8) + (i % 4) * 8));
+      const uint32_t k = s * 32 + g * 8 + i / 4, x = base + row_of(j, i % 4 * 4);
+      const four lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(lds + place(k, x / 8) + x % 8 * 2));
+      const four hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lptr)(lds + place(k + 4, x / 8) + x % 8 * 2));
       typedef uint32_t two __attribute__((ext_vector_type(2)));
       const two l = __builtin_bit_cast(two, lo), h = __builtin_bit_cast(two, hi);
       return hcnn_word4{l.x, l.y, h.x, h.y};
     } else {
       hcnn_word4 v;
+      const uint32_t x = base + row_of(j, i);
 #pragma unroll
-      for (uint32_t j = 0; j < 4; ++j)
-        v[j] = *reinterpret_cast<const uint32_t*>(lds + place(s * 16 + g * 4 + j, base / 4) + i * 4);
+      for (uint32_t e = 0; e < 4; ++e)
+        v[e] = *reinterpret_cast<const uint32_t*>(lds + place(s * 16 + g * 4 + e, x / 4) + x % 4 * 4);
       return v;
     }
   }
@@ -507,18 +539,17 @@ template <class T, int LA, int LB, int BM, int BN, int WM, int WN, int EPI, bool
 struct Gemm {
   static constexpr int kThreads = WM * WN * 64;
   static constexpr int kLoopPhases = 2;
-  // the sums leave through LDS, as many rows at a time as the stages' memory holds
-  static constexpr int kParts = BM * BN * 4 > 2 * (BM + BN) * 128 ? 2 : 1;
-  static constexpr int kPhases = EPI == kEpiStats ? 4 : 2 + 2 * kParts;
+  static constexpr int kPhases = EPI == kEpiStats ? 4 : 3;
   static constexpr int kMinWavesPerSimd = 2;
   static constexpr uint32_t kStage = GemmNum<T>::kStage;
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
   typedef GemmOperand<T, LA, BM, kThreads> A;
-  typedef GemmOperand<T, LB, BN, kThreads> B;
+  // 16-bit sums: a lane's lie side by side, 32 bytes of a row; 32-bit ones: those of four lanes do, 64 bytes of a row in one store
+  static constexpr int kGroup = sizeof(T) == 2 ? 4 * FN : 4;
+  typedef GemmOperand<T, LB, BN, kThreads, kGroup> B;
   static constexpr uint32_t kBuffer = A::kLdsBytes + B::kLdsBytes;
   static constexpr size_t kLdsBytes = 2 * kBuffer;
   static_assert(EPI != kEpiStats || BM * WN * 4 * 8 <= kLdsBytes, "the statistics fit the stages' memory");
-  static_assert(BM / kParts * BN * 4 <= kLdsBytes && WM % kParts == 0, "a part's sums fit the stages' memory");
 
   // Operands of the running step.  The next one's take the place of an a as soon as its products are under way; b and the last kAhead
   // of a have two places, so that their reads come first and the step's end does not wait for one that was just asked for.
@@ -649,10 +680,10 @@ struct Gemm {
   static constexpr int a_place(int s, int i) { return s && i >= FM - kAhead ? i + kAhead : i; }
 #if defined(__HIP_DEVICE_COMPILE__)
   __device__ __forceinline__ static void read_a(const char* lds, int s, int i, int tid, Regs& r) {
-    r.step.a[a_place(s, i)] = A::read(lds, m_wave(tid) + i * 16, s, tid % 64);
+    r.step.a[a_place(s, i)] = A::read(lds, m_wave(tid), i, s, tid % 64);
   }
   __device__ __forceinline__ static void read_b(const char* lds, int s, int j, int tid, Regs& r) {
-    r.step.b[s][j] = B::read(lds + A::kLdsBytes, n_wave(tid) + j * 16, s, tid % 64);
+    r.step.b[s][j] = B::read(lds + A::kLdsBytes, n_wave(tid), j, s, tid % 64);
   }
   __device__ __forceinline__ static void products(int s, int i, Regs& r) {
 #pragma unroll
@@ -665,7 +696,7 @@ struct Gemm {
   }
   HCNN_HD static void read_b(const char* lds, int s, int j, int tid, Regs& r) {
     for (uint32_t e = 0; e < 4; ++e)
-      for (uint32_t k = 0; k < kStep; ++k) r.step.b[s][j * 4 + e][k] = B::at(lds + A::kLdsBytes, n_wave(tid) + j * 16 + tid % 64 / 16 * 4 + e, s * kStep + k);
+      for (uint32_t k = 0; k < kStep; ++k) r.step.b[s][j * 4 + e][k] = B::at(lds + A::kLdsBytes, n_wave(tid) + B::row_of(j, tid % 64 / 16 * 4 + e), s * kStep + k);
   }
   HCNN_HD static void products(int s, int i, Regs& r) {
     for (int j = 0; j < FN; ++j)
@@ -693,7 +724,7 @@ struct Gemm {
   HCNN_HD static void phase(const GemmArgs& a, unsigned, int tid, uint32_t* lds_words, Regs& r) {
     char* lds = reinterpret_cast<char*>(lds_words);
     const uint32_t wave = (uint32_t)tid / 64, lane = (uint32_t)tid % 64;
-    const uint32_t m_lane = wave / WN * (FM * 16) + lane % 16, n_lane = wave % WN * (FN * 16) + lane / 16 * 4;   // in the tile
+    const uint32_t m_lane = wave / WN * (FM * 16) + lane % 16, n_wave0 = wave % WN * (FN * 16);   // in the tile
     if constexpr (PH < 2) {
       char *here = lds + r.iter % 2 * kBuffer, *next = lds + (r.iter + 1) % 2 * kBuffer;
       const uint32_t k0 = r.k_begin + r.iter * kStage;
@@ -718,48 +749,31 @@ struct Gemm {
         if (k0 < r.k_end) multiply(next, 1, tid, r, [](int) {});
       }
     } else if constexpr (EPI != kEpiStats) {
-      constexpr uint32_t kPart = (PH - 2) / 2, kRows = BM / kParts, kQuads = BN / 4;
-      if constexpr (PH % 2 == 0) {
-        if (wave / WN / (WM / kParts) != kPart) return;
+      // a lane has W numbers side by side of FM rows, 4 FN / W times; R rows at a time (two: their residuals come together)
+      constexpr int W = kGroup, R = FM % 2 == 0 ? 2 : 1;
 #pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-          for (int j = 0; j < FN; ++j) {
-            const uint32_t m = m_lane + i * 16 - kPart * kRows;
-            float v[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = r.acc[i][j][e];
-            __builtin_memcpy(lds + (m * kQuads + quad_at(m, n_lane / 4 + j * 4)) * 16, v, 16);
-          }
-      } else {
-        // a thread keeps its columns and goes down the rows
-        constexpr uint32_t W = sizeof(T) == 2 && kQuads % 2 == 0 ? 8 : 4, kAcross = BN / W;
-        static_assert(kThreads % kAcross == 0, "whole rows");
-        const uint32_t c = (uint32_t)tid % kAcross, n = r.n0 + c * W;
-        if (n >= a.N) return;
+      for (int j0 = 0; j0 < FN; j0 += W / 4) {
+        const uint32_t n = r.n0 + n_wave0 + B::row_of(j0, lane / 16 * 4);
+        if (n >= a.N) continue;
         const uint32_t left = a.N - n;
         float bias[W] = {};
         if (EPI == kEpiOut && a.bias) load_row(static_cast<const T*>(a.bias) + n, left, bias);
-        constexpr uint32_t kDown = kThreads / kAcross, kTurns = kRows / kDown, R = kTurns % 4 == 0 ? 4 : kTurns % 2 == 0 ? 2 : 1;
-        static_assert(kRows % kDown == 0, "whole turns");
-#pragma unroll 1
-        for (uint32_t turn = 0; turn < kTurns; turn += R) {
+#pragma unroll
+        for (int i0 = 0; i0 < FM; i0 += R) {
           uint32_t m[R];
           float v[R][W];
 #pragma unroll
-          for (uint32_t i = 0; i < R; ++i) {
-            const uint32_t line = (uint32_t)tid / kAcross + (turn + i) * kDown;
-            m[i] = r.m0 + kPart * kRows + line;
+          for (int i = 0; i < R; ++i) {
+            m[i] = r.m0 + m_lane + (i0 + i) * 16;
             if (m[i] >= r.M) m[i] = ~0u;
 #pragma unroll
-            for (uint32_t q = 0; q < W / 4; ++q) __builtin_memcpy(v[i] + q * 4, lds + (line * kQuads + quad_at(line, c * (W / 4) + q)) * 16, 16);
+            for (int e = 0; e < W; ++e) v[i][e] = r.acc[i0 + i][j0 + e / 4][e % 4];
           }
-          if (m[0] == ~0u) break;
           if constexpr (EPI == kEpiDelta) {
             // the gradient of the row's loss for its scores, times delta_scale: an operand of the two products after this, so that
             // it is rounded to their type here
 #pragma unroll
-            for (uint32_t i = 0; i < R; ++i) {
+            for (int i = 0; i < R; ++i) {
               if (m[i] == ~0u) continue;
               const float lse = a.lse[m[i]];
               const uint32_t t = a.target[m[i]] - a.n_offset;
@@ -768,21 +782,23 @@ struct Gemm {
               store_row(static_cast<T*>(a.out) + (size_t)m[i] * a.ld_out + n, left, v[i]);
             }
           } else {
+            // (rows of sums have room for whole quads)
+            const uint32_t quads = (left + 3) / 4 * 4;
             if (a.addend && r.split == 0) {
 #pragma unroll
-              for (uint32_t i = 0; i < R; ++i) {
+              for (int i = 0; i < R; ++i) {
                 if (m[i] == ~0u) continue;
                 float old[W];
-                load_row(a.addend + (size_t)m[i] * a.ld_sums + n, old);
+                load_row(a.addend + (size_t)m[i] * a.ld_sums + n, quads, old);
 #pragma unroll
-                for (uint32_t e = 0; e < W; ++e) v[i][e] += old[e];
+                for (int e = 0; e < W; ++e) v[i][e] += old[e];
               }
             }
             if constexpr (EPI == kEpiOut) finish<T>(a, m, n, bias, v);
             else {
 #pragma unroll
-              for (uint32_t i = 0; i < R; ++i)
-                if (m[i] != ~0u) store_row(a.sums + ((size_t)r.split * a.M + m[i]) * a.ld_sums + n, v[i]);
+              for (int i = 0; i < R; ++i)
+                if (m[i] != ~0u) store_row(a.sums + ((size_t)r.split * a.M + m[i]) * a.ld_sums + n, quads, v[i]);
             }
           }
         }
@@ -800,12 +816,12 @@ struct Gemm {
           for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              if (r.n0 + n_lane + j * 16 + e < a.N) top = fmaxf(top, r.acc[i][j][e]);
+              if (r.n0 + n_wave0 + B::row_of(j, lane / 16 * 4 + e) < a.N) top = fmaxf(top, r.acc[i][j][e]);
 #pragma unroll
           for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const uint32_t n = r.n0 + n_lane + j * 16 + e;
+              const uint32_t n = r.n0 + n_wave0 + B::row_of(j, lane / 16 * 4 + e);
               if (n < a.N) sum += exp_of(r.acc[i][j][e] - top);
               if (n == t) a.target_score[m] = r.acc[i][j][e];
             }
@@ -825,11 +841,6 @@ struct Gemm {
         to[a.ld_stats] = sum;
       }
     }
-  }
-  // 16 bytes of sums in LDS: the rows that a wave writes at once go to different banks
-  HCNN_HD static uint32_t quad_at(uint32_t m, uint32_t quad) {
-    constexpr uint32_t kQuads = BN / 4;
-    return kQuads >= 16 ? quad ^ (m & 15) : quad ^ (m / (16 / kQuads) & (kQuads - 1));
   }
 };
 
