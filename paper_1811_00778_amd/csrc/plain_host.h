@@ -77,7 +77,7 @@ Shape choose(const hcnn_plain* h, size_t M, size_t N, size_t K, bool may_split, 
   for (int t = kTile256; t <= kFlat; ++t) {
     if (t == kTile256 && (wide || !direct)) continue;
     const size_t tiles = std::max<size_t>(1, blocks(M, kTileRows[t]) * blocks(N, kTileCols[t]));
-    for (size_t s = 1; s == 1 || (may_split && s * 2 <= stages && s <= 64); s += s < 4 ? 1 : s / 2) {
+    for (size_t s = 1; s == 1 || (may_split && s * 2 <= stages && s <= 64); s += s < 8 ? 1 : s / 4) {
       const double load = std::ceil((double)(tiles * s) / units), turns = std::ceil(load / kHeld[t]);
       const double stage = std::max(kAlone * turns, load * kFull[t]) * (direct ? 1.0 : 1.6);
       double us = (double)blocks(stages, s) * stage + turns * kEnds[t];
@@ -109,9 +109,11 @@ bool direct_input(const Input& x) {
   const bool aligned = x.packed || (reinterpret_cast<uintptr_t>(x.p) % 16 == 0 && x.ld * sizeof(T) % 16 == 0);
   return aligned && 257 * x.ld * sizeof(T) < ((size_t)1 << 32);
 }
-// Copies pay from some size of the products that take the operand on: `work` = M N K of all of them.  By measurement (bfloat16,
-// M = N = K, us with / without copies of both operands): see kPackWork.
-constexpr double kPackWork = 3e-15, kPackByte = 5e-13, kPackLaunch = 5e-6;
+// Copies pay from some size of the products that take the operand on: `work` = M N K of all of them against a launch and the bytes read
+// and written.  Measured with and without copies of both operands, bfloat16 products of odd sizes M = N = K, us: 1001 20.4 / 15.0,
+// 2001 54.6 / 50.0, 2501 70.0 / 70.8, 4001 157 / 225; 8192 x 517 x 1000 34.5 / 24.4, 256 x 4001 x 4001 43.5 / 35.7.  32-bit
+// products are bound by the matrix unit either way.
+constexpr double kPackWork = 0.6e-15, kPackByte = 2e-13, kPackLaunch = 4e-6;       // seconds
 template <class T>
 void plan_pack(Input& x, Arena& a, double work) {
   if (sizeof(T) != 2 || direct_input<T>(x) || x.rows == 0 || x.cols == 0) return;
