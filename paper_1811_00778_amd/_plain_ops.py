@@ -179,25 +179,31 @@ class PlainOpsMixin:
             if [t[1:] for t in to] != [f[1:] for f in flat]:
                 raise ValueError("out must match grads in number, sizes and types")
             if any(t[0] != f[0] for t, f in zip(to, flat)):
-                self._clip_apart(grads, out, flat, to)
+                self._clip_apart(flat, to)
             outs = (C.c_void_p * n)(*[t[0] for t in to])
         norm = self._new((), None)
         self._pre_call()
         self.raw.call("hcnn_clip_grad_norm", n, ptrs, counts, types, outs, float(max_norm), float(eps), self._address(norm))
         return norm
 
-    def _clip_apart(self, grads, out, flat, to):
+    def _clip_apart(self, flat, to):
         """No result may overlap a gradient other than its own, which it may replace, nor another result."""
-        spans = [(f[0], f[0] + f[1] * (4 if f[2] == _capi.F32 else 2), i, 0) for i, f in enumerate(flat) if f[1]]
-        spans += [(t[0], t[0] + t[1] * (4 if t[2] == _capi.F32 else 2), i, 1) for i, t in enumerate(to) if t[1] and t[0] != flat[i][0]]
+        size = {_capi.F32: 4, _capi.F16: 2, _capi.BF16: 2}
+        spans = []                             # (first byte, one past the last, written)
+        for f, t in zip(flat, to):
+            if f[1]:
+                n = f[1] * size[f[2]]
+                spans.append((f[0], f[0] + n, f[0] == t[0]))
+                if f[0] != t[0]:
+                    spans.append((t[0], t[0] + n, True))
         spans.sort()
         end = written = 0                      # the furthest byte so far, of all and of what is written
-        for a, b, i, kind in spans:
-            if a < (end if kind or flat[i][0] == to[i][0] else written):
+        for first, last, writes in spans:
+            if first < (end if writes else written):
                 raise ValueError("out must not overlap grads or itself")
-            end = max(end, b)
-            if kind or flat[i][0] == to[i][0]:
-                written = max(written, b)
+            end = max(end, last)
+            if writes:
+                written = max(written, last)
 
     # ---- diagnostics
     def bad_inputs(self):

@@ -125,6 +125,7 @@ class PlainContext(PlainOpsMixin):
         if self.device.index is None:
             self.device = torch.device(self.device.type, torch.cuda.current_device())
         torch.cuda.set_device(self.device)
+        self._index = self.device.index
         self._stream = torch.cuda.current_stream(self.device).cuda_stream
         self.raw = _capi.RawPlain(lib(), self._stream)
 
@@ -136,11 +137,11 @@ class PlainContext(PlainOpsMixin):
 
     def _pre_call(self):
         # (the raw handle: a stream object's making takes a fifth of a small call)
-        if torch._C._cuda_getCurrentRawStream(self.device.index) != self._stream:
+        if torch._C._cuda_getCurrentRawStream(self._index) != self._stream:
             Context._pre_call(self)
 
     def _matrix(self, x, what):
-        if not isinstance(x, torch.Tensor) or x.dtype not in _PLAIN_DT or x.device != self.device or x.dim() != 2:
+        if not isinstance(x, torch.Tensor) or x.dtype not in _PLAIN_DT or x.get_device() != self._index or x.dim() != 2:
             raise TypeError("%s must be a 2-D float32, float16 or bfloat16 tensor on %s" % (what, self.device))
         rows, cols = x.shape
         stride, step = x.stride()
@@ -149,7 +150,7 @@ class PlainContext(PlainOpsMixin):
         return x.data_ptr(), rows, cols, stride, _PLAIN_DT[x.dtype]
 
     def _flat(self, x, what):
-        if not isinstance(x, torch.Tensor) or x.dtype not in _PLAIN_DT or x.device != self.device or not x.is_contiguous():
+        if not isinstance(x, torch.Tensor) or x.dtype not in _PLAIN_DT or x.get_device() != self._index or not x.is_contiguous():
             raise TypeError("%s must be contiguous float32, float16 or bfloat16 tensors on %s" % (what, self.device))
         return x.data_ptr(), x.numel(), _PLAIN_DT[x.dtype]
 
@@ -160,8 +161,8 @@ class PlainContext(PlainOpsMixin):
         return got
 
     def _targets(self, x, what):
-        if not isinstance(x, torch.Tensor) or x.dtype not in (torch.int32, torch.int64) or x.device != self.device or x.dim() != 1 \
-                or not x.is_contiguous():
+        if not isinstance(x, torch.Tensor) or x.dtype not in (torch.int32, torch.int64) or x.get_device() != self._index \
+                or x.dim() != 1 or not x.is_contiguous():
             raise TypeError("%s must be a contiguous 1-D int32 or int64 tensor on %s" % (what, self.device))
         return x.data_ptr(), x.numel(), x.element_size()
 

@@ -1983,5 +1983,11 @@ void hcnn_emu_device(uint32_t units, size_t largest_allocation) { emu_units = un
 }  // extern "C"
 
 #ifdef HCNN_HOSTEMU
-#include "plain.cpp"        // the checker is built from this file alone
+// The checker is built from this file alone.  (Less optimised here: half the compile time; none where its tests do not run it.)
+#ifdef HCNN_SHARED_ALL
+#pragma GCC optimize("O0")
+#else
+#pragma GCC optimize("O1")
+#endif
+#include "plain.cpp"
 #endif

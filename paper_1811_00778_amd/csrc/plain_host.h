@@ -102,7 +102,7 @@ struct Input {
   size_t ld, rows, cols;
   bool packed = false;
   size_t offset = 0;
-  size_t extent() const { return rows && cols ? (rows - 1) * ld + cols : 0; }
+  size_t extent() const { return rows && cols ? packed ? rows * ld : (rows - 1) * ld + cols : 0; }
 };
 template <class T>
 bool direct_input(const Input& x) {
@@ -119,7 +119,7 @@ void plan_pack(Input& x, Arena& a, double work) {
   if (sizeof(T) != 2 || direct_input<T>(x) || x.rows == 0 || x.cols == 0) return;
   if (work * kPackWork < kPackLaunch + 4.0 * (double)x.rows * (double)x.cols * kPackByte) return;
   x.packed = true;
-  x.ld = up(x.cols, 8);
+  x.ld = up(x.cols, GemmNum<T>::kStage);                // whole stages along the row, zeros at its end
   x.offset = a.take(x.rows * x.ld * sizeof(T));
 }
 template <class T>
@@ -200,7 +200,7 @@ int linear(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void* x, 
   int e = reserve(h, ar.bytes);
   if (e || (e = pack<T>(h, ix, x, ldx)) || (e = pack<T>(h, iw, w, ldw))) return e;
   GemmArgs g = operands(ix, iw);
-  g.M = (uint32_t)M; g.N = (uint32_t)N; g.K = (uint32_t)K;
+  g.M = (uint32_t)M; g.N = (uint32_t)N; g.K = (uint32_t)(ix.packed && iw.packed ? ix.ld : K);
   g.act = act; g.bias = bias; g.residual = residual; g.ld_residual = ld_residual;
   g.out = y; g.ld_out = ldy; g.z = z; g.ld_z = ldz;
   return product<T, kAlongK, kAlongK>(h, g, s, at<float>(h, o_sums));
@@ -311,7 +311,7 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
   plan_pack<T>(ix, a, work);
   plan_pack<T>(iw, a, work);
   // the rows that take part, one behind the other: used where they are not all rows, or where x is copied anyway
-  Input ikept{c.x, up(K, 16 / sizeof(T)), M, K, true, ix.offset};
+  Input ikept{c.x, ix.packed ? ix.ld : up(K, 16 / sizeof(T)), M, K, true, ix.offset};
   if (!ix.packed) ikept.offset = a.take(M * ikept.ld * sizeof(T));
   // columns of a piece: whole tiles, all columns where they fit
   const size_t fit = kDeltaBytes / (std::max<size_t>(M, 1) * sizeof(T)) / 256 * 256;
@@ -343,7 +343,7 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
   }
   if (ix.packed) ix.p = at<void>(h, ikept.offset);
   GemmArgs g = operands(ix, iw);
-  g.M = (uint32_t)M; g.N = (uint32_t)V; g.K = (uint32_t)K;
+  g.M = (uint32_t)M; g.N = (uint32_t)V; g.K = (uint32_t)(ix.packed && iw.packed ? ix.ld : K);
   g.count = count; g.count_of = kCountM; g.kept = at<void>(h, ikept.offset); g.ld_kept = ikept.ld; g.kept_always = ix.packed;
   g.stats = at<float>(h, o_stats); g.ld_stats = ld_stats; g.target = target; g.target_score = score; g.lse = lse;
   g.delta_scale = delta_scale<T>();
@@ -363,7 +363,7 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
 
   for (size_t p = 0; p < pieces; ++p) {
     const size_t v0 = p * piece, n = std::min(piece, V - v0);
-    Input wp{static_cast<const char*>(iw.p) + v0 * iw.ld * sizeof(T), iw.ld, n, K};
+    Input wp{static_cast<const char*>(iw.p) + v0 * iw.ld * sizeof(T), iw.ld, n, K, iw.packed};
     idelta.cols = n;
     if (M && !narrow) {
       GemmArgs d = g;

@@ -387,11 +387,21 @@ struct GemmOperand {
     }
     return v;
   }
-  // ... straight to LDS, one piece after the other: for the one stage of a sum that is not whole, where registers are dear
+  // ... straight to LDS, DEEP pieces at a time: for the one stage of a sum that is not whole
+  template <int DEEP>
   HCNN_HD static void copy(const T* p, size_t ld, size_t extent, uint32_t X, uint32_t K, uint32_t x0, uint32_t k0, char* lds, int tid) {
 #pragma unroll 1
-    for (uint32_t c = (uint32_t)tid; c < (uint32_t)kPieces; c += THREADS)
-      *reinterpret_cast<U4*>(lds + place(c / kRowPieces, c % kRowPieces)) = load_one(p, ld, extent, X, K, x0, k0, c);
+    for (int i0 = 0; i0 < kEach; i0 += DEEP) {
+      U4 v[DEEP];
+#pragma unroll
+      for (int i = 0; i < DEEP; ++i)
+        if (i0 + i < kEach && mine(tid, i0 + i)) v[i] = load_one(p, ld, extent, X, K, x0, k0, (uint32_t)(tid + (i0 + i) * THREADS));
+#pragma unroll
+      for (int i = 0; i < DEEP; ++i) {
+        const uint32_t c = (uint32_t)(tid + (i0 + i) * THREADS);
+        if (i0 + i < kEach && mine(tid, i0 + i)) *reinterpret_cast<U4*>(lds + place(c / kRowPieces, c % kRowPieces)) = v[i];
+      }
+    }
   }
   HCNN_HD static uint32_t place(uint32_t line, uint32_t pc) {                  // byte of piece pc of stored row `line`
     if constexpr (LAYOUT == kAlongK) return line * 128 + ((pc ^ turn(line)) << 4);
@@ -606,8 +616,8 @@ struct Gemm {
     r.b = static_cast<const T*>(kept && a.count_of == kCountK ? a.kept : a.b);
     r.lda = kept && a.count_of == kCountM ? a.ld_kept : a.lda;
     r.ldb = kept && a.count_of == kCountK ? a.ld_kept : a.ldb;
-    r.a_extent = kept && a.count_of == kCountM ? (a.M - 1) * a.ld_kept + a.K : a.a_extent;
-    r.b_extent = kept && a.count_of == kCountK ? (a.K - 1) * a.ld_kept + a.N : a.b_extent;
+    r.a_extent = kept && a.count_of == kCountM ? a.M * a.ld_kept : a.a_extent;
+    r.b_extent = kept && a.count_of == kCountK ? a.K * a.ld_kept : a.b_extent;
     const uint32_t K = counted(a, kCountK, a.K), run = loop_count(a) * kStage;
     r.k_begin = r.split * run;
     r.k_end = K < r.k_begin + run ? K : r.k_begin + run;
@@ -622,6 +632,7 @@ struct Gemm {
   }
   // The stage at k0 to LDS, past the registers where it may be read whole: then in kDirect pieces that the caller spreads out
   static constexpr int kDirect = A::kEach + B::kEach;
+  static constexpr int kCopyDeep = FM * FN >= 32 ? 1 : 4;      // (the largest tile has no registers to spare)
   struct Bring {
     const T *pa, *pb;
     char* lds;
@@ -632,8 +643,8 @@ struct Gemm {
       pa = A::direct_base(r.a, r.lda, r.m0, k0);
       pb = B::direct_base(r.b, r.ldb, r.n0, k0);
       if (whole) return;
-      A::copy(r.a, r.lda, r.a_extent, r.M, r.k_end, r.m0, k0, lds, tid);
-      B::copy(r.b, r.ldb, r.b_extent, a.N, r.k_end, r.n0, k0, lds + A::kLdsBytes, tid);
+      A::template copy<kCopyDeep>(r.a, r.lda, r.a_extent, r.M, r.k_end, r.m0, k0, lds, tid);
+      B::template copy<kCopyDeep>(r.b, r.ldb, r.b_extent, a.N, r.k_end, r.n0, k0, lds + A::kLdsBytes, tid);
     }
     HCNN_HD void piece(int i, int tid, const Regs& r) const {
       if (i < A::kEach) A::direct(pa, lds, tid, i, r.oa);
@@ -890,7 +901,7 @@ struct GemmJoin {
   }
 };
 
-// A matrix of 16-bit numbers with rows that start on 16 bytes: eight numbers per thread.
+// A matrix of 16-bit numbers with rows that start on 16 bytes and end in zeros: eight numbers per thread.
 struct PackArgs {
   const void* from;
   size_t ld_from;
@@ -910,8 +921,10 @@ struct PackRows {
     if (at >= a.pieces) return;
     const size_t each = a.ld_to / 8, row = at / each;
     const uint32_t c = (uint32_t)(at - row * each) * 8;
-    const U4 v = Op::piece(static_cast<const Half*>(a.from), row * a.ld_from + c, (a.rows - 1) * a.ld_from + a.cols);
-    *reinterpret_cast<U4*>(static_cast<Half*>(a.to) + row * a.ld_to + c) = Op::first(v, a.cols - c < 8 ? a.cols - c : 8);
+    const uint32_t left = c < a.cols ? a.cols - c : 0;
+    U4 v{};
+    if (left) v = Op::first(Op::piece(static_cast<const Half*>(a.from), row * a.ld_from + c, (a.rows - 1) * a.ld_from + a.cols), left);
+    *reinterpret_cast<U4*>(static_cast<Half*>(a.to) + row * a.ld_to + c) = v;
   }
 };
 
@@ -1200,7 +1213,7 @@ struct Strip {
   static constexpr int R = SHARE == 8 ? 1 : 4, kDeep = SHARE == 8 ? 8 : 2;
   static constexpr uint32_t kRows = SHARE == 8 ? 16 : kWaves * R * 16;         // of the streamed operand in a workgroup
   static constexpr int kPhases = LOSS ? 3 : SHARE == 8 ? 2 : 1;
-  static constexpr uint32_t kStep = GemmNum<T>::kStage / 2, kPer16 = GemmNum<T>::kPer16, kSpan = SHARE * kStep * kDeep;
+  static constexpr uint32_t kStep = GemmNum<T>::kStage / 2, kPer16 = GemmNum<T>::kPer16;
   static constexpr size_t kLdsBytes = (SHARE == 8 ? kWaves * 256 : LOSS ? kWaves * R * 256 : 0) * 4 + (LOSS ? kThreads * 8 : 0);
   typedef GemmOperand<T, kAlongK, 16, 64> Op;
   struct Regs {};
@@ -1222,7 +1235,7 @@ struct Strip {
     if constexpr (PH == 0) {
       const bool kept = LOSS && a.kept && (a.kept_always || M < a.M);
       const T *pa = static_cast<const T*>(kept ? a.kept : a.a), *pb = static_cast<const T*>(a.b);
-      const size_t lda = kept ? a.ld_kept : a.lda, a_extent = kept ? (a.M - 1) * a.ld_kept + a.K : a.a_extent;
+      const size_t lda = kept ? a.ld_kept : a.lda, a_extent = kept ? a.M * a.ld_kept : a.a_extent;
       const T *ps = NARROW ? pa : pb, *po = NARROW ? pb : pa;
       const size_t lds_ = NARROW ? lda : a.ldb, ldo = NARROW ? a.ldb : lda;
       const size_t es = NARROW ? a_extent : a.b_extent, eo = NARROW ? a.b_extent : a_extent;
@@ -1235,34 +1248,46 @@ struct Strip {
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[r][e] = 0.0f;
 #if defined(__HIP_DEVICE_COMPILE__)
-        const uint32_t first = (SHARE == 8 ? wave * kStep : 0) + g * kPer16;
+        const uint32_t mine = SHARE == 8 ? wave_uniform(wave) : 0, whole = a.K / kStep;        // the wave's first step; steps that are whole
         const T* at[R];
 #pragma unroll
-        for (int r = 0; r < R; ++r) at[r] = ps + (row + r * 16 < XS ? row + r * 16 : XS - 1) * lds_ + first;
-        const T* other = po + (i < XO ? i : XO - 1) * ldo + first;
-        for (uint32_t k0 = 0; k0 < a.K; k0 += kSpan) {
-          U4 fs[R][kDeep], fo[kDeep];
+        for (int r = 0; r < R; ++r) at[r] = ps + (row + r * 16 < XS ? row + r * 16 : XS - 1) * lds_ + g * kPer16;
+        const T* other = po + (i < XO ? i : XO - 1) * ldo + g * kPer16;
+        auto add = [&](const U4 (&fs)[R], const U4& fo) {
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            const hcnn_word4 s4{fs[r].x, fs[r].y, fs[r].z, fs[r].w}, o4{fo.x, fo.y, fo.z, fo.w};
+            mma<T>(acc[r], NARROW ? o4 : s4, NARROW ? s4 : o4);
+          }
+        };
+        // the step that is not whole, asked for before the others are waited for
+        const bool rest = whole * kStep < a.K && whole % SHARE == mine;
+        U4 rs[R], ro{};
+        if (rest) {
+          const uint32_t k = whole * kStep + g * kPer16;
+#pragma unroll
+          for (int r = 0; r < R; ++r) rs[r] = piece(ps, lds_, es, XS, a.K, row + r * 16, k);
+          ro = piece(po, ldo, eo, XO, a.K, i, k);
+        }
+        for (uint32_t s = mine; s < whole; s += SHARE * kDeep) {
+          U4 fs[kDeep][R], fo[kDeep];
 #pragma unroll
           for (int d = 0; d < kDeep; ++d) {
-            const uint32_t step = k0 + d * (SHARE * kStep) + (SHARE == 8 ? wave_uniform(wave) * kStep : 0);
-            if (step + kStep <= a.K) {
+            const uint32_t step = s + d * SHARE;
+            if (step < whole) {
 #pragma unroll
-              for (int r = 0; r < R; ++r) fs[r][d] = ld16(reinterpret_cast<const char*>(at[r] + k0 + d * (SHARE * kStep)));
-              fo[d] = ld16(reinterpret_cast<const char*>(other + k0 + d * (SHARE * kStep)));
+              for (int r = 0; r < R; ++r) fs[d][r] = ld16(reinterpret_cast<const char*>(at[r] + step * kStep));
+              fo[d] = ld16(reinterpret_cast<const char*>(other + step * kStep));
             } else {
 #pragma unroll
-              for (int r = 0; r < R; ++r) fs[r][d] = piece(ps, lds_, es, XS, a.K, row + r * 16, step + g * kPer16);
-              fo[d] = piece(po, ldo, eo, XO, a.K, i, step + g * kPer16);
+              for (int r = 0; r < R; ++r) fs[d][r] = U4{};
+              fo[d] = U4{};
             }
           }
 #pragma unroll
-          for (int d = 0; d < kDeep; ++d)
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-              const hcnn_word4 s4{fs[r][d].x, fs[r][d].y, fs[r][d].z, fs[r][d].w}, o4{fo[d].x, fo[d].y, fo[d].z, fo[d].w};
-              mma<T>(acc[r], NARROW ? o4 : s4, NARROW ? s4 : o4);
-            }
+          for (int d = 0; d < kDeep; ++d) add(fs[d], fo[d]);
         }
+        if (rest) add(rs, ro);
 #else
         for (int r = 0; r < R; ++r)
           for (uint32_t k0 = SHARE == 8 ? wave * kStep : 0; k0 < a.K; k0 += SHARE * kStep)
@@ -1390,6 +1415,7 @@ struct SortRows {
 #pragma unroll 4
     for (size_t b = (size_t)lane * 16; b < whole; b += 1024) st16(to + b, ld16(from + b));
     for (size_t b = whole + (size_t)lane * 2; b < a.row_bytes; b += 128) *reinterpret_cast<uint16_t*>(to + b) = *reinterpret_cast<const uint16_t*>(from + b);
+    for (size_t b = a.row_bytes + (size_t)lane * 2; b < a.ld_kept; b += 128) *reinterpret_cast<uint16_t*>(to + b) = 0;
   }
 };
 
