@@ -176,7 +176,7 @@ int hcnn_clip_grad_norm(hcnn_plain* h, size_t n_tensors, const void* const* grad
       if (!down) n.part_first += n.first[n.tensors];
     }
   };
-  // one workgroup takes up to 32768 numbers in one launch (14375 numbers of three tensors: 8 us, in three launches 22)
+  // one workgroup takes up to 32768 numbers in one launch (14375 numbers of three tensors: 12.5 us a call, in three launches 21.8)
   if (numbers <= kClipSmall && filled <= kNormTensors) {
     for (size_t i = 0; i < n_tensors; ++i)
       if (counts_host[i]) add(i);

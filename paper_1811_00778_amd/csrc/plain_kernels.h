@@ -170,7 +170,7 @@ HCNN_HD float recip(float x) {            // to about one unit of the last place
 }
 // P(X <= z) of a normal X, and bell = e^(-z^2 / 2).  The tail is bell * Q(t) with t = 1 / (1 + 0.2333 |z|) and Q the polynomial without
 // constant term that fits P(X <= -a) e^(a^2 / 2) on a >= 0 best in the sense of the largest relative error (9e-8; 4e-7 as evaluated here):
-// the tail's own digits stay right, and it costs a third of the library's erf (134 M numbers of a layer's ending: 100 us, now 38).
+// the tail's own digits stay right, and it costs a third of the library's erf (134 M numbers of a layer's ending: 100 us, now 55).
 HCNN_HD float normal_cdf(float z, float* bell) {
   const float t = recip(1.0f + 0.23333333333f * fabsf(z)), e = exp2_of(-0.72134752044f * z * z);
   float q = -0.06778094120f;
@@ -856,7 +856,7 @@ struct Gemm {
 };
 
 // Joins the parts of k: four outputs of a row for SIDE threads, which share the parts.  (50 x 125 outputs of 63 parts: 9.1 us with one
-// thread each, in 7 workgroups; few outputs need the parts side by side.)
+// thread each, in 7 workgroups; few outputs need the parts side by side: 4.1.)
 template <class T, int SIDE>
 struct GemmJoin {
   static constexpr int kThreads = 256, kQuads = kThreads / SIDE;
@@ -1200,8 +1200,8 @@ struct MeanLoss {
 // the registers that the products read (lane: row lane % 16, 16 bytes lane / 16 of a 64-byte step of k); no wave waits for another.
 //   SHARE 8  a workgroup takes 16 of its rows, eight waves every eighth step of k each, kDeep steps asked for at a time; sums join in LDS
 //   SHARE 1  a wave takes 4 x 16 rows and all of k (short rows: at most 1 KiB)
-// GPU us: one row of 4096 x 4096 bfloat16 weights in tiles of 16 x 128, 16 parts of k and their join 5.4 + 4.5, this 7.2; 147456 rows of
-// 25 numbers by 5 filters in tiles of 128 x 16 10.2, this 6.4.
+// GPU us: one row of 4096 x 4096 bfloat16 weights in tiles of 16 x 128, 16 parts of k and their join 5.4 + 4.5, this 8.1; 147456 rows of
+// 25 numbers by 5 filters in tiles of 128 x 16 10.2, this 8.5.
 // LOSS (NARROW): the scores of at most 16 classes end in the rows' losses and the gradients for the scores.
 struct StripLossArgs { GemmArgs g; RowStatsArgs rows; };
 template <bool LOSS> struct StripArgs { typedef GemmArgs type; };

@@ -63,7 +63,7 @@ def _reference(weights, x, labels):
             h = h.reshape(h.shape[0], -1) @ w.t()
     loss = F.cross_entropy(h, labels.cpu())
     loss.backward()
-    return float(loss), [None if w is None else w.grad for w in ws]
+    return float(loss.detach()), [None if w is None else w.grad for w in ws]
 
 
 @pytest.mark.gpu
