@@ -828,12 +828,14 @@ struct Gemm {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (r.n0 + n_wave0 + B::row_of(j, lane / 16 * 4 + e) < a.N) top = fmaxf(top, r.acc[i][j][e]);
+          // (scores of -infinity only: relative to 0, so that they add nothing, where the difference of two infinities is no number)
+          const float from = top == -INFINITY ? 0.0f : top;
 #pragma unroll
           for (int j = 0; j < FN; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const uint32_t n = r.n0 + n_wave0 + B::row_of(j, lane / 16 * 4 + e);
-              if (n < a.N) sum += exp_of(r.acc[i][j][e] - top);
+              if (n < a.N) sum += exp_of(r.acc[i][j][e] - from);
               if (n == t) a.target_score[m] = r.acc[i][j][e];
             }
           const uint32_t at = (wave % WN * 4 + lane / 16) * BM + m_lane + i * 16;
@@ -1116,7 +1118,7 @@ HCNN_HD float row_loss(const RowStatsArgs& a, uint32_t m, float top, float sum, 
   *lse_out = lse;
   return l;
 }
-// 64 rows per workgroup, four threads each.
+// 64 rows per workgroup, four threads each.  A part without a sum adds nothing: its scores are all -infinity, or there are none.
 struct RowStats {
   static constexpr int kThreads = 256;
   static constexpr uint32_t kRows = 64;
@@ -1135,7 +1137,7 @@ struct RowStats {
         for (uint32_t t = tid / kRows; t < a.tiles; t += 4) {
           const float* s = a.stats + (size_t)t * 2 * a.ld_stats + m;
           const float x = s[0], y = s[a.ld_stats], high = fmaxf(top, x);
-          sum = (sum != 0.0f ? sum * exp_of(top - high) : 0.0f) + y * exp_of(x - high);
+          sum = (sum != 0.0f ? sum * exp_of(top - high) : 0.0f) + (y != 0.0f ? y * exp_of(x - high) : 0.0f);
           top = high;
         }
       lds[tid] = top;
