@@ -362,7 +362,9 @@ int hcnn_linear(hcnn_plain* h, int dtype, int activation, size_t rows, size_t n_
 
 /* Gradients of hcnn_linear for dy_dev [rows][n_out]: with dz = dy * act'(z),
  *   dx = dz w,  dw = dz^T x,  db = sum over rows of dz   (the residual's is dy); NULL for those not wanted.
- * dz is rounded to the call's type before the two products take it (and not for db).  z_dev may be NULL when the activation is NONE,
+ * dz is rounded to the call's type before the two products take it (and not for db).  In binary16, where such products of two numbers leave the
+ * range, dz is held times a power of two for each row of dx and of dw (not with the activations NONE and RELU, whose dz are dy's numbers): a
+ * number keeps its 11 bits down to 2^-28 of the largest finite one of its row or column, and vanishes below 2^-39 of it.  z_dev may be NULL when the activation is NONE,
  * w_dev without dx_dev, x_dev without dw_dev. */
 int hcnn_linear_grad(hcnn_plain* h, int dtype, int activation, size_t rows, size_t n_in, size_t n_out,
                      const void* dy_dev, size_t dy_stride, const void* x_dev, size_t x_stride, const void* w_dev, size_t w_stride,

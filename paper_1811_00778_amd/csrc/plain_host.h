@@ -206,20 +206,29 @@ int linear(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void* x, 
   return product<T, kAlongK, kAlongK>(h, g, s, at<float>(h, o_sums));
 }
 
+enum { kSizeOnly, kTops, kGradients };
+template <class T, int LANES>
+int act_grad_lanes(hcnn_plain* h, const ActGradArgs& a, size_t grid, int what) {
+  if constexpr (std::is_same_v<T, Half>) {
+    if (what == kTops) return launch<ActTops<T, LANES>>(h->stream, grid, ActTops<T, LANES>::kLdsBytes, a);
+    if (a.row_top || a.col_top) return launch<ActGrad<T, LANES, kRoom>>(h->stream, grid, ActGrad<T, LANES, kRoom>::kLdsBytes, a);
+  }
+  return launch<ActGrad<T, LANES, kNoRoom>>(h->stream, grid, ActGrad<T, LANES, kNoRoom>::kLdsBytes, a);
+}
 template <class T>
-int act_grad(hcnn_plain* h, ActGradArgs a, size_t* row_blocks, bool only_size) {
+int act_grad(hcnn_plain* h, ActGradArgs a, size_t* row_blocks, int what) {
   // at least 64 rows a workgroup, and no more workgroups than eight for each compute unit
   const int lanes = a.N <= 16 ? 4 : a.N <= 64 ? 16 : 64;
   a.col_blocks = (uint32_t)std::max<size_t>(1, blocks(a.N, lanes * 4));
   const size_t most = std::max<size_t>(1, (size_t)h->compute_units * 8 / a.col_blocks);
   a.rows_each = (uint32_t)std::max<size_t>(64, up(blocks(a.M, most), 64));
   *row_blocks = blocks(a.M, a.rows_each);
-  if (only_size) return 0;
+  if (what == kSizeOnly) return 0;
   const size_t grid = *row_blocks * a.col_blocks;
   switch (lanes) {
-    case 4: return launch<ActGrad<T, 4>>(h->stream, grid, ActGrad<T, 4>::kLdsBytes, a);
-    case 16: return launch<ActGrad<T, 16>>(h->stream, grid, ActGrad<T, 16>::kLdsBytes, a);
-    default: return launch<ActGrad<T, 64>>(h->stream, grid, ActGrad<T, 64>::kLdsBytes, a);
+    case 4: return act_grad_lanes<T, 4>(h, a, grid, what);
+    case 16: return act_grad_lanes<T, 16>(h, a, grid, what);
+    default: return act_grad_lanes<T, 64>(h, a, grid, what);
   }
 }
 
@@ -232,16 +241,21 @@ int linear_grad(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void
   if (act != kActNone) { ag.z = z; ag.ld_z = ldz; }
   ag.ld_part = up(N, 4);
   size_t row_blocks = 0;
-  act_grad<T>(h, ag, &row_blocks, true);
+  act_grad<T>(h, ag, &row_blocks, kSizeOnly);
+  // dz in binary16 of a slope that is any number: times powers of two of its rows (for dx) and of its columns (for dw), see ActGrad
+  const bool room = std::is_same_v<T, Half> && act != kActNone && act != kActRelu;
   Arena ar;
   Input ix{x, ldx, M, K}, iw{w, ldw, N, K}, idz{dy, ld_dy, M, N};
   if (act != kActNone) {                                   // dz: aligned rows in the work memory
     idz.packed = true;
     idz.ld = up(N, 16 / sizeof(T));
-    idz.offset = ar.take(M * idz.ld * sizeof(T));
+    if (!room || dx) idz.offset = ar.take(M * idz.ld * sizeof(T));
   } else {
     plan_pack<T>(idz, ar, work * ((dx != nullptr) + (dw != nullptr)));
   }
+  Input idw = idz;                                         // dw's
+  if (room && dw) idw.offset = ar.take(M * idz.ld * sizeof(T));
+  const size_t o_tops = ar.take(room ? (M + N) * 4 : 0);
   if (dw) plan_pack<T>(ix, ar, work);
   if (dx) plan_pack<T>(iw, ar, work);
   const bool direct = direct_input<T>(idz);
@@ -252,14 +266,24 @@ int linear_grad(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void
   if (e || (e = pack<T>(h, ix, x, ldx)) || (e = pack<T>(h, iw, w, ldw))) return e;
   if (act == kActNone) {
     if ((e = pack<T>(h, idz, dy, ld_dy))) return e;
+    idw.p = idz.p;
   } else {
     idz.p = at<void>(h, idz.offset);
-    ag.dz = at<void>(h, idz.offset);
+    idw.p = at<void>(h, idw.offset);
+    ag.dz = room && !dx ? nullptr : at<void>(h, idz.offset);
     ag.ld_dz = idz.ld;
+  }
+  if (M && N && room && (dx || dw)) {
+    uint32_t* tops = at<uint32_t>(h, o_tops);
+    ag.row_top = dx ? tops : nullptr;
+    ag.col_top = dw ? tops + M : nullptr;
+    ag.dz_cols = dw ? at<void>(h, idw.offset) : nullptr;
+    if ((e = launch<ZeroWords>(h->stream, blocks(M + N, ZeroWords::kThreads), 0, ZeroWordsArgs{tops, M + N}))) return e;
+    if ((e = act_grad<T>(h, ag, &row_blocks, kTops))) return e;
   }
   if (M && N && (act != kActNone || db)) {
     if (db) ag.part = at<float>(h, o_part);
-    if ((e = act_grad<T>(h, ag, &row_blocks, false))) return e;
+    if ((e = act_grad<T>(h, ag, &row_blocks, kGradients))) return e;
   }
   if (db && N) {
     const ColumnSumArgs cs{at<float>(h, o_part), ag.ld_part, (uint32_t)(M ? row_blocks : 0), (uint32_t)N, db};
@@ -268,12 +292,14 @@ int linear_grad(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void
   if (dx) {
     GemmArgs g = operands(idz, iw);
     g.M = (uint32_t)M; g.N = (uint32_t)K; g.K = (uint32_t)N;
+    g.top = ag.row_top;
     g.out = dx; g.ld_out = ld_dx;
     if ((e = product<T, kAlongK, kAcrossK>(h, g, sx, at<float>(h, o_sums)))) return e;
   }
   if (dw) {
-    GemmArgs g = operands(idz, ix);
+    GemmArgs g = operands(idw, ix);
     g.M = (uint32_t)N; g.N = (uint32_t)K; g.K = (uint32_t)M;
+    g.top = ag.col_top;
     g.out = dw; g.ld_out = ld_dw;
     if ((e = product<T, kAcrossK, kAcrossK>(h, g, sw, at<float>(h, o_sums)))) return e;
   }

@@ -159,6 +159,13 @@ HCNN_HD void store_row(T* p, uint32_t left, const float (&v)[W]) {
   }
 }
 
+// ---------------------------------------------------------------- room in binary16
+// The power of two that brings numbers, the largest of them of magnitude `top` (its bits), to below 2^15, the largest to 2^14 or more (numbers below
+// 2^-86: times 2^100); and its inverse.
+HCNN_HD uint32_t room_exponent(uint32_t top) { return top >> 23 > 41 ? top >> 23 : 41; }
+HCNN_HD float room_of(uint32_t top) { return bits_float((268 - room_exponent(top)) << 23); }
+HCNN_HD float room_back(uint32_t top) { return bits_float((room_exponent(top) - 14) << 23); }
+
 // ---------------------------------------------------------------- activations
 enum { kActNone = 0, kActSquare = 1, kActRelu = 2, kActGelu = 3, kActSilu = 4, kActCount = 5 };
 HCNN_HD float recip(float x) {            // to about one unit of the last place
@@ -262,6 +269,7 @@ struct GemmArgs {
   size_t ld_sums;              // a multiple of 8
   const float* addend;         // [M][ld_sums], added to the sums of the first part (may be null; may be `sums`)
   const float* alpha;          // device factor of the sums (may be null)
+  const uint32_t* top;         // [M] binary16: the sums of row m are room_of(top[m]) times too large (may be null)
   int act;
   const void* bias;            // [N]
   const void* residual;
@@ -295,6 +303,15 @@ HCNN_HD void finish(const GemmArgs& a, const uint32_t (&m)[B], uint32_t n, const
 #pragma unroll
       for (int e = 0; e < W; ++e) v[i][e] *= alpha;
   }
+  if constexpr (std::is_same_v<T, Half>)
+    if (a.top) {
+#pragma unroll
+      for (int i = 0; i < B; ++i) {
+        const float back = m[i] != ~0u ? room_back(a.top[m[i]]) : 0.0f;
+#pragma unroll
+        for (int e = 0; e < W; ++e) v[i][e] *= back;
+      }
+    }
 #pragma unroll
   for (int i = 0; i < B; ++i)
 #pragma unroll
@@ -933,15 +950,22 @@ struct PackRows {
 // ---------------------------------------------------------------- gradient of the activation and of the bias
 // dz = dy * act'(z) (written where z is there: rounded to T, the operand type of the two products that take it) and, per block of
 // rows, the columns' sums of it in 32 bits.  A workgroup takes `rows_each` rows and kCols columns: lanes along the row, four numbers each.
+// binary16 does not hold the products of two of its numbers: 300 x 200 x 2 is infinite there, 1e-4 x 1e-4 nothing.  Where the slope is any
+// number (kRoom), dz is held once for each product, times a power of two for each row of dx or of dw (room_of the largest finite number of that row
+// or column of dz), which goes back out of the product's sums; ActTops finds the largest ones before.  What it costs, us of the whole call with silu,
+// bfloat16 / binary16: 8192 x 4096 -> 4096 485 / 580, 1024 x 1024 -> 1024 41.5 / 63, 16384 x 125 -> 50 29 / 43.
+enum { kNoRoom = 0, kRoom = 1 };
 struct ActGradArgs {
   const void *dy, *z;
   void* dz;
+  void* dz_cols;              // kRoom: dz times the columns' powers of two (dz: the rows'); either may be null there
+  uint32_t *row_top, *col_top;   // kRoom: bits of the largest magnitudes, 0 before ActTops; either may be null
   float* part;                // [row blocks][ld_part], null: no sums
   size_t ld_dy, ld_z, ld_dz, ld_part;
   uint32_t M, N, rows_each, col_blocks;
   int act;
 };
-template <class T, int LANES>
+template <class T, int LANES, int ROOM>
 struct ActGrad {
   static constexpr int kThreads = 256;
   static constexpr int kPhases = 2;
@@ -959,6 +983,11 @@ struct ActGrad {
       float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
       if (n < a.N) {
         const uint32_t left = a.N - n;
+        float room[4] = {};
+        if constexpr (ROOM == kRoom)
+          if (a.dz_cols)
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e) room[e] = e < left ? room_of(a.col_top[n + e]) : 0.0f;
 #pragma unroll 4
         for (uint32_t m = m0 + line; m < m1; m += kLines) {
           float v[4];
@@ -968,7 +997,22 @@ struct ActGrad {
             load_row(static_cast<const T*>(a.z) + m * a.ld_z + n, left, z);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] *= slope_of(z[e], a.act);
-            store_row(static_cast<T*>(a.dz) + m * a.ld_dz + n, left, v);
+            if constexpr (ROOM == kRoom) {
+              float t[4];
+              if (a.dz) {
+                const float of_row = room_of(a.row_top[m]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] = v[e] * of_row;
+                store_row(static_cast<T*>(a.dz) + m * a.ld_dz + n, left, t);
+              }
+              if (a.dz_cols) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) t[e] = v[e] * room[e];
+                store_row(static_cast<T*>(a.dz_cols) + m * a.ld_dz + n, left, t);
+              }
+            } else {
+              store_row(static_cast<T*>(a.dz) + m * a.ld_dz + n, left, v);
+            }
           }
 #pragma unroll
           for (int e = 0; e < 4; ++e) sum[e] += v[e];
@@ -983,6 +1027,84 @@ struct ActGrad {
         if (cb * kCols + c < a.N) a.part[(size_t)rb * a.ld_part + cb * kCols + c] = s;
       }
     }
+  }
+};
+// Largest finite magnitudes of dz in each row and column, in ActGrad's shape.  A largest number does not depend on the order of the atomics.
+template <class T, int LANES>
+struct ActTops {
+  static constexpr int kThreads = 256;
+  static constexpr int kPhases = 2;
+  static constexpr uint32_t kCols = LANES * 4, kLines = kThreads / LANES;
+  static constexpr size_t kLdsBytes = kThreads * 16;
+  struct Regs {};
+  HCNN_HD static uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
+  // The largest of a line's lanes for four rows, kLines apart: two exchanges leave a lane with one row's largest of four lanes, the others
+  // make it that of the line, and four lanes hand it over (7 exchanges of 64 lanes, 24 for each row by itself).
+  HCNN_HD static void row_tops(uint32_t* to, uint32_t rows, uint32_t lane, const uint32_t (&v)[4]) {   // to: the first row's; rows: that exist of it and those behind it
+#if defined(__HIP_DEVICE_COMPILE__)
+    const bool odd = lane & 1, high = lane & 2;
+    const uint32_t a0 = larger(odd ? v[2] : v[0], (uint32_t)__shfl_xor((int)(odd ? v[0] : v[2]), 1));
+    const uint32_t a1 = larger(odd ? v[3] : v[1], (uint32_t)__shfl_xor((int)(odd ? v[1] : v[3]), 1));
+    uint32_t b = larger(high ? a1 : a0, (uint32_t)__shfl_xor((int)(high ? a0 : a1), 2));
+#pragma unroll
+    for (int d = 4; d < LANES; d *= 2) b = larger(b, (uint32_t)__shfl_xor((int)b, d));
+    const uint32_t at = (odd ? 2 : 0) + (high ? 1 : 0);
+    if (lane < 4 && at * kLines < rows) atomic_max32(to + at * kLines, b);
+#else
+    for (uint32_t i = 0; i < 4; ++i)
+      if (i * kLines < rows) atomic_max32(to + i * kLines, v[i]);
+#endif
+  }
+  template <int PH>
+  HCNN_HD static void phase(const ActGradArgs& a, unsigned bid, int tid, uint32_t* lds, Regs&) {
+    const uint32_t cb = bid % a.col_blocks, rb = bid / a.col_blocks;
+    const uint32_t lane = (uint32_t)tid % LANES, line = (uint32_t)tid / LANES;
+    const uint32_t n = cb * kCols + lane * 4;
+    if constexpr (PH == 0) {
+      const uint32_t m0 = rb * a.rows_each, m1 = a.M - m0 < a.rows_each ? a.M : m0 + a.rows_each;
+      uint32_t top[4] = {};
+      // four rows at a time; what lies beyond the rows or columns is another look at the last of them
+      const uint32_t at = n < a.N ? n : (a.N - 1) / 4 * 4;
+      for (uint32_t mi = m0 + line; mi < m1; mi += 4 * kLines) {
+        float v[4][4], z[4][4];
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i) {
+          const uint32_t m = mi + i * kLines < m1 ? mi + i * kLines : m1 - 1;
+          load_row(static_cast<const T*>(a.dy) + m * a.ld_dy + at, a.N - at, v[i]);
+          load_row(static_cast<const T*>(a.z) + m * a.ld_z + at, a.N - at, z[i]);
+        }
+        uint32_t of_row[4] = {};
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e) {
+            uint32_t b = float_bits(v[i][e] * slope_of(z[i][e], a.act)) & 0x7fffffffu;
+            if (b >= 0x7f800000u) b = 0;
+            top[e] = larger(top[e], b);
+            of_row[i] = larger(of_row[i], b);
+          }
+        if (a.row_top) row_tops(a.row_top + mi, m1 - mi, lane, of_row);
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) lds[line * kCols + lane * 4 + e] = top[e];
+    } else if (a.col_top) {
+      for (uint32_t c = tid; c < kCols; c += kThreads) {
+        uint32_t t = 0;
+        for (uint32_t l = 0; l < kLines; ++l) t = larger(t, lds[l * kCols + c]);
+        if (cb * kCols + c < a.N) atomic_max32(a.col_top + cb * kCols + c, t);
+      }
+    }
+  }
+};
+struct ZeroWordsArgs { uint32_t* to; size_t count; };
+struct ZeroWords {
+  static constexpr int kThreads = 256;
+  static constexpr int kPhases = 1;
+  struct Regs {};
+  template <int PH>
+  HCNN_HD static void phase(const ZeroWordsArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
+    const size_t at = (size_t)bid * kThreads + tid;
+    if (at < a.count) a.to[at] = 0;
   }
 };
 struct ColumnSumArgs {

@@ -47,3 +47,62 @@ def check_low_classes(b, dtype, M, D, V, first, last, masked=0.2, seed=0):
         within(b.values(dx), DX, U[dtype] * np.abs(DX) + (q + (V + 8) * E * np.abs(p)) @ np.abs(W) + LEAST[dtype], "dx")
     within(b.values(dw)[~low], DW, U[dtype] * np.abs(DW) + (q + (M + 8) * E * np.abs(p)).T @ np.abs(X) + LEAST[dtype], "dw")
     assert (b.values(dw)[low] == 0).all()
+
+
+# (activation, rows, n_in, n_out, sizes of z, dy, w and x): gradients of binary16 whose dz leaves that type's range on either side,
+# though its operands and results do not
+RANGE = [("square", 20, 20, 20, 300.0, 200.0, 1e-3, 1e-4), ("square", 20, 20, 20, 1e-4, 1e-4, 1e4, 1e4), ("square", 65, 33, 270, 30.0, 1000.0, 1e-4, 1e-4),
+         ("square", 700, 9, 5, 200.0, 3000.0, 1e-4, 1e-6), ("gelu", 37, 41, 19, 1.0, 1.5e4, 1e-2, 1e-3), ("silu", 37, 41, 19, 2.0, 1e-5, 1e4, 1e4),
+         ("gelu", 130, 17, 50, 1.0, 1e-6, 1.5e4, 1e4), ("relu", 20, 30, 40, 1.0, 1.5e4, 1e-2, 1e-3)]
+
+
+def check_range(b, name, M, K, N, z, dy, w, x, seed=0, rows=None, cols=None):
+    """linear_grad in binary16.  dz may be held with a factor for each row (dx) or column (dw), whose largest number then has room for 2^-39 of itself:
+    what the type's 11 bits and smallest step leave.  rows, cols: factors of z and dy."""
+    rng = np.random.default_rng([seed, M, K, N, 6])
+
+    def sized(m, n, size):
+        return np.clip(normal(rng, m, n, std=size), -4 * size, 4 * size)
+
+    r, c = np.ones(M) if rows is None else rows, np.ones(N) if cols is None else cols
+    X, W = b.make(sized(M, K, x), "f16"), b.make(sized(N, K, w), "f16")
+    Z, DY = b.make(sized(M, N, z) * r[:, None] * c, "f16"), b.make(sized(M, N, dy) * r[:, None] * c, "f16")
+    dx, dw, db = b.ctx.linear_grad(DY, X, W, Z, activation=name, bias=True)
+    X, W, Z, DY = b.values(X), b.values(W), b.values(Z), b.values(DY)
+    assert all(np.isfinite(v).all() for v in (X, W, Z, DY))
+    DZ = DY * pc.act(Z, name)[1]
+    curve = np.abs(DY) * FN * 4 if name in ("gelu", "silu") else np.zeros_like(DY)
+    u, least = U["f16"], LEAST["f16"]
+    dDZ = (u + 4 * E) * np.abs(DZ) + curve
+    ex = dDZ + 2.0 ** -39 * np.abs(DZ).max(1, keepdims=True)
+    ew = dDZ + 2.0 ** -39 * np.abs(DZ).max(0, keepdims=True)
+    DX, DW, DB = DZ @ W, DZ.T @ X, DZ.sum(0)
+    assert max(np.abs(DX).max(), np.abs(DW).max()) < 60000
+    within(b.values(dx), DX, u * np.abs(DX) + (ex + (N + 4) * E * np.abs(DZ)) @ np.abs(W) + least, "dx")
+    within(b.values(dw), DW, u * np.abs(DW) + (ew + (M + 4) * E * np.abs(DZ)).T @ np.abs(X) + least, "dw")
+    fits = np.abs(DB) < 60000
+    within(b.values(db)[fits], DB[fits], (u * np.abs(DB) + ((M + 8) * E * np.abs(DZ) + curve).sum(0) + least)[fits], "db")
+
+
+def check_range_of_each_row(b):
+    """rows, and columns, whose dz lie 2^40 apart"""
+    far = np.where(np.arange(23) % 3 == 0, 1e3, 1e-3)
+    check_range(b, "square", 23, 31, 17, 1.0, 1.0, 1e-4, 1e-4, rows=far)
+    check_range(b, "square", 23, 31, 17, 1.0, 1.0, 1e-4, 1e-4, cols=far[:17])
+    check_range(b, "square", 300, 31, 290, 1.0, 1.0, 1e-4, 1e-4, rows=np.where(np.arange(300) % 7, 1e-2, 1e2), cols=np.where(np.arange(290) % 5, 1.0, 10.0))
+
+
+def check_rows_that_are_not_finite(b, M=70, K=20, N=270):
+    """an infinity or NaN among dy or z is its own row's affair in dx, and its own column's in dw and db"""
+    rng = np.random.default_rng(11)
+    x, w, z, dy = (normal(rng, *s) for s in ((M, K), (N, K), (M, N), (M, N)))
+    clean = b.ctx.linear_grad(b.make(dy, "f16"), b.make(x, "f16"), b.make(w, "f16"), b.make(z, "f16"), activation="square", bias=True)
+    dy[3, 5], dy[69, 200], z[40, 269] = np.inf, np.nan, -np.inf
+    got = b.ctx.linear_grad(b.make(dy, "f16"), b.make(x, "f16"), b.make(w, "f16"), b.make(z, "f16"), activation="square", bias=True)
+    rows, cols = np.ones(M, bool), np.ones(N, bool)
+    rows[[3, 40, 69]] = cols[[5, 200, 269]] = False
+    for g, c, fine in zip(got, clean, (rows, cols, cols)):
+        g, c = b.values(g), b.values(c)
+        assert np.isfinite(g[fine]).all() and not np.isfinite(g[~fine]).any()
+        if fine is not rows:
+            assert np.array_equal(g[fine], c[fine])
