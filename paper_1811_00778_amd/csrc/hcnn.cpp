@@ -1978,6 +1978,7 @@ const char* hcnn_strerror(int code) {
 
 #ifdef HCNN_HOSTEMU
 void hcnn_emu_device(uint32_t units, size_t largest_allocation) { emu_units = units; emu_largest = largest_allocation; }
+size_t hcnn_emu_record(int on) { emu_recording = on != 0; return emu_frees; }
 #endif
 
 }  // extern "C"

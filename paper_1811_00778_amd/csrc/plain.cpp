@@ -60,6 +60,11 @@ int hcnn_plain_destroy(hcnn_plain* h) {
   if (!h) return HCNN_ERR_NULL;
   stream_sync(h->stream);
   if (h->work) dev_free(h->work);
+  while (hcnn_plain::Block* b = h->kept) {
+    h->kept = b->next;
+    dev_free(b->p);
+    delete b;
+  }
   if (h->d_bad) dev_free(h->d_bad);
   delete h;
   return HCNN_OK;

@@ -12,9 +12,12 @@
 using namespace hcnn;
 
 struct hcnn_plain {
+  struct Block { char* p; Block* next; };
   hcnn_stream_t stream = nullptr;
   char* work = nullptr;                       // grows to the largest call's need
   size_t work_bytes = 0;
+  bool recorded = false;                      // `work` is in the launches of a recorded graph
+  Block* kept = nullptr;                      // outgrown blocks that are
   unsigned long long* d_bad = nullptr;
   uint32_t compute_units = 256;
 };
@@ -39,20 +42,32 @@ struct Arena {
     return at;
   }
 };
+// A recorded graph reads and writes the block that its calls had: such a block is outgrown, but not freed before the handle.
 inline int reserve(hcnn_plain* h, size_t bytes) {
-  if (bytes <= h->work_bytes) return 0;
-  if (h->work) {
-    const int e = stream_sync(h->stream);
-    if (e) return e;
-    dev_free(h->work);
-    h->work = nullptr;
-    h->work_bytes = 0;
+  const bool recording = stream_recording(h->stream);
+  if (bytes > h->work_bytes) {
+    const bool keep = h->work && (h->recorded || recording);      // (while it is recorded, the stream cannot be waited for)
+    hcnn_plain::Block* old = keep ? new (std::nothrow) hcnn_plain::Block{h->work, h->kept} : nullptr;
+    if (keep && !old) return HCNN_ERR_ARG;
+    if (h->work && !keep) {
+      const int e = stream_sync(h->stream);
+      if (e) return e;
+      dev_free(h->work);
+      h->work = nullptr;
+      h->work_bytes = 0;
+    }
+    void* p = nullptr;
+    const int e = dev_malloc(&p, bytes);
+    if (e) {
+      delete old;
+      return e;
+    }
+    if (keep) h->kept = old;
+    h->work = static_cast<char*>(p);
+    h->work_bytes = bytes;
+    h->recorded = false;
   }
-  void* p = nullptr;
-  const int e = dev_malloc(&p, bytes);
-  if (e) return e;
-  h->work = static_cast<char*>(p);
-  h->work_bytes = bytes;
+  if (recording) h->recorded = true;
   return 0;
 }
 template <class V> V* at(hcnn_plain* h, size_t offset) { return reinterpret_cast<V*>(h->work + offset); }

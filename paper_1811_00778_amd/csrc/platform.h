@@ -200,11 +200,15 @@ template <class K> struct LoopPhases<K, std::void_t<decltype(K::kLoopPhases)>> {
 // What a test may set (hcnn_emu_device): compute units of the contexts created from then on, the largest allocation that is granted
 static uint32_t emu_units = 1;           // small rounds: the checker's little batches reach every batch-splitting path
 static size_t emu_largest = ~(size_t)0;
+// ... (hcnn_emu_record): whether streams are being recorded; and the frees since the checker was loaded
+static bool emu_recording = false;
+static size_t emu_frees = 0;
 inline int dev_malloc(void** p, size_t bytes) {
   *p = bytes <= emu_largest ? std::malloc(bytes ? bytes : 1) : nullptr;
   return *p ? 0 : 2;
 }
-inline int dev_free(void* p) { std::free(p); return 0; }
+inline int dev_free(void* p) { std::free(p); ++emu_frees; return 0; }
+inline bool stream_recording(hcnn_stream_t) { return emu_recording; }
 inline int dev_memset(void* p, int v, size_t bytes, hcnn_stream_t) { std::memset(p, v, bytes); return 0; }
 inline int copy_h2d(void* d, const void* h, size_t bytes, hcnn_stream_t) { std::memcpy(d, h, bytes); return 0; }
 inline int copy_d2h(void* h, const void* d, size_t bytes, hcnn_stream_t) { std::memcpy(h, d, bytes); return 0; }
@@ -311,6 +315,15 @@ inline int copy_d2d(void* d, const void* s_, size_t bytes, hcnn_stream_t s) {
   return (int)hipMemcpyAsync(d, s_, bytes, hipMemcpyDeviceToDevice, s);
 }
 inline int stream_sync(hcnn_stream_t s) { return (int)hipStreamSynchronize(s); }
+// Is what the stream is given being recorded into a graph?
+inline bool stream_recording(hcnn_stream_t s) {
+  hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+  if (hipStreamIsCapturing(s, &status) != hipSuccess) {     // (the default stream, while another one is recorded)
+    (void)hipGetLastError();
+    return false;
+  }
+  return status != hipStreamCaptureStatusNone;
+}
 typedef hipEvent_t hcnn_event_t;
 inline int event_create(hcnn_event_t* e) { return (int)hipEventCreate(e); }
 inline int event_destroy(hcnn_event_t e) { return (int)hipEventDestroy(e); }

@@ -1,7 +1,11 @@
 """The training operators on the CPU checker, at the edges of their numbers, memory and arguments."""
+import ctypes
+
+import numpy as np
 import pytest
 
 import emu
+import plain_cases as pc
 import plain_edge_cases as pe
 from test_plain_ops import Backend
 
@@ -28,3 +32,35 @@ def test_range_of_each_row_and_column(b):
 
 def test_rows_that_are_not_finite(b):
     pe.check_rows_that_are_not_finite(b)
+
+
+def _recording(on):
+    """Whether streams count as being recorded from now on; the frees of the checker's device memory so far."""
+    f = emu.lib().hcnn_emu_record
+    f.argtypes, f.restype = [ctypes.c_int], ctypes.c_size_t
+    return f(int(on))
+
+
+def test_work_memory_that_a_recording_has_seen_stays():
+    """a recorded graph reads the work memory of its calls: a later call that needs more must not free it before the handle goes"""
+    b = Backend()
+
+    def loss(rows):
+        x, w, t = pc.loss_inputs(b, "f32", rows, 20, 40)
+        return [v.copy() for v in b.ctx.cross_entropy_grad(x, w, b.ints(t, np.int64))]
+
+    small = loss(30)
+    _recording(True)
+    for u, v in zip(small, loss(30)):
+        assert np.array_equal(u, v)
+    frees, held = _recording(False), b.ctx.scratch_bytes()
+    loss(300)
+    assert b.ctx.scratch_bytes() > held
+    assert _recording(False) == frees                    # the recorded block is still there
+    loss(900)
+    assert _recording(False) == frees + 1                # the one between, which no recording has seen, is not
+    _recording(True)
+    loss(1500)                                           # grows while it is recorded: its old block may be in use
+    assert _recording(False) == frees + 1
+    b.ctx.close()
+    assert _recording(False) == frees + 5                # three blocks, the one in use, the counter
