@@ -389,7 +389,8 @@ int hcnn_cross_entropy_grad(hcnn_plain* h, int dtype, size_t rows, size_t n_in, 
 
 /* norm[0] = sqrt of the sum of squares of all numbers of all tensors (summed in 64 bits), and every tensor times
  * min(1, max_norm / (norm + eps)).  The arrays are host arrays of n_tensors device pointers, counts and types (one type each);
- * outs_host NULL: in place, else where each result goes (a tensor's own place allowed).  A norm that is not finite: the factor is 0
+ * outs_host NULL: in place, else where each result goes (a tensor's own place allowed).  A place that is written must not overlap another
+ * tensor or place of the list (in place too: a tensor named twice would be scaled once or twice).  A norm that is not finite: the factor is 0
  * (infinity) or not a number, as the formula gives it. */
 int hcnn_clip_grad_norm(hcnn_plain* h, size_t n_tensors, const void* const* grads_host, const size_t* counts_host,
                         const int* dtypes_host, void* const* outs_host, double max_norm, double eps, float* norm_dev);

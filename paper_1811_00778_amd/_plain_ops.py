@@ -163,7 +163,8 @@ class PlainOpsMixin:
     # ---- step
     def clip_grad_norm(self, grads, max_norm, out=None, eps=1e-6):
         """Euclidean norm over all numbers of the list `grads` (contiguous arrays of any shapes, types mixed), as one 32-bit float; every
-        array is scaled by min(1, max_norm / (norm + eps)), in place or into the arrays of `out` (hcnn_clip_grad_norm)."""
+        array is scaled by min(1, max_norm / (norm + eps)), in place or into the arrays of `out` (hcnn_clip_grad_norm).  What is written
+        must not overlap anything else of the list: a tensor that shares its numbers with another is named once."""
         grads = list(grads)
         if not max_norm >= 0 or not eps >= 0:
             raise ValueError("max_norm and eps must not be negative")
@@ -172,15 +173,14 @@ class PlainOpsMixin:
         ptrs = (C.c_void_p * n)(*[f[0] for f in flat])
         counts = (C.c_size_t * n)(*[f[1] for f in flat])
         types = (C.c_int * n)(*[f[2] for f in flat])
-        outs = None
+        outs, to = None, flat
         if out is not None:
             out = list(out)
             to = [self._flat(g, "out") for g in out]
             if [t[1:] for t in to] != [f[1:] for f in flat]:
                 raise ValueError("out must match grads in number, sizes and types")
-            if any(t[0] != f[0] for t, f in zip(to, flat)):
-                self._clip_apart(flat, to)
             outs = (C.c_void_p * n)(*[t[0] for t in to])
+        self._clip_apart(flat, to)
         norm = self._new((), None)
         self._pre_call()
         self.raw.call("hcnn_clip_grad_norm", n, ptrs, counts, types, outs, float(max_norm), float(eps), self._address(norm))
@@ -200,7 +200,7 @@ class PlainOpsMixin:
         end = written = 0                      # the furthest byte so far, of all and of what is written
         for first, last, writes in spans:
             if first < (end if writes else written):
-                raise ValueError("out must not overlap grads or itself")
+                raise ValueError("a tensor that is written must not overlap another one of the list")
             end = max(end, last)
             if writes:
                 written = max(written, last)

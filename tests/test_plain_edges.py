@@ -64,3 +64,17 @@ def test_work_memory_that_a_recording_has_seen_stays():
     assert _recording(False) == frees + 1
     b.ctx.close()
     assert _recording(False) == frees + 5                # three blocks, the one in use, the counter
+
+
+def test_clipping_refuses_numbers_named_twice(b):
+    """a number in two tensors of the list would be scaled by two workgroups, once or twice"""
+    g = b.make(np.linspace(-3, 3, 200), "f32")
+    before = g.copy()
+    for grads, out in (([g, g], None), ([g, g[:-1]], None), ([g[:100], g[99:]], None), ([g, g], [g, g]), ([g[:100], g[50:150]], [g[:100], g[50:150]]),
+                       ([g[10:20], g], [g[10:20], g])):
+        with pytest.raises(ValueError):
+            b.ctx.clip_grad_norm(grads, 1.0, out=out)
+        assert np.array_equal(g, before)
+    norm = b.ctx.clip_grad_norm([g[:100], g[100:], g[:0]], 1.0)          # side by side: no overlap
+    pc.within(b.values(norm), np.linalg.norm(b.values(before)), 1e-6 * np.linalg.norm(b.values(before)), "norm")
+    pc.within(b.values(b.ctx.clip_grad_norm([g, g], 1.0, out=[b.make(np.zeros(200), "f32") for _ in range(2)])), 2 ** 0.5, 1e-5, "norm of a tensor read twice")
