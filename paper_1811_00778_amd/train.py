@@ -121,16 +121,19 @@ class PlainNetwork:
         return loss, grads
 
     def train_step(self, x, labels, state, lr=0.05, momentum=0.9, max_norm=1.0, scale=1.0):
-        """One clipped step of gradient descent with momentum (state: a dict that the caller keeps); returns (loss, norm)."""
+        """One clipped step of gradient descent with momentum (state: a dict that the caller keeps); returns (loss, norm).  Where the norm is
+        not finite (binary16 gradients that overflow under their `scale`), weights and state stay as they are: the caller lowers the scale."""
         loss, grads = self.loss_and_gradients(x, labels, scale)
         mine = [(w, g) for w, g in zip(self.weights, grads) if g is not None]
         norm = self.ctx.clip_grad_norm([g for _, g in mine], max_norm * scale)
         if "moments" not in state:
             state["master"] = [w.float() for w, _ in mine]
             state["moments"] = [torch.zeros_like(m) for m in state["master"]]
+        finite = torch.isfinite(norm)                             # (decided on the device: no wait for the step)
         for (w, g), m, v in zip(mine, state["master"], state["moments"]):
-            v.mul_(momentum).add_(g.float(), alpha=1.0 / scale)
-            m.sub_(v, alpha=lr)
+            moved = (v * momentum).add_(g.float(), alpha=1.0 / scale)
+            m.copy_(torch.where(finite, m.sub(moved, alpha=lr), m))
+            v.copy_(torch.where(finite, moved, v))
             w.copy_(m)
         return loss, norm / scale
 
@@ -228,13 +231,14 @@ def _main(argv=None):
     ctx = binding.PlainContext()
     dtype = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[args.dtype]
     net = PlainNetwork(spec, in_shape, ctx, dtype)
-    protos, state = None, {}
+    protos, state, scale = None, {}, 1024.0 if args.dtype == "f16" else 1.0
     t0 = time.perf_counter()
     for step in range(args.steps):
         images, labels, protos = made_up_images(args.batch, in_shape, classes, rng, levels, protos)
         x = torch.from_numpy(images).to(ctx.device, dtype) / (levels - 1)
-        loss, norm = net.train_step(x, torch.from_numpy(labels).to(ctx.device), state, lr=args.lr,
-                                    scale=1024.0 if args.dtype == "f16" else 1.0)
+        loss, norm = net.train_step(x, torch.from_numpy(labels).to(ctx.device), state, lr=args.lr, scale=scale)
+        if args.dtype == "f16" and not np.isfinite(float(norm)):
+            scale /= 2
         if step % 25 == 0 or step == args.steps - 1:
             print("step %4d  loss %.4f  gradient norm %.3f" % (step, float(loss), float(norm)), flush=True)
     print("%d steps of %d images in %.2f s" % (args.steps, args.batch, time.perf_counter() - t0))
