@@ -14,6 +14,7 @@ CEILINGS = ["copy_GBps", "read_GBps", "write_GBps", "mul_lo_u32_Tops", "mul_hi_u
             "mad_i64_i32_Tops", "add_u32_Tops"]
 MAX_LIMBS, MAX_FILTERS = 32, 16
 F32, F16, BF16 = 0, 1, 2
+SIZES = {F32: 4, F16: 2, BF16: 2}
 ACTIVATIONS = {"none": 0, "square": 1, "relu": 2, "gelu": 3, "silu": 4}
 
 # name -> argtypes; every entry point returns int except hcnn_strerror

@@ -50,8 +50,22 @@ class PlainOpsMixin:
             if y is None:
                 continue
             b0, b1 = self._span(y)
-            if a0 < b1 and b0 < a1:
+            if a0 < b1 and b0 < a1 and not (y.ndim == 2 and self._other_columns(x, y)):
                 raise ValueError("%s must not overlap an input" % what)
+
+    def _other_columns(self, x, y):
+        """Do the rows of two matrices of one type, whose memory interleaves, lie beside each other: other columns of one array?"""
+        xp, x_rows, x_cols, x_pitch, dtype = self._matrix(x, "x")
+        yp, y_rows, y_cols, y_pitch, _ = self._matrix(y, "y")
+        if y_rows == 1:
+            y_pitch = x_pitch
+        if x_rows == 1:
+            x_pitch = y_pitch
+        if x_pitch != y_pitch or x_pitch <= 0:
+            return False
+        size = _capi.SIZES[dtype]
+        behind = (yp - xp) % (x_pitch * size)                  # of a row of y, from the row of x in front of it
+        return behind >= x_cols * size and behind + y_cols * size <= x_pitch * size
 
     # ---- layers
     def linear(self, x, w, bias=None, residual=None, activation="none", keep=False, out=None):
@@ -188,11 +202,10 @@ class PlainOpsMixin:
 
     def _clip_apart(self, flat, to):
         """No result may overlap a gradient other than its own, which it may replace, nor another result."""
-        size = {_capi.F32: 4, _capi.F16: 2, _capi.BF16: 2}
         spans = []                             # (first byte, one past the last, written)
         for f, t in zip(flat, to):
             if f[1]:
-                n = f[1] * size[f[2]]
+                n = f[1] * _capi.SIZES[f[2]]
                 spans.append((f[0], f[0] + n, f[0] == t[0]))
                 if f[0] != t[0]:
                     spans.append((t[0], t[0] + n, True))

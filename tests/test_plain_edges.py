@@ -78,3 +78,27 @@ def test_clipping_refuses_numbers_named_twice(b):
     norm = b.ctx.clip_grad_norm([g[:100], g[100:], g[:0]], 1.0)          # side by side: no overlap
     pc.within(b.values(norm), np.linalg.norm(b.values(before)), 1e-6 * np.linalg.norm(b.values(before)), "norm")
     pc.within(b.values(b.ctx.clip_grad_norm([g, g], 1.0, out=[b.make(np.zeros(200), "f32") for _ in range(2)])), 2 ** 0.5, 1e-5, "norm of a tensor read twice")
+
+
+def test_output_in_other_columns_of_the_inputs_array(b):
+    """columns of one array: what a layer writes beside what it reads is no overlap, what reaches into it is"""
+    rng = np.random.default_rng(12)
+    w = b.make(pc.normal(rng, 5, 6), "f32")
+    big = b.make(pc.normal(rng, 11, 24), "f32")
+    x = big[:, 4:10]
+    want = b.ctx.linear(x.copy(), w)
+    for at in (10, 19):
+        b.ctx.linear(x, w, out=big[:, at:at + 5])
+        assert np.array_equal(big[:, at:at + 5], want)
+    kept = big.copy()
+    for at in (0, 5, 9):
+        with pytest.raises(ValueError):
+            b.ctx.linear(x, w, out=big[:, at:at + 5])
+    with pytest.raises(ValueError):                             # rows of another pitch
+        b.ctx.linear(x, w, out=np.lib.stride_tricks.as_strided(big[:, 10:], (11, 5), (23 * 4, 4)))
+    assert np.array_equal(big, kept)
+    # the residual's array, in other columns too
+    r = big[:, 10:15]
+    want = b.ctx.linear(x.copy(), w, residual=r.copy())
+    b.ctx.linear(x, w, residual=r, out=big[:, 15:20])
+    assert np.array_equal(big[:, 15:20], want)
