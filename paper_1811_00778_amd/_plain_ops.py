@@ -37,12 +37,13 @@ class PlainOpsMixin:
         return got
 
     def _output(self, x, shape, dtype, what, *inputs):
-        """An output that the caller gave: shape, type, rows that do not overlap, no memory shared with the inputs."""
+        """An output that the caller gave: shape, type, rows that do not overlap, no memory shared with the inputs.  (A single row has no
+        next one: whatever its stride, the library is told its length.)"""
         got = self._like(x, shape, dtype, what)
         if got[1] > 1 and got[3] < got[2]:
             raise ValueError("the rows of %s must not overlap" % what)
         self._apart(x, what, *inputs)
-        return got
+        return got if got[1] > 1 else (*got[:3], max(got[2:4]), got[4])
 
     def _apart(self, x, what, *inputs):
         a0, a1 = self._span(x)
@@ -90,7 +91,7 @@ class PlainOpsMixin:
         else:
             y = out
             yp, _, _, ldy, _ = self._output(y, (rows, n_out), dtype, "out", x, w, bias)
-            if residual is not None and not (yp == rp and ldy == ldr):
+            if residual is not None and not (yp == rp and (ldy == ldr or rows == 1)):
                 self._apart(y, "out", residual)
         zp, z = None, None
         if keep:

@@ -102,3 +102,16 @@ def test_output_in_other_columns_of_the_inputs_array(b):
     want = b.ctx.linear(x.copy(), w, residual=r.copy())
     b.ctx.linear(x, w, residual=r, out=big[:, 15:20])
     assert np.array_equal(big[:, 15:20], want)
+
+
+def test_output_of_one_row_with_any_stride(b):
+    """a single row has no next one: its stride says nothing"""
+    rng = np.random.default_rng(13)
+    x, w, r = (b.make(pc.normal(rng, *s), "f32") for s in ((1, 9), (6, 9), (1, 6)))
+    want = b.ctx.linear(x, w, residual=r)
+    for stride in (0, 4, 5 * 4, 400):
+        out = np.lib.stride_tricks.as_strided(b.make(np.zeros(6), "f32"), (1, 6), (stride, 4))
+        assert b.ctx.linear(x, w, residual=r, out=out) is out and np.array_equal(out, want)
+    place = np.lib.stride_tricks.as_strided(r, (1, 6), (4, 4))           # the residual's own memory
+    b.ctx.linear(x, w, residual=r, out=place)
+    assert np.array_equal(r, want)
