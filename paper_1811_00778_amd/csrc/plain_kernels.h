@@ -489,7 +489,11 @@ struct GemmOperand {
 #if defined(__HIP_DEVICE_COMPILE__)
     const uint32_t at = wave_uniform((uint32_t)(uintptr_t)lds);             // (the low half of an LDS pointer is its offset)
     // (as an instruction of its own: of the builtin the compiler only knows that it writes LDS, and has every later LDS read wait for it)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(base) : "memory");
+    // (m0: what the compiler has put there for an access of its own is gone; its warning that m0 is reserved is about allocating it)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(base) : "memory", "m0");
+#pragma clang diagnostic pop
 #else
     __builtin_memcpy(lds + lane * 16, reinterpret_cast<const char*>(base) + off, 16);
 #endif

@@ -1,5 +1,8 @@
 """The training operators on the CPU checker, at the edges of their numbers, memory and arguments."""
 import ctypes
+import glob
+import os
+import re
 
 import numpy as np
 import pytest
@@ -7,6 +10,7 @@ import pytest
 import emu
 import plain_cases as pc
 import plain_edge_cases as pe
+from paper_1811_00778_amd import _capi
 from test_plain_ops import Backend
 
 
@@ -115,3 +119,16 @@ def test_output_of_one_row_with_any_stride(b):
     place = np.lib.stride_tricks.as_strided(r, (1, 6), (4, 4))           # the residual's own memory
     b.ctx.linear(x, w, residual=r, out=place)
     assert np.array_equal(r, want)
+
+
+def test_assembly_names_the_registers_it_writes():
+    """every asm statement of the kernels that sets m0 or vcc names it as clobbered"""
+    found = 0
+    for path in glob.glob(os.path.join(os.path.dirname(_capi.__file__), "csrc", "*")):
+        with open(path) as f:
+            for statement in re.findall(r"\basm\b[^;]*;", f.read()):
+                for register in ("m0", "vcc"):
+                    if re.search(r"\b[sv]_\w+ (?:%\d, )?" + register + r"\b", statement):
+                        found += 1
+                        assert '"%s"' % register in statement, (os.path.basename(path), statement)
+    assert found >= 3
