@@ -195,4 +195,24 @@ int hcnn_clip_grad_norm(hcnn_plain* h, size_t n_tensors, const void* const* grad
   return e;
 }
 
+#ifdef HCNN_HOSTEMU
+// What the checker's tests force and ask (see platform.h)
+void hcnn_emu_shape(int tile, uint32_t parts, int copies) {
+  emu_tile = tile;
+  emu_parts = parts;
+  emu_copies = copies != 0;
+  emu_taken = emu_copied = 0;
+}
+void hcnn_emu_taken(uint64_t* taken, uint64_t* copied) {
+  *taken = emu_taken;
+  *copied = emu_copied;
+}
+// Tile (low byte) and parts of k that a product of these sizes takes on the handle's device; does an unaligned operand of a product get copied?
+uint32_t hcnn_emu_choice(hcnn_plain* h, int dtype, size_t M, size_t N, size_t K, int may_split, int direct) {
+  const Shape s = PLAIN_BY_TYPE(dtype, choose, h, M, N, K, may_split != 0, direct != 0);
+  return (uint32_t)s.tile | s.splits << 8;
+}
+int hcnn_emu_copies(size_t rows, size_t cols, double work) { return copy_pays(Input{nullptr, cols, rows, cols}, work); }
+#endif
+
 }  // extern "C"

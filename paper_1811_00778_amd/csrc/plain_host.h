@@ -87,6 +87,10 @@ Shape choose(const hcnn_plain* h, size_t M, size_t N, size_t K, bool may_split, 
   constexpr double kHeld[] = {1, 2, 4, 4, 4}, kEnds[] = {10, 6, 4, 4, 4}, kAlone = 0.7;
   const double units = h->compute_units;
   const size_t stages = std::max<size_t>(1, blocks(K, GemmNum<T>::kStage));
+#ifdef HCNN_HOSTEMU
+  if (emu_tile >= 0 && (emu_tile != kTile256 || (!wide && direct)))
+    return Shape{emu_tile, kTileRows[emu_tile], kTileCols[emu_tile], may_split ? (uint32_t)std::max<size_t>(1, std::min<size_t>(emu_parts, stages / 2)) : 1, direct};
+#endif
   Shape best{kTile64, 64, 64, 1, direct};
   double least = 1e300;
   for (int t = kTile256; t <= kFlat; ++t) {
@@ -129,10 +133,16 @@ bool direct_input(const Input& x) {
 // 2001 54.6 / 50.0, 2501 70.0 / 70.8, 4001 157 / 225; 8192 x 517 x 1000 34.5 / 24.4, 256 x 4001 x 4001 43.5 / 35.7.  32-bit
 // products are bound by the matrix unit either way.
 constexpr double kPackWork = 0.6e-15, kPackByte = 2e-13, kPackLaunch = 4e-6;       // seconds
+inline bool copy_pays(const Input& x, double work) {
+#ifdef HCNN_HOSTEMU
+  if (emu_copies) return true;
+#endif
+  return work * kPackWork >= kPackLaunch + 4.0 * (double)x.rows * (double)x.cols * kPackByte;
+}
 template <class T>
 void plan_pack(Input& x, Arena& a, double work) {
   if (sizeof(T) != 2 || direct_input<T>(x) || x.rows == 0 || x.cols == 0) return;
-  if (work * kPackWork < kPackLaunch + 4.0 * (double)x.rows * (double)x.cols * kPackByte) return;
+  if (!copy_pays(x, work)) return;
   x.packed = true;
   x.ld = up(x.cols, GemmNum<T>::kStage);                // whole stages along the row, zeros at its end
   x.offset = a.take(x.rows * x.ld * sizeof(T));
@@ -140,6 +150,9 @@ void plan_pack(Input& x, Arena& a, double work) {
 template <class T>
 int pack(hcnn_plain* h, Input& x, const void* from, size_t ld_from) {
   if (!x.packed) return 0;
+#ifdef HCNN_HOSTEMU
+  ++emu_copied;
+#endif
   const PackArgs p{from, ld_from, at<void>(h, x.offset), x.ld, (uint32_t)x.rows, (uint32_t)x.cols, x.rows * (x.ld / 8)};
   x.p = p.to;
   return launch<PackRows>(h->stream, blocks(p.pieces, PackRows::kThreads), 0, p);
@@ -148,6 +161,9 @@ template <class T, int LA, int LB, int EPI>
 int gemm(hcnn_plain* h, const GemmArgs& a, const Shape& s) {
   const size_t grid = blocks(a.M, s.bm) * blocks(a.N, s.bn) * s.splits;
   if (grid > kMaxSize) return HCNN_ERR_ARG;
+#ifdef HCNN_HOSTEMU
+  emu_taken |= (uint64_t)1 << (EPI * 16 + s.tile * 2 + s.direct);
+#endif
 #define PLAIN_TILE(BM, BN, WM, WN) \
   return s.direct ? start<Gemm<T, LA, LB, BM, BN, WM, WN, EPI, true>>(h, a, grid) : start<Gemm<T, LA, LB, BM, BN, WM, WN, EPI, false>>(h, a, grid)
   switch (s.tile) {

@@ -203,6 +203,12 @@ static size_t emu_largest = ~(size_t)0;
 // ... (hcnn_emu_record): whether streams are being recorded; and the frees since the checker was loaded
 static bool emu_recording = false;
 static size_t emu_frees = 0;
+// ... (hcnn_emu_shape): a tile of plain_host.h's and a number of parts of k for its products in place of the estimate's (-1: none), copies of every
+// unaligned operand; and what was launched since: a bit for each ending, tile and way to LDS, the copies
+static int emu_tile = -1;
+static uint32_t emu_parts = 1;
+static bool emu_copies = false;
+static uint64_t emu_taken = 0, emu_copied = 0;
 inline int dev_malloc(void** p, size_t bytes) {
   *p = bytes <= emu_largest ? std::malloc(bytes ? bytes : 1) : nullptr;
   return *p ? 0 : 2;

@@ -106,3 +106,10 @@ def check_rows_that_are_not_finite(b, M=70, K=20, N=270):
         assert np.isfinite(g[fine]).all() and not np.isfinite(g[~fine]).any()
         if fine is not rows:
             assert np.array_equal(g[fine], c[fine])
+
+
+# (dtype, rows, n_in, n_out) for the device: products that take the largest tile in all three of a layer's products, every edge ragged
+WIDE = [("bf16", 4091, 4088, 4072), ("f16", 4005, 4080, 4064)]
+# ... and ones whose odd rows are worth copying
+COPIED = [("bf16", 2501, 2503, 2507), ("f16", 2503, 2601, 2705)]
+COPIED_LOSS = [("bf16", 2051, 1021, 7001), ("f16", 1021, 517, 30011)]

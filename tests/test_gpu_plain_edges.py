@@ -76,3 +76,92 @@ def test_recorded_step_after_larger_calls():
     assert b.ctx.scratch_bytes() > held
     del graph
     b.ctx.close()
+
+
+def _within(got, want, bound, what):
+    """|got - want| <= bound, number by number, on the device"""
+    off = (got.double() - want).abs() - bound
+    assert bool(torch.isfinite(got).all()) and float(off.max()) <= 0, (what, float(off.max()))
+
+
+def _act(z, name):
+    """(value, slope) in 64 bits"""
+    if name == "none":
+        return z, torch.ones_like(z)
+    if name == "square":
+        return z * z, 2 * z
+    cdf = torch.special.ndtr(z)
+    return z * cdf, cdf + z * torch.exp(-z * z / 2) / (2 * np.pi) ** 0.5
+
+
+def _wide_linear(b, dtype, M, K, N, strides):
+    """linear with everything and linear_grad, at sizes whose 64-bit products belong on the device; plain_cases' bounds"""
+    rng = np.random.default_rng([M, K, N])
+    u, least, E, FN = pc.U[dtype], pc.LEAST[dtype], pc.E, pc.FN
+    x, w = b.make(pc.normal(rng, M, K), dtype, strides), b.make(pc.normal(rng, N, K, std=K ** -0.5), dtype, strides)
+    bias, r = b.make(pc.normal(rng, N), dtype), b.make(pc.normal(rng, M, N), dtype, strides)
+    X, W, B, R = (v.double() for v in (x, w, bias, r))
+    y, z = b.ctx.linear(x, w, bias, r, activation="gelu", keep=True)
+    mag = X.abs() @ W.abs().t() + B.abs()
+    Z = X @ W.t() + B
+    dz = (K + 4) * E * mag
+    _within(z, Z, u * Z.abs() + dz + least, "z")
+    Y = _act(Z, "gelu")[0]
+    _within(y, Y + R, u * (Y + R).abs() + 1.2 * dz + FN * (Z.abs() + 1e-30) * (2 + Z.abs()) + 2 * E * R.abs() + least, "y")
+    assert torch.equal(b.ctx.linear(x, w, bias, r, activation="gelu"), y)
+    for name in ("none", "square"):
+        dy = b.make(pc.normal(rng, M, N), dtype, strides)
+        dx, dw, db = b.ctx.linear_grad(dy, x, w, z, activation=name, bias=True)
+        DY = dy.double()
+        DZ = DY * _act(z.double(), name)[1]
+        room = 0.0 if name == "none" else (u + 4 * E)
+        low = 0.0 if name == "none" else least + (2.0 ** -39 * float(DZ.abs().max()) if dtype == "f16" else 0.0)
+        err = room * DZ.abs() + low
+        _within(dx, DZ @ W, u * (DZ @ W).abs() + (err + (N + 4) * E * DZ.abs()) @ W.abs() + least, "dx " + name)
+        _within(dw, DZ.t() @ X, u * (DZ.t() @ X).abs() + (err + (M + 4) * E * DZ.abs()).t() @ X.abs() + least, "dw " + name)
+        _within(db, DZ.sum(0), u * DZ.sum(0).abs() + ((M + 8) * E * DZ.abs()).sum(0) + least, "db " + name)
+
+
+@pytest.mark.parametrize("case", pe.WIDE, ids=str)
+def test_largest_tiles_with_ragged_edges(b, case):
+    say("largest tiles", case)
+    _wide_linear(b, *case, strides=None)
+
+
+@pytest.mark.parametrize("case", pe.COPIED, ids=str)
+@pytest.mark.parametrize("strides", [None, (3, 1)])
+def test_copied_operands(b, case, strides):
+    """odd rows, with NaN between them"""
+    say("copied operands", case, strides)
+    _wide_linear(b, *case, strides=strides)
+
+
+@pytest.mark.parametrize("case", pe.COPIED_LOSS, ids=str)
+@pytest.mark.parametrize("masked", [0.0, 0.3])
+def test_copied_operands_of_the_loss(b, case, masked):
+    dtype, M, K, V = case
+    say("loss of copied operands", case, masked)
+    u, least, E, FN = pc.U[dtype], pc.LEAST[dtype], pc.E, pc.FN
+    x, w, t = pc.loss_inputs(b, dtype, M, K, V, masked, strides=(3, 1), junk=True)
+    scale = 1024.0 if dtype == "f16" else 1.0
+    loss, dx, dw = b.ctx.cross_entropy_grad(x, w, b.ints(t, np.int64), scale=scale)
+    keep = torch.from_numpy(np.nonzero(t != pc.IGNORE)[0]).cuda()
+    n = len(keep)
+    X, W = x.double()[keep], w.double()
+    L = X @ W.t()
+    lse = torch.logsumexp(L, 1, keepdim=True)
+    at = (torch.arange(n, device="cuda"), torch.from_numpy(t).cuda()[keep])
+    rows = lse[:, 0] - L[at]
+    row_err = 2 * (K + 4) * E * (X.abs() @ W.abs().t()).amax(1) + 8 * E * (L.abs().amax(1) + np.log(V) + 1) + FN
+    assert abs(float(loss) - float(rows.mean())) <= float(row_err.mean()) + E * abs(float(rows.mean()))
+    e = torch.exp(L - lse)
+    q = (scale / n) * (e * (row_err[:, None] * 2 + FN * (1 + (L - lse).abs())) + least * (2.0 ** -15 if dtype == "f16" else 1.0))
+    p = e.clone()
+    p[at] -= 1
+    p *= scale / n
+    q += u * p.abs()
+    DX, DW = p @ W, p.t() @ X
+    _within(dx[keep], DX, u * DX.abs() + (q + (V + 8) * E * p.abs()) @ W.abs() + least, "dx")
+    _within(dw, DW, u * DW.abs() + (q + (M + 8) * E * p.abs()).t() @ X.abs() + least, "dw")
+    hidden = torch.from_numpy(np.nonzero(t == pc.IGNORE)[0]).cuda()
+    assert not hidden.numel() or float(dx[hidden].abs().max()) == 0
