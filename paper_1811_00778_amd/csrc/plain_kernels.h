@@ -450,7 +450,6 @@ struct GemmOperand {
   }
   // ---- memory to LDS without registers: whole stages of operands whose stored rows all start on 16 bytes.  The LDS side of such a load
   // is fixed (a wave writes 64 x 16 bytes in a row), so that the order of the pieces within a stored row is made on the memory side.
-  static constexpr bool kEvenWaves = kPieces % 64 == 0;
   HCNN_HD static uint32_t numbers(uint32_t c) {                                 // of a row at LDS piece c, from the stage's first number
     const uint32_t line = c / kRowPieces, pc = c % kRowPieces;
     if constexpr (LAYOUT == kAlongK) return (pc ^ turn(line)) * kPer16;
