@@ -203,6 +203,7 @@ void hcnn_emu_shape(int tile, uint32_t parts, int copies) {
   emu_copies = copies != 0;
   emu_taken = emu_copied = 0;
 }
+void hcnn_emu_threads(uint64_t most) { emu_threads = most; }
 void hcnn_emu_taken(uint64_t* taken, uint64_t* copied) {
   *taken = emu_taken;
   *copied = emu_copied;

@@ -153,9 +153,10 @@ int pack(hcnn_plain* h, Input& x, const void* from, size_t ld_from) {
 #ifdef HCNN_HOSTEMU
   ++emu_copied;
 #endif
-  const PackArgs p{from, ld_from, at<void>(h, x.offset), x.ld, (uint32_t)x.rows, (uint32_t)x.cols, x.rows * (x.ld / 8)};
+  const size_t pieces = x.rows * (x.ld / 8), grid = std::min(blocks(pieces, PackRows::kThreads), most_workgroups(PackRows::kThreads));
+  const PackArgs p{from, ld_from, at<void>(h, x.offset), x.ld, (uint32_t)x.rows, (uint32_t)x.cols, pieces, grid * PackRows::kThreads};
   x.p = p.to;
-  return launch<PackRows>(h->stream, blocks(p.pieces, PackRows::kThreads), 0, p);
+  return launch<PackRows>(h->stream, grid, 0, p);
 }
 template <class T, int LA, int LB, int EPI>
 int gemm(hcnn_plain* h, const GemmArgs& a, const Shape& s) {
@@ -394,9 +395,10 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
   KeepRowsArgs kr{c.targets, c.target_bytes == 8, c.ignore, (uint32_t)M, (uint32_t)V, rows, target, count, h->d_bad, c.loss, alpha, c.scale / delta_scale<T>()};
   if ((e = launch<KeepRows>(h->stream, 1, KeepRows::kLdsBytes, kr))) return e;
   if (M) {
+    const size_t grid = std::min(blocks(M, 4), most_workgroups(SortRows::kThreads));
     const SortRowsArgs sr{kr, K ? c.dx : nullptr, c.ld_dx * sizeof(T), K * sizeof(T), c.row_loss, c.row_lse,
-                          c.x, c.ldx * sizeof(T), at<void>(h, ikept.offset), ikept.ld * sizeof(T), ix.packed};
-    if ((e = launch<SortRows>(h->stream, blocks(M, 4), 0, sr))) return e;
+                          c.x, c.ldx * sizeof(T), at<void>(h, ikept.offset), ikept.ld * sizeof(T), ix.packed, (uint32_t)grid * 4};
+    if ((e = launch<SortRows>(h->stream, grid, 0, sr))) return e;
   }
   if (ix.packed) ix.p = at<void>(h, ikept.offset);
   GemmArgs g = operands(ix, iw);

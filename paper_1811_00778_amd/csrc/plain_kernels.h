@@ -931,6 +931,7 @@ struct PackArgs {
   size_t ld_to;               // a multiple of 8
   uint32_t rows, cols;
   size_t pieces;              // rows * ld_to / 8
+  size_t threads;             // of the launch
 };
 struct PackRows {
   static constexpr int kThreads = 256;
@@ -939,14 +940,15 @@ struct PackRows {
   template <int PH>
   HCNN_HD static void phase(const PackArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
     typedef GemmOperand<Half, kAlongK, 16, 64> Op;
-    const size_t at = (size_t)bid * kThreads + tid;
-    if (at >= a.pieces) return;
-    const size_t each = a.ld_to / 8, row = at / each;
-    const uint32_t c = (uint32_t)(at - row * each) * 8;
-    const uint32_t left = c < a.cols ? a.cols - c : 0;
-    U4 v{};
-    if (left) v = Op::first(Op::piece(static_cast<const Half*>(a.from), row * a.ld_from + c, (a.rows - 1) * a.ld_from + a.cols), left);
-    *reinterpret_cast<U4*>(static_cast<Half*>(a.to) + row * a.ld_to + c) = v;
+    const size_t each = a.ld_to / 8;
+    for (size_t at = (size_t)bid * kThreads + tid; at < a.pieces; at += a.threads) {
+      const size_t row = at / each;
+      const uint32_t c = (uint32_t)(at - row * each) * 8;
+      const uint32_t left = c < a.cols ? a.cols - c : 0;
+      U4 v{};
+      if (left) v = Op::first(Op::piece(static_cast<const Half*>(a.from), row * a.ld_from + c, (a.rows - 1) * a.ld_from + a.cols), left);
+      *reinterpret_cast<U4*>(static_cast<Half*>(a.to) + row * a.ld_to + c) = v;
+    }
   }
 };
 
@@ -1515,6 +1517,7 @@ struct SortRowsArgs {
   void* kept;
   size_t ld_kept;             // bytes, a multiple of 16
   uint32_t always;
+  uint32_t rows;              // that the launch takes at a time
 };
 struct SortRows {
   static constexpr int kThreads = 256;
@@ -1522,9 +1525,11 @@ struct SortRows {
   struct Regs {};
   template <int PH>
   HCNN_HD static void phase(const SortRowsArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
-    const uint32_t m = bid * 4 + tid / 64, lane = tid % 64;
     const uint32_t n = *a.keep.count;
-    if (m >= a.keep.M || (n == a.keep.M && !a.always)) return;
+    if (n == a.keep.M && !a.always) return;
+    for (uint32_t m = bid * 4 + tid / 64; m < a.keep.M; m += a.rows) row(a, m, n, tid % 64);
+  }
+  HCNN_HD static void row(const SortRowsArgs& a, uint32_t m, uint32_t n, uint32_t lane) {
     const size_t whole = a.row_bytes / 16 * 16;
     if (!KeepRows::kept(a.keep, KeepRows::target(a.keep, m))) {
       if (lane == 0 && a.row_loss) a.row_loss[m] = 0.0f;

@@ -209,6 +209,9 @@ static int emu_tile = -1;
 static uint32_t emu_parts = 1;
 static bool emu_copies = false;
 static uint64_t emu_taken = 0, emu_copied = 0;
+static uint64_t emu_threads = 0xffffffff;        // (hcnn_emu_threads) most threads of a launch
+// Most workgroups of a kernel whose threads go round over what there is to do
+inline size_t most_workgroups(int threads) { return (size_t)(emu_threads / threads); }
 inline int dev_malloc(void** p, size_t bytes) {
   *p = bytes <= emu_largest ? std::malloc(bytes ? bytes : 1) : nullptr;
   return *p ? 0 : 2;
@@ -255,7 +258,7 @@ EmuPhase<K, Args> emu_phase(int ph, std::integer_sequence<int, PH...>) {
 
 template <class K, class Args>
 int launch(hcnn_stream_t, size_t grid, size_t lds_bytes, const Args& a) {
-  if (lds_bytes > max_lds_bytes()) return 1;
+  if (lds_bytes > max_lds_bytes() || (uint64_t)grid * K::kThreads > emu_threads) return 1;
   std::vector<uint32_t> lds(lds_bytes / 4 + 4);
   std::vector<typename K::Regs> regs(K::kThreads);
   constexpr int LP = LoopPhases<K>::value;
@@ -321,6 +324,8 @@ inline int copy_d2d(void* d, const void* s_, size_t bytes, hcnn_stream_t s) {
   return (int)hipMemcpyAsync(d, s_, bytes, hipMemcpyDeviceToDevice, s);
 }
 inline int stream_sync(hcnn_stream_t s) { return (int)hipStreamSynchronize(s); }
+// Most workgroups of a kernel whose threads go round over what there is to do (a launch has fewer than 2^32 threads)
+inline size_t most_workgroups(int threads) { return (size_t)(0x7fffffff / threads); }
 // Is what the stream is given being recorded into a graph?
 inline bool stream_recording(hcnn_stream_t s) {
   hipStreamCaptureStatus status = hipStreamCaptureStatusNone;

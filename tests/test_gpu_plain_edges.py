@@ -165,3 +165,55 @@ def test_copied_operands_of_the_loss(b, case, masked):
     _within(dw, DW, u * DW.abs() + (q + (M + 8) * E * p.abs()).t() @ X.abs() + least, "dw")
     hidden = torch.from_numpy(np.nonzero(t == pc.IGNORE)[0]).cuda()
     assert not hidden.numel() or float(dx[hidden].abs().max()) == 0
+
+
+def test_rows_beyond_one_launchs_threads(b):
+    """2^26 rows and a few: with 64 threads each, more than a launch can have"""
+    M, K, V = 2 ** 26 + 37, 2, 3
+    say("rows", M)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    t = torch.randint(0, V, (M,), generator=g, device="cuda", dtype=torch.int32)
+    w = torch.randn((V, K), generator=g, device="cuda").bfloat16()
+    x = torch.randn((M, K), generator=g, device="cuda").bfloat16()
+    hide = torch.rand(M, generator=g, device="cuda") < 0.1
+    hide[-3] = True
+    t[hide] = pc.IGNORE
+    x[hide] = float("nan")
+    loss, rows, lse = b.ctx.cross_entropy(x, w, t, rows=True)
+    mean, dx, dw = b.ctx.cross_entropy_grad(x, w, t, scale=float(M))
+    assert float(mean) == float(loss)
+    n = int((~hide).sum())
+    total, dws = 0.0, torch.zeros((V, K), dtype=torch.float64, device="cuda")
+    for at in range(0, M, 2 ** 24):
+        s = slice(at, min(M, at + 2 ** 24))
+        keep = ~hide[s]
+        X, T = x[s].double().nan_to_num(), t[s].long().clamp(min=0)
+        L = X @ w.double().t()
+        want = torch.logsumexp(L, 1)
+        want_rows = (want - L.gather(1, T[:, None])[:, 0]) * keep
+        # three scores of two products each: a few units of the last place of the largest
+        err = 16 * pc.E * (1 + L.abs().amax(1)) + pc.FN
+        assert bool(((rows[s].double() - want_rows).abs() <= err).all()) and bool(((lse[s].double() - want * keep).abs() <= err).all()), at
+        p = torch.exp(L - want[:, None])
+        p.scatter_add_(1, T[:, None], torch.full_like(L[:, :1], -1.0))
+        p *= keep[:, None] * (float(M) / n)
+        DX = p @ w.double()
+        # the scores' gradients and the result are rounded to 8 bits each
+        bound = pc.U["bf16"] * DX.abs() + (p.abs() @ w.double().abs().contiguous()) * (pc.U["bf16"] + 64 * pc.FN) + 64 * pc.FN
+        assert bool(((dx[s].double() - DX).abs() <= bound).all()), at
+        assert float(dx[s][hide[s]].abs().max()) == 0
+        total, dws = total + float(want_rows.sum()), dws + p.t().contiguous() @ X
+    assert abs(float(loss) - total / n) <= 1e-5 * total / n
+    # 6 x 10^7 gradients of both signs: their roundings, 2^-9 each at most, add up to far less than 2^-9 of their magnitudes' sum
+    assert float((dw.double() - dws).abs().max()) <= pc.U["bf16"] * (float(dws.abs().max()) + 2.0 ** -4 * M)
+
+
+def test_copy_of_many_numbers(b):
+    M, K, N = 20001, 7001, 2001
+    say("copy of", M * K, "numbers")
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x, w = torch.randn((M, K), generator=g, device="cuda").bfloat16(), (torch.randn((N, K), generator=g, device="cuda") / K ** 0.5).bfloat16()
+    y = b.ctx.linear(x, w)
+    X, W = x.double(), w.double()
+    Z = X @ W.t()
+    _within(y, Z, pc.U["bf16"] * Z.abs() + (K + 4) * pc.E * (X.abs() @ W.abs().t()) + pc.LEAST["bf16"], "y")

@@ -149,3 +149,28 @@ def test_what_the_devices_cases_take():
             assert all(n % 8 for n in (K, N)) and all(_copies(r, c, work) for r, c in ((M, K), (N, K), (M, N)))
         for dtype, M, K, V in pe.COPIED_LOSS:
             assert K % 8 and _copies(M, K, 3.0 * M * K * V) and _copies(V, K, 3.0 * M * K * V)
+
+
+class thread_limit:
+    """The most threads of one launch, while the block runs."""
+
+    def __init__(self, most):
+        self.set, self.most = emu.lib().hcnn_emu_threads, most
+        self.set.argtypes, self.set.restype = [ctypes.c_uint64], None
+
+    def __enter__(self):
+        self.set(self.most)
+
+    def __exit__(self, *_):
+        self.set(2 ** 32 - 1)
+
+
+def test_rows_and_copies_beyond_one_threads_each(b):
+    """a launch has fewer than 2^32 threads: the kernels whose threads follow rows (64 each) and copied bytes go round instead"""
+    with thread_limit(2 ** 14):
+        pc.check_loss(b, "f32", 700, 3, 5, 0.3, junk=True)
+        pc.check_loss(b, "bf16", 600, 7, 20, 0.9)
+        with forced(T128, copies=True) as f:
+            pc.check_linear(b, "bf16", 600, 197, 40, strides=(3, 1))
+            pc.check_loss(b, "f16", 600, 197, 40, 0.3, junk=True)
+            assert f.taken()[1] == 5
