@@ -151,12 +151,12 @@ int hcnn_clip_grad_norm(hcnn_plain* h, size_t n_tensors, const void* const* grad
   }
   if (runs > kMaxSize) return HCNN_ERR_ARG;
   Arena a;
-  const size_t o_part = a.take(runs * 8), o_factor = a.take(4);
+  const size_t o_part = a.take(runs * 8), o_factor = a.take(8);
   int e = reserve(h, a.bytes);
   if (e) return e;
   NormArgs n{};
   n.part = at<double>(h, o_part);
-  n.factor = at<float>(h, o_factor);
+  n.factor = at<double>(h, o_factor);
   n.max_norm = max_norm;
   n.eps = eps;
   n.norm = norm;
@@ -189,7 +189,7 @@ int hcnn_clip_grad_norm(hcnn_plain* h, size_t n_tensors, const void* const* grad
   }
   each_list(false, [&] { return launch<SumSquares>(h->stream, n.first[n.tensors], SumSquares::kLdsBytes, n); });
   if (e) return e;
-  const NormTotalArgs t{at<double>(h, o_part), (uint32_t)runs, max_norm, eps, norm, at<float>(h, o_factor)};
+  const NormTotalArgs t{at<double>(h, o_part), (uint32_t)runs, max_norm, eps, norm, at<double>(h, o_factor)};
   if ((e = launch<NormTotal>(h->stream, 1, NormTotal::kLdsBytes, t))) return e;
   each_list(true, [&] { return launch<ScaleGrads>(h->stream, n.first[n.tensors], 0, n); });
   return e;

@@ -1564,7 +1564,7 @@ struct NormArgs {
   uint32_t tensors;
   double* part;                            // sums of squares of the whole list, a number per workgroup
   uint32_t part_first;                     // of this launch
-  const float* factor;
+  const double* factor;
   double max_norm, eps;                    // ClipSmall
   float* norm;
 };
@@ -1607,10 +1607,10 @@ HCNN_HD double sum_any(const NormRun& r, int tid, int threads) {
                      : sum_squares(reinterpret_cast<const Bfloat*>(r.in), r.n, tid, threads);
 }
 // The norm, and the factor that goes with it: a norm that is no number makes it none
-HCNN_HD float norm_factor(double squares, double max_norm, double eps, float* norm_out) {
+HCNN_HD double norm_factor(double squares, double max_norm, double eps, float* norm_out) {
   const double norm = sqrt(squares), c = max_norm / (norm + eps);
   *norm_out = (float)norm;
-  return c < 1.0 || c != c ? (float)c : 1.0f;
+  return c < 1.0 || c != c ? c : 1.0;
 }
 struct SumSquares {
   static constexpr int kThreads = 256;
@@ -1641,7 +1641,7 @@ struct NormTotalArgs {
   uint32_t parts;
   double max_norm, eps;
   float* norm;
-  float* factor;
+  double* factor;
 };
 struct NormTotal {
   static constexpr int kThreads = 1024;
@@ -1668,8 +1668,8 @@ struct NormTotal {
     }
   }
 };
-template <class T>
-HCNN_HD void scale_run(const T* p, T* to, uint32_t n, float c, int tid, int threads) {
+template <class T, class C>
+HCNN_HD void scale_run(const T* p, T* to, uint32_t n, C c, int tid, int threads) {
   constexpr uint32_t kPer16 = 16 / sizeof(T);
   const uint32_t whole = n / kPer16;
 #pragma unroll 4
@@ -1678,16 +1678,22 @@ HCNN_HD void scale_run(const T* p, T* to, uint32_t n, float c, int tid, int thre
     T t[kPer16];
     __builtin_memcpy(t, &w, 16);
 #pragma unroll
-    for (uint32_t e = 0; e < kPer16; ++e) t[e] = Num<T>::narrow(Num<T>::widen(t[e]) * c);
+    for (uint32_t e = 0; e < kPer16; ++e) t[e] = Num<T>::narrow((float)(Num<T>::widen(t[e]) * c));
     __builtin_memcpy(&w, t, 16);
     st16(reinterpret_cast<char*>(to + (size_t)i * kPer16), w);
   }
-  for (uint32_t i = whole * kPer16 + tid; i < n; i += threads) to[i] = Num<T>::narrow(Num<T>::widen(p[i]) * c);
+  for (uint32_t i = whole * kPer16 + tid; i < n; i += threads) to[i] = Num<T>::narrow((float)(Num<T>::widen(p[i]) * c));
 }
-HCNN_HD void scale_any(const NormRun& r, float c, int tid, int threads) {
+template <class C>
+HCNN_HD void scale_by(const NormRun& r, C c, int tid, int threads) {
   if (r.type == 0) scale_run(reinterpret_cast<const float*>(r.in), reinterpret_cast<float*>(r.out), r.n, c, tid, threads);
   else if (r.type == 1) scale_run(reinterpret_cast<const Half*>(r.in), reinterpret_cast<Half*>(r.out), r.n, c, tid, threads);
   else scale_run(reinterpret_cast<const Bfloat*>(r.in), reinterpret_cast<Bfloat*>(r.out), r.n, c, tid, threads);
+}
+// (a factor near or below the smallest normal 32-bit number has few bits there, or none, where its products with large numbers have all)
+HCNN_HD void scale_any(const NormRun& r, double c, int tid, int threads) {
+  if (c < 7.888609052210118e-31) scale_by(r, c, tid, threads);      // 2^-100
+  else scale_by(r, (float)c, tid, threads);
 }
 struct ScaleGrads {
   static constexpr int kThreads = 256;
@@ -1695,9 +1701,9 @@ struct ScaleGrads {
   struct Regs {};
   template <int PH>
   HCNN_HD static void phase(const NormArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
-    const float c = *a.factor;
+    const double c = *a.factor;
     const NormRun r = norm_run(a, a.first[a.tensors] - 1 - bid);      // the last ones first: the sum has just read them
-    if (c == 1.0f && r.in == r.out) return;                         // nothing to scale, nowhere to copy
+    if ((float)c == 1.0f && r.in == r.out) return;                         // nothing to scale, nowhere to copy
     scale_any(r, c, tid, kThreads);
   }
 };
@@ -1710,7 +1716,7 @@ struct ClipSmall {
   template <int PH>
   HCNN_HD static void phase(const NormArgs& a, unsigned, int tid, uint32_t* lds_words, Regs&) {
     double* lds = reinterpret_cast<double*>(lds_words);
-    float* factor = reinterpret_cast<float*>(lds + kThreads);
+    double* factor = lds + kThreads;
     if constexpr (PH == 0) {
       double s = 0.0;
       for (uint32_t i = 0; i < a.first[a.tensors]; ++i) s += sum_any(norm_run(a, i), tid, kThreads);
@@ -1732,7 +1738,7 @@ struct ClipSmall {
     } else {
       for (uint32_t i = 0; i < a.first[a.tensors]; ++i) {
         const NormRun r = norm_run(a, i);
-        if (*factor != 1.0f || r.in != r.out) scale_any(r, *factor, tid, kThreads);
+        if ((float)*factor != 1.0f || r.in != r.out) scale_any(r, *factor, tid, kThreads);
       }
     }
   }

@@ -113,3 +113,22 @@ WIDE = [("bf16", 4091, 4088, 4072), ("f16", 4005, 4080, 4064)]
 # ... and ones whose odd rows are worth copying
 COPIED = [("bf16", 2501, 2503, 2507), ("f16", 2503, 2601, 2705)]
 COPIED_LOSS = [("bf16", 2051, 1021, 7001), ("f16", 1021, 517, 30011)]
+
+
+# (size of the numbers, largest norm): factors below the smallest normal 32-bit number
+TINY = [(1e30, 1e-9), (2e30, 1e-12), (3e37, 1.0), (1e25, 1e-16)]
+
+
+def check_tiny_factor(b, std, max_norm, where):
+    """32-bit gradients so large, or a norm so small, that the factor has few bits left as a 32-bit number: the scaled numbers have theirs"""
+    rng = np.random.default_rng(15)
+    for sizes in ((50, 7), (40000, 3)):
+        grads = [b.make(np.clip(normal(rng, n, std=std), -3e38, 3e38), "f32") for n in sizes]
+        vals = [b.values(g) for g in grads]
+        norm = float(np.sqrt(sum((v ** 2).sum() for v in vals)))
+        factor = max_norm / (norm + 1e-6)
+        assert factor < 2.0 ** -120
+        out = None if where == "place" else [b.make(np.full(n, 7.0), "f32") for n in sizes]
+        b.ctx.clip_grad_norm(grads, max_norm, out=out)
+        for v, o in zip(vals, out or grads):
+            within(b.values(o), v * factor, (U["f32"] + 4 * E) * np.abs(v) * factor + LEAST["f32"], "gradient")

@@ -217,3 +217,9 @@ def test_copy_of_many_numbers(b):
     X, W = x.double(), w.double()
     Z = X @ W.t()
     _within(y, Z, pc.U["bf16"] * Z.abs() + (K + 4) * pc.E * (X.abs() @ W.abs().t()) + pc.LEAST["bf16"], "y")
+
+
+@pytest.mark.parametrize("where", ["new", "place"])
+@pytest.mark.parametrize("case", pe.TINY, ids=str)
+def test_factors_below_the_normal_numbers(b, case, where):
+    pe.check_tiny_factor(b, *case, where)

@@ -132,3 +132,9 @@ def test_assembly_names_the_registers_it_writes():
                         found += 1
                         assert '"%s"' % register in statement, (os.path.basename(path), statement)
     assert found >= 3
+
+
+@pytest.mark.parametrize("where", ["new", "place"])
+@pytest.mark.parametrize("case", pe.TINY, ids=str)
+def test_factors_below_the_normal_numbers(b, case, where):
+    pe.check_tiny_factor(b, *case, where)
