@@ -1,6 +1,7 @@
 """Further cases of the training operators, shared by the CPU checker's tests and the device's (test helper, not collected).
 Backends, bounds and definitions are plain_cases'."""
 import numpy as np
+from scipy.special import ndtr
 
 import plain_cases as pc
 from plain_cases import E, FN, LEAST, U, normal, within
@@ -132,3 +133,12 @@ def check_tiny_factor(b, std, max_norm, where):
         b.ctx.clip_grad_norm(grads, max_norm, out=out)
         for v, o in zip(vals, out or grads):
             within(b.values(o), v * factor, (U["f32"] + 4 * E) * np.abs(v) * factor + LEAST["f32"], "gradient")
+
+
+def check_gelu_tail(b):
+    """gelu's own digits, where its value is far below its argument: 1e-6 + 1e-7 z^2 of it, and a rounding of the product"""
+    z = np.concatenate([-np.linspace(0.001, 12.8, 3001), np.linspace(0.001, 12.8, 501)])[:, None]
+    x, one = b.make(z, "f32"), b.make(np.ones((1, 1)), "f32")
+    Z = b.values(x)
+    want = Z * ndtr(Z)
+    within(b.values(b.ctx.linear(x, one, activation="gelu")), want, np.abs(want) * (1e-6 + 1e-7 * Z * Z + U["f32"]), "gelu")

@@ -223,3 +223,7 @@ def test_copy_of_many_numbers(b):
 @pytest.mark.parametrize("case", pe.TINY, ids=str)
 def test_factors_below_the_normal_numbers(b, case, where):
     pe.check_tiny_factor(b, *case, where)
+
+
+def test_tail_of_gelu(b):
+    pe.check_gelu_tail(b)

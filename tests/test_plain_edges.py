@@ -6,6 +6,7 @@ import re
 
 import numpy as np
 import pytest
+from scipy.special import erfcx
 
 import emu
 import plain_cases as pc
@@ -138,3 +139,21 @@ def test_assembly_names_the_registers_it_writes():
 @pytest.mark.parametrize("case", pe.TINY, ids=str)
 def test_factors_below_the_normal_numbers(b, case, where):
     pe.check_tiny_factor(b, *case, where)
+
+
+def test_tail_of_gelu(b):
+    pe.check_gelu_tail(b)
+
+
+def test_polynomial_of_the_normal_distribution():
+    """the coefficients themselves, in 64 bits: 1.5e-7 of the tail"""
+    with open(os.path.join(os.path.dirname(_capi.__file__), "csrc", "plain_kernels.h")) as f:
+        body = f.read().split("HCNN_HD float normal_cdf")[1].split("*bell = e")[0]
+    c = float(re.search(r"1\.0f \+ ([\d.]+)f \* fabsf", body).group(1))
+    q = [float(re.search(r"float q = (-?[\d.]+)f", body).group(1))] + [float(v.replace(" ", "")) for v in re.findall(r"q = q \* t ([+-] [\d.]+)f", body)]
+    assert len(q) == 8
+    a = np.linspace(0, 14, 20001)
+    t, p = 1 / (1 + c * a), 0.0
+    for v in q:
+        p = p * t + v
+    assert np.abs(p * t / (erfcx(a / np.sqrt(2)) / 2) - 1).max() < 1.5e-7
