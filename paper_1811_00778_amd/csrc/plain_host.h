@@ -375,7 +375,7 @@ int cross_entropy(hcnn_plain* h, const LossCall& c, bool grad) {
   const size_t fit = kDeltaBytes / (std::max<size_t>(M, 1) * sizeof(T)) / 256 * 256;
   const size_t piece = grad ? std::min(V, std::max<size_t>(fit, 256)) : 0;
   const size_t pieces = grad ? blocks(V, piece) : 0, ld_delta = up(piece, 16 / sizeof(T));
-  const bool direct_x = direct_input<T>(ix), direct_w = direct_input<T>(iw);
+  const bool direct_x = direct_input<T>(ix) && direct_input<T>(ikept), direct_w = direct_input<T>(iw);
   const Shape ss = choose<T>(h, M, V, K, false, direct_x && direct_w);
   Input idelta{nullptr, ld_delta, M, piece, true, a.take(grad ? M * ld_delta * sizeof(T) : 0)};
   const bool direct_d = direct_input<T>(idelta);

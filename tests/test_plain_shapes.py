@@ -174,3 +174,14 @@ def test_rows_and_copies_beyond_one_threads_each(b):
             pc.check_linear(b, "bf16", 600, 197, 40, strides=(3, 1))
             pc.check_loss(b, "f16", 600, 197, 40, 0.3, junk=True)
             assert f.taken()[1] == 5
+
+
+def test_offsets_of_rows_that_take_part_stay_in_32_bits(b):
+    """x and w of broadcast rows have a stride of 0, the copy of the rows that take part has their length: at 4.2 million numbers a row, a tile's rows are
+    more than 2^32 bytes apart there, and its loads past the registers would reach other ones"""
+    x, w = (np.broadcast_to(b.make(np.ones((1, 4200000)), "f32"), (n, 4200000)) for n in (2, 1000))
+    with forced(FLAT) as f, thread_limit(1024):               # (the products' launches are refused: only their shape is looked at)
+        with pytest.raises(_capi.HcnnError):
+            b.ctx.cross_entropy(x, w, b.ints([3, pc.IGNORE], np.int64))
+        taken, _ = f.taken()
+    assert taken == {(STATS, FLAT, False)}
