@@ -140,7 +140,8 @@ def _copies(rows, cols, work):
 def test_what_the_devices_cases_take():
     """the device's cases of plain_edge_cases reach what they are there for, on 256 compute units"""
     with emu.device(emu.lib(), units=256):
-        h = Backend().ctx.raw.handle
+        held = Backend()                                         # (owns the handle)
+        h = held.ctx.raw.handle
         for dtype, M, K, N in pe.WIDE:
             assert _choice(h, dtype, M, N, K, True, True)[0] == T256, (dtype, M, K, N)
             assert _choice(h, dtype, M, K, N, True, True)[0] == T256 and _choice(h, dtype, N, K, M, True, True)[0] == T256
