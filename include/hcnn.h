@@ -331,6 +331,7 @@ int hcnn_measure_ceiling(hcnn_ctx* ctx, int which, double* value_out);
  * work memory (grown to the largest call's need, with a wait for the stream; a call that needs no more allocates nothing, uses no memset
  * and can be recorded into a graph).  Work memory that a recorded call has used stays until hcnn_plain_destroy, also when later calls outgrow
  * it: destroy the graphs first.  A replay uses it like a call: order it with the handle's other calls, on its stream or by events.
+ * Calls on one handle share that memory between their kernels: one thread at a time (threads of their own: handles of their own).
  * Numbers are of one type per call, HCNN_F32, HCNN_F16 (binary16) or HCNN_BF16; sums and statistics are held in 32 bits or more and
  * rounded once, to nearest, ties to even.  Matrices are row by row, numbers of a row side by side, *_stride numbers from a row to the next:
  * any stride for inputs (0: one row for all), at least the row's length for outputs.  Pointers need the alignment of one
