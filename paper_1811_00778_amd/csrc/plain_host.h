@@ -79,7 +79,8 @@ constexpr uint32_t kTileRows[] = {256, 128, 64, 128, 16}, kTileCols[] = {256, 12
 
 // Tile and parts of k by an estimate of the time in us: `load` workgroups for each compute unit, `held` of them at a time; a stage takes
 // what the unit's matrix instructions and LDS need for it (kFull, per workgroup) or a load's way (kAlone), whichever is more; a
-// workgroup's beginning and ending kEnds; parts of k are written and joined.
+// workgroup's beginning and ending kEnds; parts of k are written and joined.  (kFull is that of operands along k.  In 32 bits with both
+// across k a stage of 64 x 64 took 0.7, not 0.5: dw of 8192 x 2048 -> 256 91 us in 512 workgroups where the estimate has 68.)
 template <class T>
 Shape choose(const hcnn_plain* h, size_t M, size_t N, size_t K, bool may_split, bool direct) {
   constexpr bool wide = sizeof(T) == 4;
