@@ -282,7 +282,7 @@ int linear_grad(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void
   if (act != kActNone) {                                   // dz: aligned rows in the work memory
     idz.packed = true;
     idz.ld = up(N, 16 / sizeof(T));
-    if (!room || dx) idz.offset = ar.take(M * idz.ld * sizeof(T));
+    if (dx || (dw && !room)) idz.offset = ar.take(M * idz.ld * sizeof(T));
   } else {
     plan_pack<T>(idz, ar, work * ((dx != nullptr) + (dw != nullptr)));
   }
@@ -303,7 +303,7 @@ int linear_grad(hcnn_plain* h, int act, size_t M, size_t K, size_t N, const void
   } else {
     idz.p = at<void>(h, idz.offset);
     idw.p = at<void>(h, idw.offset);
-    ag.dz = room && !dx ? nullptr : at<void>(h, idz.offset);
+    ag.dz = dx || (dw && !room) ? at<void>(h, idz.offset) : nullptr;     // (db alone takes no dz)
     ag.ld_dz = idz.ld;
   }
   if (M && N && room && (dx || dw)) {

@@ -955,7 +955,7 @@ struct PackRows {
 };
 
 // ---------------------------------------------------------------- gradient of the activation and of the bias
-// dz = dy * act'(z) (written where z is there: rounded to T, the operand type of the two products that take it) and, per block of
+// dz = dy * act'(z) (written where z and a place for it are there: rounded to T, the operand type of the two products that take it) and, per block of
 // rows, the columns' sums of it in 32 bits.  A workgroup takes `rows_each` rows and kCols columns: lanes along the row, four numbers each.
 // binary16 does not hold the products of two of its numbers: 300 x 200 x 2 is infinite there, 1e-4 x 1e-4 nothing.  Where the slope is any
 // number (kRoom), dz is held once for each product, times a power of two for each row of dx or of dw (room_of the largest finite number of that row
@@ -965,7 +965,7 @@ enum { kNoRoom = 0, kRoom = 1 };
 struct ActGradArgs {
   const void *dy, *z;
   void* dz;
-  void* dz_cols;              // kRoom: dz times the columns' powers of two (dz: the rows'); either may be null there
+  void* dz_cols;              // kRoom: dz times the columns' powers of two (dz: the rows'); either may be null
   uint32_t *row_top, *col_top;   // kRoom: bits of the largest magnitudes, 0 before ActTops; either may be null
   float* part;                // [row blocks][ld_part], null: no sums
   size_t ld_dy, ld_z, ld_dz, ld_part;
@@ -1017,7 +1017,7 @@ struct ActGrad {
                 for (int e = 0; e < 4; ++e) t[e] = v[e] * room[e];
                 store_row(static_cast<T*>(a.dz_cols) + m * a.ld_dz + n, left, t);
               }
-            } else {
+            } else if (a.dz) {
               store_row(static_cast<T*>(a.dz) + m * a.ld_dz + n, left, v);
             }
           }

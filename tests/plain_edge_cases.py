@@ -142,3 +142,19 @@ def check_gelu_tail(b):
     Z = b.values(x)
     want = Z * ndtr(Z)
     within(b.values(b.ctx.linear(x, one, activation="gelu")), want, np.abs(want) * (1e-6 + 1e-7 * Z * Z + U["f32"]), "gelu")
+
+
+def check_some_of_the_gradients(b, dtype, name):
+    """any of dx, dw and db by itself is what it is among the others"""
+    rng = np.random.default_rng(16)
+    for M, K, N in ((70, 40, 33), (9, 300, 270)):
+        x, w, dy, z = (b.make(normal(rng, *s), dtype) for s in ((M, K), (N, K), (M, N), (M, N)))
+        z = None if name == "none" else z
+        all_three = b.ctx.linear_grad(dy, x, w, z, activation=name, bias=True)
+        for wanted in range(8):
+            need = [bool(wanted >> i & 1) for i in range(3)]
+            got = b.ctx.linear_grad(dy, x, w, z, activation=name, need_dx=need[0], need_dw=need[1], bias=need[2])
+            for g, a, n in zip(got, all_three, need):
+                assert (g is None) == (not n)
+                if n:
+                    assert np.array_equal(b.values(g), b.values(a)), (M, K, N, need)

@@ -227,3 +227,9 @@ def test_factors_below_the_normal_numbers(b, case, where):
 
 def test_tail_of_gelu(b):
     pe.check_gelu_tail(b)
+
+
+@pytest.mark.parametrize("name", ["none", "square", "relu", "gelu"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_some_of_the_gradients(b, dtype, name):
+    pe.check_some_of_the_gradients(b, dtype, name)

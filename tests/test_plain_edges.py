@@ -157,3 +157,9 @@ def test_polynomial_of_the_normal_distribution():
     for v in q:
         p = p * t + v
     assert np.abs(p * t / (erfcx(a / np.sqrt(2)) / 2) - 1).max() < 1.5e-7
+
+
+@pytest.mark.parametrize("name", ["none", "square", "relu", "gelu"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_some_of_the_gradients(b, dtype, name):
+    pe.check_some_of_the_gradients(b, dtype, name)
