@@ -158,3 +158,16 @@ def check_some_of_the_gradients(b, dtype, name):
                 assert (g is None) == (not n)
                 if n:
                     assert np.array_equal(b.values(g), b.values(a)), (M, K, N, need)
+
+
+def check_some_of_the_loss(b, dtype, M, D, V):
+    """the loss' gradients by themselves, and the loss alone, are what they are together"""
+    x, w, t = pc.loss_inputs(b, dtype, M, D, V, 0.3)
+    targets = b.ints(t, np.int64)
+    loss, dx, dw = (b.values(v) for v in b.ctx.cross_entropy_grad(x, w, targets, scale=3.0))
+    for need_dx, need_dw in ((True, False), (False, True), (False, False)):
+        got = b.ctx.cross_entropy_grad(x, w, targets, scale=3.0, need_dx=need_dx, need_dw=need_dw)
+        assert np.array_equal(b.values(got[0]), loss)
+        assert (got[1] is None) == (not need_dx) and (got[2] is None) == (not need_dw)
+        assert not need_dx or np.array_equal(b.values(got[1]), dx)
+        assert not need_dw or np.array_equal(b.values(got[2]), dw)

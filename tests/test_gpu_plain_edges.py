@@ -233,3 +233,9 @@ def test_tail_of_gelu(b):
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_some_of_the_gradients(b, dtype, name):
     pe.check_some_of_the_gradients(b, dtype, name)
+
+
+@pytest.mark.parametrize("shape", [(50, 20, 9), (70, 33, 300), (3, 0, 20), (1, 40, 1000)], ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_some_of_the_loss(b, dtype, shape):
+    pe.check_some_of_the_loss(b, dtype, *shape)

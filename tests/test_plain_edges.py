@@ -163,3 +163,29 @@ def test_polynomial_of_the_normal_distribution():
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_some_of_the_gradients(b, dtype, name):
     pe.check_some_of_the_gradients(b, dtype, name)
+
+
+@pytest.mark.parametrize("shape", [(50, 20, 9), (70, 33, 300), (3, 0, 20), (1, 40, 1000)], ids=str)
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_some_of_the_loss(b, dtype, shape):
+    pe.check_some_of_the_loss(b, dtype, *shape)
+
+
+@pytest.mark.parametrize("V", [9, 300])
+def test_outputs_of_the_losses_entry_points(b, V):
+    """each of the optional outputs by itself, as C calls them"""
+    x, w, t = pc.loss_inputs(b, "f32", 70, 33, V, 0.3)
+    loss, rows, lse = b.ctx.cross_entropy(x, w, b.ints(t, np.int64), rows=True)
+    dx, dw = b.ctx.cross_entropy_grad(x, w, b.ints(t, np.int64))[1:]
+    given = (_capi.F32, 70, 33, V, x.ctypes.data, 33, w.ctypes.data, 33, t.ctypes.data, 8, pc.IGNORE)
+    for wanted in range(8):
+        out = [np.full_like(v, np.nan) for v in (rows, lse, loss)]
+        b.ctx.raw.call("hcnn_cross_entropy", *given, *[o.ctypes.data if wanted >> i & 1 else None for i, o in enumerate(out)])
+        for i, (o, v) in enumerate(zip(out, (rows, lse, loss))):
+            assert np.array_equal(o, v) if wanted >> i & 1 else np.isnan(o).all()
+    for wanted in range(16):
+        out = [np.full_like(v, np.nan) for v in (rows, loss, dx, dw)]
+        p = [o.ctypes.data if wanted >> i & 1 else None for i, o in enumerate(out)]
+        b.ctx.raw.call("hcnn_cross_entropy_grad", *given, 1.0, p[0], p[1], p[2], 33, p[3], 33)
+        for i, (o, v) in enumerate(zip(out, (rows, loss, dx, dw))):
+            assert np.array_equal(o, v) if wanted >> i & 1 else np.isnan(o).all()
