@@ -1,0 +1,406 @@
+"""Further operators of the plain network whose speed is measured: what stands between its linear layers in training, and its answer from weights of four
+bits, through paper_1811_00778_amd.binding.PlainContext.
+
+A case is a dict of plain values; "kind" says which call it is:
+    norm       h = x + residual, y = h / sqrt(mean of h^2 + eps) * weight of every row; with "format" y leaves in mx8
+    norm-grad  its gradients from the stored h: dx = dh + the norm's, and the weight's
+    dropout    y = residual + (x / (1 - p) where a counter-based generator keeps it, else 0); without residual also the gradient's form
+    quantize   a matrix in a microscaled format, and the values that it then stands for
+    linear     y = act(x w^T + bias) + residual of a microscaled x and a w of four bits
+`own` False computes each in its plain form, True calls the library.
+
+Microscaled: blocks of 32 numbers along a row share a power of two; numbers are e2m1 (mx4) or e4m3 (mx8).  Codes are uint8 [rows][K / 2 or K], K the row's
+length up to whole 128, the lower half of a byte first, 0 behind the row; exponents are uint8 [K / 128][rows][4] (127: 2^0, also where there is no block).
+"""
+import math
+
+import torch
+
+own = False
+
+EPS = 1e-6
+DTYPES = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+ACTS = ("none", "square", "relu", "gelu", "silu")
+TOP = {"mx4": 2, "mx8": 8}               # exponent of the format's largest number
+MOST = {"mx4": 6.0, "mx8": 448.0}
+
+
+def listed():
+    return [
+        # one sample's answer: the norm in front of a layer whose weights have four bits, bound by the call itself
+        dict(name="norm-answer", kind="norm", rows=1, n=4096, dtype="bf16", residual=True, weight=True, format="mx8"),
+        # a training batch between two wide layers
+        dict(name="norm-train", kind="norm", rows=8192, n=4096, dtype="bf16", residual=True, weight=True, format=None),
+        # odd sizes, half precision, eight bits out
+        dict(name="norm-odd", kind="norm", rows=1237, n=1031, dtype="f16", residual=False, weight=True, format="mx8"),
+        # the training batch's way back, the residual's gradient added
+        dict(name="norm-grad-train", kind="norm-grad", rows=8192, n=4096, dtype="bf16", dh=True, weight=True),
+        # narrow rows of odd length, 32 bits
+        dict(name="norm-grad-odd", kind="norm-grad", rows=30011, n=77, dtype="f32", dh=False, weight=True),
+        # hidden numbers of the MNIST-shaped network in front of its class scores, one image for each slot
+        dict(name="dropout-hidden", kind="dropout", rows=8192, n=800, dtype="f32", residual=False, p=0.5),
+        # the largest: a wide layer's outputs, and the residual
+        dict(name="dropout-wide", kind="dropout", rows=8192, n=16384, dtype="bf16", residual=True, p=0.1),
+        # a wide layer's weights
+        dict(name="quantize-weights", kind="quantize", rows=16384, n=4096, dtype="bf16", format="mx4"),
+        # rows of odd length in 32 bits
+        dict(name="quantize-odd", kind="quantize", rows=1021, n=517, dtype="f32", format="mx4"),
+        # one sample's answer through one wide layer: bound by reading the weights and by the call itself
+        dict(name="linear-answer", kind="linear", rows=1, n_in=4096, n_out=16384, dtype="bf16", format="mx8", act="silu", bias=False, residual=False),
+        # odd sizes in every direction, half precision
+        dict(name="linear-odd", kind="linear", rows=517, n_in=1031, n_out=777, dtype="f16", format="mx8", act="gelu", bias=True, residual=True),
+        # a wide layer on a large batch, both sides in four bits
+        dict(name="linear-wide", kind="linear", rows=8192, n_in=4096, n_out=16384, dtype="bf16", format="mx4", act="gelu", bias=True, residual=False),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return max(lo, min(hi, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi + 0.49)))))))
+
+
+def draw(rng):
+    kind = rng.choice(["norm", "norm", "norm-grad", "dropout", "quantize", "linear", "linear", "linear"])
+    dtype = rng.choice(["f32", "f16", "bf16", "bf16"])
+    if kind == "linear":
+        while True:
+            rows, n_in, n_out = _log_int(rng, 1, 100_000), _log_int(rng, 9, 8192), _log_int(rng, 2, 16384)
+            if rng.random() < 0.4:
+                n_in, n_out = -(-n_in // 64) * 64, -(-n_out // 64) * 64
+            if rows * n_in * n_out <= 8192 * 4096 * 16384 // 2 and rows * (n_in + n_out) <= 1 << 27:
+                break
+        return dict(kind=kind, rows=rows, n_in=n_in, n_out=n_out, dtype=dtype, format=rng.choice(["mx4", "mx8"]), act=rng.choice(ACTS),
+                    bias=rng.random() < 0.6, residual=rng.random() < 0.4)
+    while True:
+        rows, n = _log_int(rng, 1, 150_000), _log_int(rng, 2, 16384)
+        if rng.random() < 0.4:
+            n = -(-n // 64) * 64
+        if rows * n <= (1 << 26 if dtype == "f32" else 1 << 27):
+            break
+    case = dict(kind=kind, rows=rows, n=n, dtype=dtype)
+    if kind == "norm":
+        case.update(residual=rng.random() < 0.6, weight=rng.random() < 0.8, format=rng.choice([None, None, "mx8"]))
+    elif kind == "norm-grad":
+        case.update(dh=rng.random() < 0.6, weight=rng.random() < 0.8)
+    elif kind == "dropout":
+        case.update(residual=rng.random() < 0.5, p=rng.choice([0.05, 0.1, 0.2, 0.5, 0.9]))
+    else:
+        case["format"] = rng.choice(["mx4", "mx4", "mx8"])
+    return case
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed * 1000003 + 29)
+    dt = DTYPES[case["dtype"]]
+
+    def normal(*shape, std=1.0, to=dt):
+        return (torch.randn(shape, generator=g, device="cuda") * std).to(to)
+
+    state = dict(case)
+    rows = case["rows"]
+    if case["kind"] == "linear":
+        # what a program has in hand: the layer's weights, quantised once, and an input that the call before has left in its format
+        n_in, n_out = case["n_in"], case["n_out"]
+        state["x"] = _encode(*_quantize(normal(rows, n_in, to=torch.float32), case["format"]), case["format"])
+        state["w"] = _encode(*_quantize(normal(n_out, n_in, std=n_in ** -0.5, to=torch.float32), "mx4"), "mx4")
+        state["b"] = normal(n_out, std=0.1) if case["bias"] else None
+        state["r"] = normal(rows, n_out) if case["residual"] else None
+        return state
+    n = case["n"]
+    # rows of different size, as they are after some layers
+    x = torch.randn((rows, n), generator=g, device="cuda") * torch.exp(torch.randn((rows, 1), generator=g, device="cuda"))
+    state["x"] = x.to(dt)
+    if case["kind"] == "quantize":
+        state["x"] = normal(rows, n, std=n ** -0.5)
+    if case["kind"] == "dropout":
+        state.update(seed=(seed * 0x9E3779B97F4A7C15 + 7) % (1 << 63), stream=seed % 1000)
+        state["r"] = normal(rows, n) if case["residual"] else None
+    if case["kind"] == "norm":
+        state["r"] = normal(rows, n) if case["residual"] else None
+    if case["kind"] == "norm-grad":
+        state.update(dy=normal(rows, n, std=0.01), dh=normal(rows, n, std=0.01) if case["dh"] else None)
+    if case["kind"].startswith("norm"):
+        state["w"] = (1 + 0.1 * torch.randn(n, generator=g, device="cuda")).to(dt) if case["weight"] else None
+    return state
+
+
+def _quantize(v, form):
+    """(numbers in the format's grid, exponents of the blocks) of the rows of v, whole blocks up to a multiple of 128 numbers: [rows][blocks][32] and [rows][blocks].
+    All steps are exact: the scale is a power of two."""
+    v = torch.nn.functional.pad(v, (0, -v.shape[1] % 128))
+    v = v.reshape(v.shape[0], -1, 32)
+    top = v.abs().amax(2)
+    e = torch.where(top > 0, torch.clamp(torch.frexp(top)[1] - 1 - TOP[form], -127, 127), torch.zeros((), dtype=torch.int32, device=v.device))
+    v = torch.ldexp(v, -e[:, :, None])
+    # steps of the grid: 2^-1 below 2 and 2^-2 of the power of two below the number above (e2m1), 2^-9 below 2^-6 and 2^-3 of that power (e4m3)
+    least, bits = (0, 1) if form == "mx4" else (-6, 3)
+    step = torch.ldexp(torch.ones((), device=v.device), torch.clamp(torch.frexp(v)[1] - 1, min=least) - bits)
+    v = torch.clamp(torch.round(v / step) * step, -MOST[form], MOST[form])
+    return v, e
+
+
+def _places(e):
+    """exponents [rows][blocks] -> [blocks / 4][rows][4], as the bytes"""
+    return (e + 127).to(torch.uint8).reshape(e.shape[0], -1, 4).transpose(0, 1).contiguous()
+
+
+def _encode(v, e, form):
+    rows = v.shape[0]
+    if form == "mx8":
+        return v.reshape(rows, -1).to(torch.float8_e4m3fn).view(torch.uint8), _places(e)
+    a = v.abs().reshape(rows, -1)
+    code = torch.where(a < 2, 2 * a, torch.where(a < 4, a + 2, a / 2 + 4)) + 8 * (v.reshape(rows, -1) < 0)
+    code = code.to(torch.uint8)
+    return code[:, 0::2] + 16 * code[:, 1::2], _places(e)
+
+
+def _decode(codes, scales, n, form, to):
+    """The first n numbers of every row, in the type `to`."""
+    rows = codes.shape[0]
+    if form == "mx8":
+        v = codes.view(torch.float8_e4m3fn).to(to)
+    else:
+        c = torch.stack([codes & 15, codes >> 4], 2).reshape(rows, -1)
+        v = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, 0, -0.5, -1, -1.5, -2, -3, -4, -6], dtype=to, device=codes.device)[c.int()]
+    e = scales.transpose(0, 1).reshape(rows, -1, 1).int() - 127
+    return torch.ldexp(v.reshape(rows, -1, 32), e).reshape(rows, -1)[:, :n]
+
+
+def _act(z, name):
+    if name == "square":
+        return z * z
+    if name == "relu":
+        return torch.where(z > 0, z, torch.zeros_like(z))
+    if name == "gelu":
+        return 0.5 * z * (1 + torch.erf(z * math.sqrt(0.5)))
+    if name == "silu":
+        return z / (1 + torch.exp(-z))
+    return z
+
+
+def _microscaled(v, e):
+    """What a matrix in mx8 holds: its numbers, 0 behind every row's end, and the scales."""
+    return {"numbers": v.reshape(v.shape[0], -1).to(torch.float8_e4m3fn), "scales": _places(e).view(torch.float8_e8m0fnu)}
+
+
+def _norm(s):
+    # (in 64 bits where the result is rounded to a few: numbers next to a border)
+    wide = torch.float32 if s["format"] is None else torch.float64
+    h = s["x"].to(wide)
+    if s["r"] is not None:
+        h = h + s["r"].to(wide)
+    y = h / torch.sqrt((h * h).mean(1, keepdim=True) + EPS)
+    if s["w"] is not None:
+        y = y * s["w"].to(wide)
+    dt = s["x"].dtype
+    out = {"y": y.to(dt)} if s["format"] is None else _microscaled(*_quantize(y, s["format"]))
+    if s["r"] is not None:
+        out["h"] = h.to(dt)
+    return out
+
+
+def _norm_grad(s):
+    h, g = s["x"].float(), s["dy"].float()
+    r = 1 / torch.sqrt((h * h).mean(1, keepdim=True) + EPS)
+    xh = h * r
+    dw = (g * xh).sum(0)
+    if s["w"] is not None:
+        g = g * s["w"].float()
+    dx = r * (g - xh * (g * xh).mean(1, keepdim=True))
+    if s["dh"] is not None:
+        dx = dx + s["dh"].float()
+    dt = s["x"].dtype
+    return {"dx": dx.to(dt), "dw": dw.to(dt)} if s["w"] is not None else {"dx": dx.to(dt)}
+
+
+def _words(rows, quads, seed, stream):
+    """Philox4x32 with ten rounds, counter (quad of columns, row, stream, 4 * 2^24), key = seed: [rows][4 quads] words below 2^32.  (The product of two
+    32-bit numbers wraps as a signed 64-bit one; both of its halves are right.)"""
+    mask = 0xFFFFFFFF
+    c0 = torch.arange(quads, device="cuda")[None, :].expand(rows, quads)
+    c1 = torch.arange(rows, device="cuda")[:, None].expand(rows, quads)
+    c2, c3 = torch.full_like(c0, stream), torch.full_like(c0, 4 << 24)
+    k0, k1 = seed & mask, seed >> 32
+    for i in range(10):
+        p0, p1 = c0 * 0xD2511F53, c2 * 0xCD9E8D57
+        c0, c1, c2, c3 = (p1 >> 32 & mask) ^ c1 ^ (k0 + i * 0x9E3779B9 & mask), p1 & mask, (p0 >> 32 & mask) ^ c3 ^ (k1 + i * 0xBB67AE85 & mask), p0 & mask
+    return torch.stack([c0, c1, c2, c3], 2).reshape(rows, -1)
+
+
+def _dropout(s):
+    rows, n = s["x"].shape
+    keep = _words(rows, -(-n // 4), s["seed"], s["stream"])[:, :n] >= round(s["p"] * 2 ** 32)
+    y = torch.where(keep, s["x"].float() * (1 / (1 - s["p"])), torch.zeros((), device="cuda"))
+    if s["r"] is not None:
+        y = y + s["r"].float()
+    return {"y": y.to(s["x"].dtype)}
+
+
+def _quantized(s):
+    v, e = _quantize(s["x"].float(), s["format"])
+    values = torch.ldexp(v, e[:, :, None]).reshape(v.shape[0], -1)[:, :s["n"]]
+    return {"values": values.to(s["x"].dtype), "scales": _places(e).view(torch.float8_e8m0fnu)}
+
+
+def _linear(s):
+    x, w = _decode(*s["x"], s["n_in"], s["format"], torch.float32), _decode(*s["w"], s["n_in"], "mx4", torch.float32)
+    z = x @ w.t()
+    if s["b"] is not None:
+        z = z + s["b"].float()
+    y = _act(z, s["act"])
+    if s["r"] is not None:
+        y = y + s["r"].float()
+    return {"y": y.to(DTYPES[s["dtype"]])}
+
+
+_handle = None
+
+
+def _context():
+    """The handle that a program keeps as long as it runs."""
+    global _handle
+    if _handle is None:
+        from paper_1811_00778_amd import binding
+        _handle = binding.PlainContext()
+    return _handle
+
+
+def run(s):
+    if not own:
+        return {"norm": _norm, "norm-grad": _norm_grad, "dropout": _dropout, "quantize": _quantized, "linear": _linear}[s["kind"]](s)
+    ctx = _context()
+    kind = s["kind"]
+    if kind == "linear":
+        from paper_1811_00778_amd.binding import Microscaled
+        x, w = Microscaled(*s["x"], s["n_in"], s["format"]), Microscaled(*s["w"], s["n_in"], "mx4")
+        return {"y": ctx.linear_mx(x, w, s["b"], s["r"], activation=s["act"], dtype=DTYPES[s["dtype"]])}
+    if kind == "quantize":
+        m, values = ctx.quantize_mx(s["x"], s["format"], values=True)
+        return {"values": values, "scales": m.scales.view(torch.float8_e8m0fnu)}
+    if kind == "dropout":
+        if s["r"] is None:
+            return {"y": ctx.dropout_grad(s["x"], s["p"], s["seed"], s["stream"])}
+        return {"y": ctx.dropout(s["x"], s["p"], s["seed"], s["stream"], residual=s["r"])}
+    if kind == "norm-grad":
+        dx, dw = ctx.rms_norm_grad(s["dy"], s["x"], s["w"], s["dh"], eps=EPS)
+        return {"dx": dx} if dw is None else {"dx": dx, "dw": dw}
+    keep = s["r"] is not None
+    got = ctx.rms_norm(s["x"], s["w"], s["r"], eps=EPS, keep=keep, format=s["format"])
+    y, h = got if keep else (got, None)
+    out = {"y": y} if s["format"] is None else {"numbers": y.codes.view(torch.float8_e4m3fn), "scales": y.scales.view(torch.float8_e8m0fnu)}
+    return {**out, "h": h} if keep else out
+
+
+def work(case):
+    size = 4 if case["dtype"] == "f32" else 2
+    rows = case["rows"]
+    held = {None: size, "mx8": 1 + 1 / 32, "mx4": 0.5 + 1 / 32}
+    if case["kind"] == "linear":
+        m, k, n = rows, case["n_in"], case["n_out"]
+        return {"bytes": m * k * held[case["format"]] + n * k * held["mx4"] + size * (m * n * (1 + case["residual"]) + n * case["bias"]), "flops": 2 * m * n * k}
+    n = case["n"]
+    cells = rows * n
+    if case["kind"] == "norm":
+        return {"bytes": cells * (size * (1 + 2 * case["residual"]) + held[case["format"]]) + size * n * case["weight"], "flops": 4 * cells}
+    if case["kind"] == "norm-grad":
+        return {"bytes": size * (cells * (3 + case["dh"]) + 2 * n * case["weight"]), "flops": 9 * cells}
+    if case["kind"] == "dropout":
+        return {"bytes": size * cells * (2 + case["residual"]), "flops": 2 * cells}
+    return {"bytes": cells * (2 * size + held[case["format"]]), "flops": 4 * cells}
+
+
+def _grid(form):
+    """The format's numbers that are not negative, in order: code i is the i-th."""
+    if form == "mx4":
+        return torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64, device="cuda")
+    c = torch.arange(127, device="cuda")
+    return torch.where(c < 8, c * 2.0 ** -9, (8 + c % 8).double() * torch.pow(2.0, (c // 8 - 10).double()))
+
+
+def _nearest(v, form):
+    """(numbers times their scale, numbers, scales as 64-bit numbers) of a 64-bit matrix by search in the list of the format's numbers."""
+    rows, n = v.shape
+    whole = torch.zeros((rows, -(-n // 128) * 128), dtype=torch.float64, device=v.device)
+    whole[:, :n] = v
+    grid = _grid(form)
+    scale = torch.ones((rows, whole.shape[1] // 32), dtype=torch.float64, device=v.device)
+    for some in torch.arange(rows, device=v.device).split(2048):
+        top = whole[some].reshape(some.numel(), -1, 32).abs().amax(2)
+        # the power of two at or below the largest magnitude (corrected where the logarithm's rounding leaves it beside)
+        k = torch.floor(torch.log2(torch.where(top > 0, top, torch.ones_like(top))))
+        k = k - (torch.pow(2.0, k) > top).double() + (torch.pow(2.0, k + 1) <= top).double()
+        scale[some] = torch.where(top > 0, torch.pow(2.0, torch.clamp(k - TOP[form], -127, 127)), torch.ones_like(top))
+        x = whole[some] / scale[some].repeat_interleave(32, 1)
+        a = x.abs().clamp(max=MOST[form])
+        above = torch.searchsorted(grid, a.reshape(-1)).reshape(a.shape).clamp(min=1, max=grid.numel() - 1)
+        lo, hi = grid[above - 1], grid[above]
+        up = (hi - a < a - lo) | ((hi - a == a - lo) & (above % 2 == 0))
+        whole[some] = torch.where(up, hi, lo) * torch.where(x < 0, -1.0, 1.0)
+    placed = scale.reshape(rows, -1, 4).transpose(0, 1)
+    return (whole * scale.repeat_interleave(32, 1))[:, :n], whole, placed
+
+
+def _high_word(a, m):
+    """Upper 32 bits of the product of two 32-bit numbers, from halves of 16."""
+    low = (a & 0xFFFF) * (m & 0xFFFF)
+    mid = (a >> 16) * (m & 0xFFFF) + (low >> 16)
+    other = (a & 0xFFFF) * (m >> 16) + (mid & 0xFFFF)
+    return (a >> 16) * (m >> 16) + (mid >> 16) + (other >> 16)
+
+
+def _kept(rows, n, seed, stream, p):
+    """Which numbers stay: the generator's definition, a column of counters at a time."""
+    keep = torch.empty((rows, n), dtype=torch.bool, device="cuda")
+    m, w0, w1, full = (0xD2511F53, 0xCD9E8D57), 0x9E3779B9, 0xBB67AE85, 2 ** 32
+    for some in torch.arange(rows, device="cuda").split(max(1, (1 << 24) // n)):
+        x = [torch.arange(-(-n // 4), device="cuda").repeat(some.numel()), some.repeat_interleave(-(-n // 4)), None, None]
+        x[2], x[3] = torch.zeros_like(x[0]) + stream, torch.zeros_like(x[0]) + (4 << 24)
+        key = [seed % full, seed // full]
+        for _ in range(10):
+            high = _high_word(x[0], m[0]), _high_word(x[2], m[1])
+            low = [(a * (f & 0xFFFF) + ((a * (f >> 16) & 0xFFFF) << 16)) & 0xFFFFFFFF for a, f in ((x[0], m[0]), (x[2], m[1]))]
+            x = [high[1] ^ x[1] ^ key[0], low[1], high[0] ^ x[3] ^ key[1], low[0]]
+            key = [(key[0] + w0) % full, (key[1] + w1) % full]
+        keep[some] = (torch.stack(x, 1).reshape(some.numel(), -1)[:, :n] >= int(p * full + 0.5))
+    return keep
+
+
+def exact(case, seed):
+    """The same from the definitions, in 64 bits."""
+    s = prepare(case, seed)
+    kind = case["kind"]
+    if kind == "linear":
+        def read(m, form):
+            codes, scales = m
+            grid = _grid(form)
+            low = codes if form == "mx8" else torch.stack((codes.remainder(16), codes.div(16, rounding_mode="floor")), -1).flatten(1)
+            sign = 128 if form == "mx8" else 8
+            v = grid[low.remainder(sign).long()] * torch.where(low >= sign, -1.0, 1.0)
+            return (v * torch.pow(2.0, scales.double() - 127).permute(1, 0, 2).flatten(1).repeat_interleave(32, 1))[:, :case["n_in"]].contiguous()
+        x, w = read(s["x"], case["format"]), read(s["w"], "mx4")
+        z = torch.addmm(s["b"].double(), x, w.t()) if case["bias"] else x.mm(w.t())
+        y = {"none": lambda: z, "square": lambda: z.pow(2), "relu": lambda: z.clamp(min=0), "gelu": lambda: z * torch.special.ndtr(z),
+             "silu": lambda: z * torch.sigmoid(z)}[case["act"]]()
+        return {"y": y + s["r"].double() if case["residual"] else y}
+    x = s["x"].double()
+    if kind == "quantize":
+        values, _, scales = _nearest(x, case["format"])
+        return {"values": values, "scales": scales}
+    if kind == "dropout":
+        y = x / (1 - case["p"]) * _kept(case["rows"], case["n"], s["seed"], s["stream"], case["p"])
+        return {"y": y + s["r"].double() if case["residual"] else y}
+    if kind == "norm":
+        h = x + s["r"].double() if case["residual"] else x
+        y = h * torch.rsqrt(torch.linalg.vector_norm(h, dim=1, keepdim=True).square() / case["n"] + EPS)
+        y = y * s["w"].double() if case["weight"] else y
+        out = {"y": y}
+        if case["format"] is not None:
+            _, numbers, scales = _nearest(y, case["format"])
+            out = {"numbers": numbers, "scales": scales}
+        return {**out, "h": h} if case["residual"] else out
+    # the derivative of sum dy y: y_c = w_c h_c r, dr / dh_c = -r^3 h_c / n
+    dy, w = s["dy"].double(), s["w"].double() if case["weight"] else torch.ones(case["n"], dtype=torch.float64, device="cuda")
+    r = (x.pow(2).sum(1) / case["n"] + EPS).pow(-0.5)[:, None]
+    along = torch.einsum("rc,rc,c->r", dy, x, w)[:, None]
+    dx = dy * w * r - x * (r.pow(3) * along / case["n"])
+    dx = dx + s["dh"].double() if case["dh"] else dx
+    return {"dx": dx, "dw": (dy * x * r).sum(0)} if case["weight"] else {"dx": dx}
