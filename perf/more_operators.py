@@ -10,7 +10,8 @@ A case is a dict of plain values; "kind" says which call it is:
 `own` False computes each in its plain form, True calls the library.
 
 Microscaled: blocks of 32 numbers along a row share a power of two; numbers are e2m1 (mx4) or e4m3 (mx8).  Codes are uint8 [rows][K / 2 or K], K the row's
-length up to whole 128, the lower half of a byte first, 0 behind the row; exponents are uint8 [K / 128][rows][4] (127: 2^0, also where there is no block).
+length up to whole 128, the lower half of a byte first, 0 behind the row; exponents are uint8 [K / 32][rows], a multiple of 64 bytes from a row to the next
+(127: 2^0, also where there is no block).
 """
 import math
 
@@ -139,8 +140,11 @@ def _quantize(v, form):
 
 
 def _places(e):
-    """exponents [rows][blocks] -> [blocks / 4][rows][4], as the bytes"""
-    return (e + 127).to(torch.uint8).reshape(e.shape[0], -1, 4).transpose(0, 1).contiguous()
+    """Exponents [rows][blocks] as the bytes that the library takes: [blocks][rows]."""
+    rows, blocks = e.shape
+    to = torch.full((blocks, -(-rows // 64) * 64), 127, dtype=torch.uint8, device=e.device)[:, :rows]
+    to.copy_((e + 127).t())
+    return to
 
 
 def _encode(v, e, form):
@@ -161,7 +165,7 @@ def _decode(codes, scales, n, form, to):
     else:
         c = torch.stack([codes & 15, codes >> 4], 2).reshape(rows, -1)
         v = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, 0, -0.5, -1, -1.5, -2, -3, -4, -6], dtype=to, device=codes.device)[c.int()]
-    e = scales.transpose(0, 1).reshape(rows, -1, 1).int() - 127
+    e = scales.t()[:, :, None].int() - 127
     return torch.ldexp(v.reshape(rows, -1, 32), e).reshape(rows, -1)[:, :n]
 
 
@@ -335,8 +339,7 @@ def _nearest(v, form):
         lo, hi = grid[above - 1], grid[above]
         up = (hi - a < a - lo) | ((hi - a == a - lo) & (above % 2 == 0))
         whole[some] = torch.where(up, hi, lo) * torch.where(x < 0, -1.0, 1.0)
-    placed = scale.reshape(rows, -1, 4).transpose(0, 1)
-    return (whole * scale.repeat_interleave(32, 1))[:, :n], whole, placed
+    return (whole * scale.repeat_interleave(32, 1))[:, :n], whole, scale.t()
 
 
 def _high_word(a, m):
@@ -375,7 +378,7 @@ def exact(case, seed):
             low = codes if form == "mx8" else torch.stack((codes.remainder(16), codes.div(16, rounding_mode="floor")), -1).flatten(1)
             sign = 128 if form == "mx8" else 8
             v = grid[low.remainder(sign).long()] * torch.where(low >= sign, -1.0, 1.0)
-            return (v * torch.pow(2.0, scales.double() - 127).permute(1, 0, 2).flatten(1).repeat_interleave(32, 1))[:, :case["n_in"]].contiguous()
+            return (v * torch.pow(2.0, scales.double() - 127).t().repeat_interleave(32, 1))[:, :case["n_in"]].contiguous()
         x, w = read(s["x"], case["format"]), read(s["w"], "mx4")
         z = torch.addmm(s["b"].double(), x, w.t()) if case["bias"] else x.mm(w.t())
         y = {"none": lambda: z, "square": lambda: z.pow(2), "relu": lambda: z.clamp(min=0), "gelu": lambda: z * torch.special.ndtr(z),
