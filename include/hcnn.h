@@ -396,6 +396,53 @@ int hcnn_cross_entropy_grad(hcnn_plain* h, int dtype, size_t rows, size_t n_in, 
 int hcnn_clip_grad_norm(hcnn_plain* h, size_t n_tensors, const void* const* grads_host, const size_t* counts_host,
                         const int* dtypes_host, void* const* outs_host, double max_norm, double eps, float* norm_dev);
 
+/* ---- between the plain network's layers ------------------------------------------------------ */
+
+/* Dropout: y = residual + (kept ? x / (1 - p) : 0), residual_dev NULL: none.  Number c of row r is kept when word c mod 4 of the four that
+ * Philox4x32 with 10 rounds (see hcnn_sample_ternary) gives for key = (seed low word, seed high word), counter = (c / 4, r, stream, 4 * 2^24) is at
+ * least p * 2^32, rounded to a whole number: no mask is stored, and the gradient for x is the same call with dy_dev in x's place and no
+ * residual (the residual's gradient is dy).  What is not kept is not looked at: it may be infinite or NaN.  p in [0, 1]; 1 keeps nothing.
+ * y_dev may be the buffer of x_dev or of residual_dev with the same stride. */
+int hcnn_dropout(hcnn_plain* h, int dtype, size_t rows, size_t n, const void* x_dev, size_t x_stride, const void* residual_dev,
+                 size_t residual_stride, double p, uint64_t seed, uint32_t stream, void* y_dev, size_t y_stride);
+
+/* Root-mean-square norm of the rows of s = x + residual (residual_dev NULL: s = x):
+ *   y = s / sqrt(mean of s^2 over the row + eps) * weight (weight_dev [n], NULL: ones).
+ * s is a 32-bit sum; sum_dev [rows][n] or NULL takes it rounded to the call's type (what the layers behind add to, and what the gradient takes), y is formed
+ * from it as it is.  Mean and root are held in 64 bits.  eps: from the smallest normal 32-bit number (2^-126) on.
+ * Either y_dev [rows][n], or codes_dev and scales_dev: y in the microscaled format HCNN_MX8, rounded to it once (see hcnn_quantize_mx). */
+int hcnn_rms_norm(hcnn_plain* h, int dtype, size_t rows, size_t n, const void* x_dev, size_t x_stride, const void* residual_dev,
+                  size_t residual_stride, const void* weight_dev, double eps, void* sum_dev, size_t sum_stride, void* y_dev, size_t y_stride,
+                  uint8_t* codes_dev, uint8_t* scales_dev, size_t scale_pitch);
+
+/* Gradients of hcnn_rms_norm at the stored sums sum_dev [rows][n] for dy_dev [rows][n]: with q = 1 / sqrt(mean of s^2 + eps) and u = s q,
+ *   dx = q (weight dy - u * mean of (weight dy u)) + dsum,  dweight = sum over rows of dy u
+ * (dx is the gradient for x and for the residual alike; dsum_dev [rows][n] is what reaches the sums by other ways, NULL: nothing; dweight_dev
+ * [n] NULL: not wanted).  dx_dev may be the buffer of dsum_dev with the same stride. */
+int hcnn_rms_norm_grad(hcnn_plain* h, int dtype, size_t rows, size_t n, const void* dy_dev, size_t dy_stride, const void* sum_dev, size_t sum_stride,
+                       const void* weight_dev, const void* dsum_dev, size_t dsum_stride, double eps, void* dx_dev, size_t dx_stride,
+                       void* dweight_dev);
+
+/* Microscaled formats (OCP Microscaling Formats specification, 2023): blocks of 32 numbers of a row share a power of two 2^e, and numbers are
+ * HCNN_MX4: e2m1, or HCNN_MX8: e4m3.  e = floor(log2 A) - 2 or - 8 for a block whose largest magnitude is A, at least -127; numbers are x 2^-e to nearest, ties
+ * to even, at most 6 or 448 in magnitude.  A block of zeros has e = 0.  A block that holds an infinity or a NaN stands for NaN: byte 255, codes 0.
+ *   codes_dev [rows][K / 2] (HCNN_MX4, the earlier number in a byte's lower half) or [rows][K], K = n up to a multiple of 128: codes 0 behind n;
+ *   scales_dev [K / 32][scale_pitch]: byte e + 127 of every row of a block, side by side; scale_pitch is a multiple of 64 and at least rows, and what lies
+ *   between rows and scale_pitch is neither written nor looked at (but may be read).  Both are aligned to 16 bytes. */
+enum { HCNN_MX4 = 4, HCNN_MX8 = 8 };
+
+/* x_dev [rows][n] in that format; values_dev [rows][n] (NULL: not wanted) takes the numbers that codes and scales stand for, in the call's type. */
+int hcnn_quantize_mx(hcnn_plain* h, int dtype, int format, size_t rows, size_t n, const void* x_dev, size_t x_stride, uint8_t* codes_dev,
+                     uint8_t* scales_dev, size_t scale_pitch, void* values_dev, size_t values_stride);
+
+/* y = act(x w^T + bias) + residual like hcnn_linear, of microscaled matrices: x [rows][n_in] in x_format, w [n_out][n_in] in HCNN_MX4; bias_dev, residual_dev
+ * and y_dev are of the type dtype (y_dev may be residual_dev's buffer with the same stride).  Products of four-bit numbers are exact, their sums are of 32 bits.  Of
+ * eight-bit x the matrix unit cuts the products of eight neighbours to multiples of 2^-13 of the power of two in the largest of them before it adds them up, where
+ * y has 16 bits; where it has 32, x is taken in two parts that lose nothing, at half the rate. */
+int hcnn_linear_mx(hcnn_plain* h, int dtype, int x_format, int activation, size_t rows, size_t n_in, size_t n_out, const uint8_t* x_codes_dev,
+                   const uint8_t* x_scales_dev, size_t x_pitch, const uint8_t* w_codes_dev, const uint8_t* w_scales_dev, size_t w_pitch,
+                   const void* bias_dev, const void* residual_dev, size_t residual_stride, void* y_dev, size_t y_stride);
+
 const char* hcnn_strerror(int code);
 
 #ifdef __cplusplus

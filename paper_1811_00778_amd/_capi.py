@@ -15,6 +15,7 @@ CEILINGS = ["copy_GBps", "read_GBps", "write_GBps", "mul_lo_u32_Tops", "mul_hi_u
 MAX_LIMBS, MAX_FILTERS = 32, 16
 F32, F16, BF16 = 0, 1, 2
 SIZES = {F32: 4, F16: 2, BF16: 2}
+MX_BITS = {"mx4": 4, "mx8": 8}          # HCNN_MX4, HCNN_MX8: also the bits of a number
 ACTIVATIONS = {"none": 0, "square": 1, "relu": 2, "gelu": 3, "silu": 4}
 
 # name -> argtypes; every entry point returns int except hcnn_strerror
@@ -55,6 +56,11 @@ SIGNATURES = {
     "hcnn_cross_entropy_grad": [ptr, C.c_int] + [C.c_size_t] * 3 + [ptr, C.c_size_t] * 2 + [ptr, C.c_int, C.c_int64, C.c_float, ptr, ptr]
                                + [ptr, C.c_size_t] * 2,
     "hcnn_clip_grad_norm": [ptr, C.c_size_t, ptr, ptr, ptr, ptr, C.c_double, C.c_double, ptr],
+    "hcnn_dropout": [ptr, C.c_int] + [C.c_size_t] * 2 + [ptr, C.c_size_t] * 2 + [C.c_double, C.c_uint64, C.c_uint32, ptr, C.c_size_t],
+    "hcnn_rms_norm": [ptr, C.c_int] + [C.c_size_t] * 2 + [ptr, C.c_size_t] * 2 + [ptr, C.c_double] + [ptr, C.c_size_t] * 2 + [ptr, ptr, C.c_size_t],
+    "hcnn_rms_norm_grad": [ptr, C.c_int] + [C.c_size_t] * 2 + [ptr, C.c_size_t] * 2 + [ptr] + [ptr, C.c_size_t] + [C.c_double] + [ptr, C.c_size_t] + [ptr],
+    "hcnn_quantize_mx": [ptr, C.c_int, C.c_int] + [C.c_size_t] * 2 + [ptr, C.c_size_t] + [ptr, ptr, C.c_size_t] + [ptr, C.c_size_t],
+    "hcnn_linear_mx": [ptr] + [C.c_int] * 3 + [C.c_size_t] * 3 + [ptr, ptr, C.c_size_t] * 2 + [ptr] + [ptr, C.c_size_t] * 2,
     "hcnn_strerror": [C.c_int],
 }
 

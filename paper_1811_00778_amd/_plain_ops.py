@@ -6,11 +6,30 @@ A subclass provides
     _targets(x, what)           (address, length, bytes of a number) of a 1-D int32 or int64 array without gaps
     _new(shape, like)           new uninitialised array of the type and place of `like` (None: 32-bit floats)
     _span(x)                    (first byte, one past the last) of the array's memory
+    _bytes(x, what)             (address, shape, strides, bytes from there to the end of the memory it is a view of) of a 2-D array of bytes
+    _new_bytes(rows, cols)      new uninitialised 2-D array of bytes
+    _new_of(shape, dtype)       (new uninitialised array of the type, the type's code)
 Marshalling and checks only: no arithmetic of the method happens here.
 """
 import ctypes as C
 
 from . import _capi
+
+
+class Microscaled:
+    """A matrix of `columns` numbers a row in a microscaled format, "mx4" or "mx8" (hcnn_quantize_mx): codes [rows][bytes of a row], the rows' numbers with zeros up
+    to whole 128, and scales [blocks of 32][rows], the exponents' bytes; in the memory of scales a block's bytes begin a multiple of 64 behind the last one's."""
+
+    __slots__ = ("codes", "scales", "columns", "format")
+
+    def __init__(self, codes, scales, columns, format):
+        if format not in _capi.MX_BITS:
+            raise ValueError("format must be one of %s, got %r" % (", ".join(_capi.MX_BITS), format))
+        self.codes, self.scales, self.columns, self.format = codes, scales, int(columns), format
+
+    @property
+    def shape(self):
+        return self.codes.shape[0], self.columns
 
 
 class PlainOpsMixin:
@@ -101,12 +120,12 @@ class PlainOpsMixin:
         self.raw.call("hcnn_linear", dtype, self._activation(activation), rows, n_in, n_out, xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, zp, n_out)
         return (y, z) if keep else y
 
-    def _bias(self, bias, n_out, dtype):
-        bp, n, b_dtype = self._vector(bias, "bias")
+    def _bias(self, bias, n_out, dtype, what="bias"):
+        bp, n, b_dtype = self._vector(bias, what)
         if n != n_out:
-            raise ValueError("bias must have shape (%d,), got (%d,)" % (n_out, n))
+            raise ValueError("%s must have shape (%d,), got (%d,)" % (what, n_out, n))
         if b_dtype != dtype:
-            raise TypeError("bias must have the type of x")
+            raise TypeError("%s must have the type of x" % what)
         return bp
 
     def linear_grad(self, dy, x, w, z=None, activation="none", bias=False, need_dx=True, need_dw=True):
@@ -174,6 +193,168 @@ class PlainOpsMixin:
         self.raw.call("hcnn_cross_entropy_grad", *args, int(ignore_index), float(scale), None, self._address(loss), self._address(dx), n_in,
                       self._address(dw), n_in)
         return loss, dx, dw
+
+    # ---- between the layers
+    def dropout(self, x, p, seed, stream=0, residual=None, out=None):
+        """residual + (x / (1 - p) where it is kept, else 0) (hcnn_dropout).  What is kept is a function of (seed, stream, row, column) alone: no mask is
+        stored, dropout_grad forms it again.  stream: below 2^32, another one for every layer and step that must not share a mask.  out: where the
+        result goes (the memory of x or of the residual allowed)."""
+        xp, rows, n, ldx, dtype = self._matrix(x, "x")
+        p, seed, stream = float(p), int(seed), int(stream)
+        if not 0.0 <= p <= 1.0:
+            raise ValueError("p must lie between 0 and 1")
+        if not 0 <= seed < 1 << 64 or not 0 <= stream < 1 << 32:
+            raise ValueError("seed must lie between 0 and 2^64 - 1, stream between 0 and 2^32 - 1")
+        rp, ldr = None, 0
+        if residual is not None:
+            rp, _, _, ldr, _ = self._like(residual, (rows, n), dtype, "residual")
+        if out is None:
+            y = self._new((rows, n), x)
+            yp, ldy = self._address(y), n
+        else:
+            y = out
+            yp, _, _, ldy, _ = self._output(y, (rows, n), dtype, "out")
+            for other, at, ld in ((x, xp, ldx), (residual, rp, ldr)):
+                if other is not None and not (yp == at and (ldy == ld or rows == 1)):
+                    self._apart(y, "out", other)
+        self._pre_call()
+        self.raw.call("hcnn_dropout", dtype, rows, n, xp, ldx, rp, ldr, p, seed, stream, yp, ldy)
+        return y
+
+    def dropout_grad(self, dy, p, seed, stream=0, out=None):
+        """Gradient of dropout for x: dy / (1 - p) where x was kept, else 0.  The residual's is dy."""
+        return self.dropout(dy, p, seed, stream, out=out)
+
+    def rms_norm(self, x, weight=None, residual=None, eps=1e-6, keep=False, format=None):
+        """s / sqrt(mean of s^2 over the row + eps) * weight, s = x + residual (hcnn_rms_norm).  x, residual [rows][n], weight [n]; rows may have any stride.
+        With keep returns (y, s): what the next layers add to and rms_norm_grad takes.  format "mx8": y is a Microscaled matrix, what linear_mx takes."""
+        xp, rows, n, ldx, dtype = self._matrix(x, "x")
+        rp = wp = sp = yp = None
+        ldr = pitch = 0
+        if residual is not None:
+            rp, _, _, ldr, _ = self._like(residual, (rows, n), dtype, "residual")
+        if weight is not None:
+            wp = self._bias(weight, n, dtype, "weight")
+        if format not in (None, "mx8"):
+            raise ValueError("format must be None or 'mx8', got %r" % (format,))
+        self._eps(eps)
+        s, codes, scales = None, None, None
+        if keep:
+            s = self._new((rows, n), x)
+            sp = self._address(s)
+        if format is None:
+            y = self._new((rows, n), x)
+            yp = self._address(y)
+        else:
+            y = self._new_microscaled(rows, n, format)
+            codes, _, scales, pitch = self._microscaled(y, "y")
+        self._pre_call()
+        self.raw.call("hcnn_rms_norm", dtype, rows, n, xp, ldx, rp, ldr, wp, float(eps), sp, n, yp, n, codes, scales, pitch)
+        return (y, s) if keep else y
+
+    def rms_norm_grad(self, dy, s, weight=None, ds=None, eps=1e-6, need_dweight=True):
+        """(dx, dweight) of rms_norm for dy [rows][n] at the sums s that it returned with keep (hcnn_rms_norm_grad); ds [rows][n]: the gradient that reaches
+        s by other ways, added.  dx is the gradient for x and for the residual.  dweight is None without a weight or need_dweight."""
+        sp, rows, n, lds, dtype = self._matrix(s, "s")
+        dyp, _, _, ld_dy, _ = self._like(dy, (rows, n), dtype, "dy")
+        wp = dsp = None
+        ld_ds = 0
+        if weight is not None:
+            wp = self._bias(weight, n, dtype, "weight")
+        if ds is not None:
+            dsp, _, _, ld_ds, _ = self._like(ds, (rows, n), dtype, "ds")
+        self._eps(eps)
+        dx = self._new((rows, n), s)
+        dw = self._new((n,), s) if weight is not None and need_dweight else None
+        self._pre_call()
+        self.raw.call("hcnn_rms_norm_grad", dtype, rows, n, dyp, ld_dy, sp, lds, wp, dsp, ld_ds, float(eps), self._address(dx), n, self._address(dw))
+        return dx, dw
+
+    @staticmethod
+    def _eps(eps):
+        if not 2.0 ** -126 <= eps <= 3e38:
+            raise ValueError("eps must be a positive number that 32 bits hold")
+
+    # ---- few bits
+    def _new_microscaled(self, rows, n, format):
+        wide = -(-n // 128) * 128
+        return Microscaled(self._new_bytes(rows, wide // 8 * _capi.MX_BITS[format]), self._new_bytes(wide // 32, -(-rows // 64) * 64)[:, :rows], n, format)
+
+    def _microscaled(self, m, what):
+        """(codes' address, rows, scales' address, their pitch) of a Microscaled matrix whose arrays are what its format says"""
+        if not isinstance(m, Microscaled):
+            raise TypeError("%s must be a Microscaled matrix" % what)
+        if m.columns < 0:
+            raise ValueError("%s must have columns" % what)
+        wide = -(-m.columns // 128) * 128
+        cp, shape, strides, _ = self._bytes(m.codes, "the codes of " + what)
+        rows, row_bytes = shape
+        if row_bytes != wide // 8 * _capi.MX_BITS[m.format] or (rows > 1 and row_bytes and strides[0] != row_bytes) or (rows and row_bytes and strides[1] != 1):
+            raise ValueError("the codes of %s must be a contiguous array of shape (rows, %d)" % (what, wide // 8 * _capi.MX_BITS[m.format]))
+        sp, shape, strides, room = self._bytes(m.scales, "the scales of " + what)
+        if shape != (wide // 32, rows):
+            raise ValueError("the scales of %s must have shape %r, got %r" % (what, (wide // 32, rows), shape))
+        pitch = strides[0] if rows and wide else -(-rows // 64) * 64
+        if rows and wide:
+            if (rows > 1 and strides[1] != 1) or pitch % 64 or pitch < rows:
+                raise ValueError("the scales of %s must be the first bytes of rows that lie a multiple of 64 bytes apart" % what)
+            if room < wide // 32 * pitch:
+                raise ValueError("the memory of the scales of %s must reach to the end of their last row's %d bytes" % (what, pitch))
+            if cp % 16 or sp % 16:
+                raise ValueError("codes and scales of %s must start on 16 bytes" % what)
+        return cp, rows, sp, pitch
+
+    def quantize_mx(self, x, format="mx4", values=False):
+        """x [rows][n] as a Microscaled matrix (hcnn_quantize_mx); with values returns (matrix, the numbers that it stands for, in the type of x)."""
+        xp, rows, n, ldx, dtype = self._matrix(x, "x")
+        if format not in _capi.MX_BITS:
+            raise ValueError("format must be one of %s, got %r" % (", ".join(_capi.MX_BITS), format))
+        m = self._new_microscaled(rows, n, format)
+        cp, _, sp, pitch = self._microscaled(m, "the result")
+        v = self._new((rows, n), x) if values else None
+        self._pre_call()
+        self.raw.call("hcnn_quantize_mx", dtype, _capi.MX_BITS[format], rows, n, xp, ldx, cp, sp, pitch, self._address(v), n)
+        return (m, v) if values else m
+
+    def linear_mx(self, x, w, bias=None, residual=None, activation="none", dtype=None, out=None):
+        """act(x w^T + bias) + residual of Microscaled matrices x [rows][n_in] ("mx4" or "mx8") and w [n_out][n_in] ("mx4") (hcnn_linear_mx).  The result, bias and
+        residual are of one type: dtype, or that of out, residual or bias.  out: where the result goes (the residual's own memory allowed)."""
+        xc, rows, xs, x_pitch = self._microscaled(x, "x")
+        wc, n_out, ws, w_pitch = self._microscaled(w, "w")
+        n_in = x.columns
+        if w.format != "mx4":
+            raise ValueError("w must be of the format 'mx4', got %r" % w.format)
+        if w.columns != n_in:
+            raise ValueError("w must have shape (n_out, %d), got %r" % (n_in, (n_out, w.columns)))
+        if dtype is None:
+            given = [a for a in (out, residual, bias) if a is not None]
+            if not given:
+                raise ValueError("dtype is required without out, residual and bias")
+            dtype = given[0].dtype
+        y, code = (out, None) if out is not None else self._new_of((rows, n_out), dtype)
+        if out is not None:
+            code = self._matrix(out, "out")[4]
+            if out.dtype != dtype:
+                raise TypeError("out must have the type dtype")
+        bp = rp = None
+        ldr = 0
+        if bias is not None:
+            bp = self._bias(bias, n_out, code)
+        if residual is not None:
+            rp, _, _, ldr, _ = self._like(residual, (rows, n_out), code, "residual")
+        if out is None:
+            yp, ldy = self._address(y), n_out
+        else:
+            yp, _, _, ldy, _ = self._output(y, (rows, n_out), code, "out", bias)
+            spans = [self._span(y)] + [self._span(a) for a in (x.codes, x.scales, w.codes, w.scales)]
+            if any(spans[0][0] < b and a < spans[0][1] for a, b in spans[1:]):
+                raise ValueError("out must not overlap an input")
+            if residual is not None and not (yp == rp and (ldy == ldr or rows == 1)):
+                self._apart(y, "out", residual)
+        self._pre_call()
+        self.raw.call("hcnn_linear_mx", code, _capi.MX_BITS[x.format], self._activation(activation), rows, n_in, n_out, xc, xs, x_pitch, wc, ws, w_pitch,
+                      bp, rp, ldr, yp, ldy)
+        return y
 
     # ---- step
     def clip_grad_norm(self, grads, max_norm, out=None, eps=1e-6):

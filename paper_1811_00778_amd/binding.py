@@ -11,7 +11,7 @@ import torch
 
 from . import _capi
 from ._ops import OpsMixin
-from ._plain_ops import PlainOpsMixin
+from ._plain_ops import Microscaled, PlainOpsMixin  # noqa: F401  (Microscaled: for the callers)
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "lib", "libhcnn.so")
 _lib = None
@@ -170,6 +170,19 @@ class PlainContext(PlainOpsMixin):
 
     def _new(self, shape, like):
         return torch.empty(shape, dtype=torch.float32 if like is None else like.dtype, device=self.device)
+
+    def _bytes(self, x, what):
+        if not isinstance(x, torch.Tensor) or x.dtype != torch.uint8 or x.get_device() != self._index or x.dim() != 2:
+            raise TypeError("%s must be a 2-D uint8 tensor on %s" % (what, self.device))
+        return x.data_ptr(), tuple(x.shape), x.stride(), x.untyped_storage().nbytes() - x.storage_offset()
+
+    def _new_bytes(self, rows, cols):
+        return torch.empty((rows, cols), dtype=torch.uint8, device=self.device)
+
+    def _new_of(self, shape, dtype):
+        if dtype not in _PLAIN_DT:
+            raise TypeError("dtype must be torch.float32, torch.float16 or torch.bfloat16, got %r" % (dtype,))
+        return torch.empty(shape, dtype=dtype, device=self.device), _PLAIN_DT[dtype]
 
     @staticmethod
     def _address(x):

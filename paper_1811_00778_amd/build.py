@@ -6,8 +6,10 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(_HERE, "csrc")
 LIB_DIR = os.path.join(_HERE, "lib")
 LIB = os.path.join(LIB_DIR, "libhcnn.so")
-SOURCES = [os.path.join(CSRC, s) for s in ("hcnn.cpp", "plain.cpp", "plain_f32.cpp", "plain_f16.cpp", "plain_bf16.cpp")]
-HEADERS = [os.path.join(CSRC, h) for h in ("platform.h", "modarith.h", "ntt_kernels.h", "fv_kernels.h", "rate_kernels.h", "plain_kernels.h", "plain_host.h")]
+SOURCES = [os.path.join(CSRC, s) for s in ("hcnn.cpp", "plain.cpp", "plain_f32.cpp", "plain_f16.cpp", "plain_bf16.cpp",
+                                                  "plain_rows_f32.cpp", "plain_rows_f16.cpp", "plain_rows_bf16.cpp")]
+HEADERS = [os.path.join(CSRC, h) for h in ("platform.h", "modarith.h", "ntt_kernels.h", "fv_kernels.h", "rate_kernels.h", "philox.h",
+                                                  "plain_kernels.h", "plain_host.h", "plain_rows.h", "plain_mx.h", "plain_rows_host.h")]
 HEADERS.append(os.path.join(os.path.dirname(_HERE), "include", "hcnn.h"))
 
 HIPCC_FLAGS = [

@@ -6,6 +6,7 @@
 #pragma once
 #include "modarith.h"
 #include "ntt_kernels.h"
+#include "philox.h"
 
 namespace hcnn {
 
@@ -1487,17 +1488,6 @@ struct DecRoundKernel {
 // Every output element is a fixed function of (seed, stream, element index): the word source is Philox4x32 with
 // 10 rounds (Salmon et al., SC'11) keyed by the seed, with counter (index low, index high, stream, kind*2^24 +
 // attempt); a call gives four words, used in order, and a sampler that needs more moves on to attempt + 1.
-struct PhiloxWords { uint32_t w[4]; };
-HCNN_HD PhiloxWords philox4x32_10(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0, uint32_t k1) {
-  for (int round = 0; round < 10; ++round) {
-    const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
-    const uint32_t n0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0, n2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
-    c1 = (uint32_t)p1; c3 = (uint32_t)p0; c0 = n0; c2 = n2;
-    k0 += 0x9E3779B9u; k1 += 0xBB67AE85u;
-  }
-  PhiloxWords r; r.w[0] = c0; r.w[1] = c1; r.w[2] = c2; r.w[3] = c3;
-  return r;
-}
 enum { kSampleTernary = 1, kSampleGaussian = 2, kSampleUniform = 3 };
 constexpr uint32_t kSampleMaxAttempts = 256;   // 1024 words: no sampler comes anywhere near (rejection odds <= 2^-29 per try,
                                                // or 1 - 4p/2^32 for a prime p > 2^29 that is not close to 2^30)

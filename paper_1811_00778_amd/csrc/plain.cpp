@@ -1,11 +1,14 @@
 // C ABI of the plain (unencrypted) network's training: argument checks and the calls behind them.  The device build has a
 // translation unit of its own for each number type; the CPU checker is built from hcnn.cpp, which includes this file there.
-#include "plain_host.h"
+#include "plain_rows_host.h"
 
 #ifndef HCNN_HOSTEMU
 PLAIN_TYPE(extern, float)
 PLAIN_TYPE(extern, Half)
 PLAIN_TYPE(extern, Bfloat)
+PLAIN_ROWS_TYPE(extern, float)
+PLAIN_ROWS_TYPE(extern, Half)
+PLAIN_ROWS_TYPE(extern, Bfloat)
 #endif
 
 namespace plain_host {
@@ -15,6 +18,14 @@ constexpr size_t kClipSmall = 32768;
 // The call of the operator for its number type.
 #define PLAIN_BY_TYPE(dtype, fn, ...) \
   (dtype == HCNN_F32 ? fn<float>(__VA_ARGS__) : dtype == HCNN_F16 ? fn<Half>(__VA_ARGS__) : fn<Bfloat>(__VA_ARGS__))
+
+// eps is added to a mean of squares: the smallest normal 32-bit number keeps the inverse root within the range, and the largest keeps a root of it there
+constexpr double kLeastEps = 1.1754943508222875e-38, kMostEps = 3.4028234663852886e38;
+inline bool bad_format(int format) { return format != HCNN_MX4 && format != HCNN_MX8; }
+inline int bad_mx(const uint8_t* codes, const uint8_t* scales, size_t rows, size_t pitch) {
+  if ((reinterpret_cast<uintptr_t>(codes) | reinterpret_cast<uintptr_t>(scales)) % 16) return HCNN_ERR_ALIGN;
+  return pitch % 64 || pitch < rows ? HCNN_ERR_ARG : 0;
+}
 
 int loss_checked(hcnn_plain* h, int dtype, const LossCall& c, bool grad) {
   if (bad_type(dtype)) return HCNN_ERR_ARG;
@@ -193,6 +204,77 @@ int hcnn_clip_grad_norm(hcnn_plain* h, size_t n_tensors, const void* const* grad
   if ((e = launch<NormTotal>(h->stream, 1, NormTotal::kLdsBytes, t))) return e;
   each_list(true, [&] { return launch<ScaleGrads>(h->stream, n.first[n.tensors], 0, n); });
   return e;
+}
+
+int hcnn_dropout(hcnn_plain* h, int dtype, size_t rows, size_t n, const void* x, size_t x_stride, const void* residual, size_t residual_stride, double p,
+                 uint64_t seed, uint32_t stream, void* y, size_t y_stride) {
+  if (!h) return HCNN_ERR_NULL;
+  if (bad_type(dtype) || rows > kMaxSize || n > kMaxSize || !(p >= 0.0 && p <= 1.0)) return HCNN_ERR_ARG;
+  if (rows == 0 || n == 0) return HCNN_OK;
+  if (!x || !y) return HCNN_ERR_NULL;
+  for (const void* q : {x, residual, (const void*)y})
+    if (misaligned(q, dtype)) return HCNN_ERR_ALIGN;
+  if (y_stride < n) return HCNN_ERR_ARG;
+  return PLAIN_BY_TYPE(dtype, dropout, h, rows, n, x, x_stride, residual, residual_stride, p, seed, stream, y, y_stride);
+}
+
+int hcnn_rms_norm(hcnn_plain* h, int dtype, size_t rows, size_t n, const void* x, size_t x_stride, const void* residual, size_t residual_stride,
+                  const void* weight, double eps, void* sum, size_t sum_stride, void* y, size_t y_stride, uint8_t* codes, uint8_t* scales, size_t scale_pitch) {
+  if (!h) return HCNN_ERR_NULL;
+  if (bad_type(dtype) || rows > kMaxSize || n > kMaxSize || !(eps >= kLeastEps && eps <= kMostEps)) return HCNN_ERR_ARG;
+  if (rows == 0 || n == 0) return HCNN_OK;
+  if (!x || (!y && !codes) || !codes != !scales) return HCNN_ERR_NULL;
+  if (y && codes) return HCNN_ERR_ARG;
+  for (const void* q : {x, residual, weight, (const void*)sum, (const void*)y})
+    if (misaligned(q, dtype)) return HCNN_ERR_ALIGN;
+  if ((y && y_stride < n) || (sum && sum_stride < n)) return HCNN_ERR_ARG;
+  if (codes)
+    if (const int e = bad_mx(codes, scales, rows, scale_pitch)) return e;
+  const MxOut to{codes, scales, mx_row_bytes(kMx8, n), scale_pitch};
+  return PLAIN_BY_TYPE(dtype, rms_norm, h, rows, n, x, x_stride, residual, residual_stride, weight, eps, sum, sum_stride, y, y_stride, to);
+}
+
+int hcnn_rms_norm_grad(hcnn_plain* h, int dtype, size_t rows, size_t n, const void* dy, size_t dy_stride, const void* sum, size_t sum_stride,
+                       const void* weight, const void* dsum, size_t dsum_stride, double eps, void* dx, size_t dx_stride, void* dweight) {
+  if (!h) return HCNN_ERR_NULL;
+  if (bad_type(dtype) || rows > kMaxSize || n > kMaxSize || !(eps >= kLeastEps && eps <= kMostEps)) return HCNN_ERR_ARG;
+  if (n == 0) return HCNN_OK;
+  if (rows && (!dy || !sum || !dx)) return HCNN_ERR_NULL;
+  for (const void* q : {dy, sum, weight, dsum, (const void*)dx, (const void*)dweight})
+    if (misaligned(q, dtype)) return HCNN_ERR_ALIGN;
+  if (rows && dx_stride < n) return HCNN_ERR_ARG;
+  return PLAIN_BY_TYPE(dtype, rms_norm_grad, h, rows, n, dy, dy_stride, sum, sum_stride, weight, dsum, dsum_stride, eps, dx, dx_stride, dweight);
+}
+
+int hcnn_quantize_mx(hcnn_plain* h, int dtype, int format, size_t rows, size_t n, const void* x, size_t x_stride, uint8_t* codes, uint8_t* scales,
+                     size_t scale_pitch, void* values, size_t values_stride) {
+  if (!h) return HCNN_ERR_NULL;
+  if (bad_type(dtype) || bad_format(format) || rows > kMaxSize || n > kMaxSize) return HCNN_ERR_ARG;
+  if (rows == 0 || n == 0) return HCNN_OK;
+  if (!x || !codes || !scales) return HCNN_ERR_NULL;
+  if (misaligned(x, dtype) || misaligned(values, dtype)) return HCNN_ERR_ALIGN;
+  if (values && values_stride < n) return HCNN_ERR_ARG;
+  if (const int e = bad_mx(codes, scales, rows, scale_pitch)) return e;
+  const MxOut to{codes, scales, mx_row_bytes(format, n), scale_pitch};
+  return PLAIN_BY_TYPE(dtype, quantize, h, format, rows, n, x, x_stride, to, values, values_stride);
+}
+
+int hcnn_linear_mx(hcnn_plain* h, int dtype, int x_format, int activation, size_t rows, size_t n_in, size_t n_out, const uint8_t* x_codes,
+                   const uint8_t* x_scales, size_t x_pitch, const uint8_t* w_codes, const uint8_t* w_scales, size_t w_pitch, const void* bias,
+                   const void* residual, size_t residual_stride, void* y, size_t y_stride) {
+  if (!h) return HCNN_ERR_NULL;
+  if (bad_type(dtype) || bad_format(x_format) || activation < 0 || activation >= kActCount) return HCNN_ERR_ARG;
+  if (rows > kMaxSize || n_in > kMaxSize || n_out > kMaxSize) return HCNN_ERR_ARG;
+  if (rows == 0 || n_out == 0) return HCNN_OK;
+  if ((n_in && (!x_codes || !x_scales || !w_codes || !w_scales)) || !y) return HCNN_ERR_NULL;
+  for (const void* q : {bias, residual, (const void*)y})
+    if (misaligned(q, dtype)) return HCNN_ERR_ALIGN;
+  if (y_stride < n_out) return HCNN_ERR_ARG;
+  if (n_in)
+    for (const int e : {bad_mx(x_codes, x_scales, rows, x_pitch), bad_mx(w_codes, w_scales, n_out, w_pitch)})
+      if (e) return e;
+  const MxCall c{x_format, activation, rows, n_in, n_out, x_codes, x_scales, x_pitch, w_codes, w_scales, w_pitch, bias, residual, residual_stride, y, y_stride};
+  return PLAIN_BY_TYPE(dtype, linear_mx, h, c);
 }
 
 #ifdef HCNN_HOSTEMU

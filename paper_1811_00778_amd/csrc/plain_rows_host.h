@@ -1,0 +1,181 @@
+// Host side of the operators along rows and of the microscaled products: choice of the kernels' shapes and their order.
+#pragma once
+#include "plain_host.h"
+#include "plain_mx.h"
+
+namespace plain_host {
+
+inline Chunks chunks_of(size_t rows, size_t per_row, int threads, int each) {
+  Chunks c;
+  c.all = (uint64_t)rows * per_row;
+  c.per_row = fast_div((uint32_t)per_row);
+  c.groups = (uint32_t)std::min<uint64_t>((c.all + threads * each - 1) / (threads * each), most_workgroups(threads));
+  return c;
+}
+
+template <class T>
+int dropout(hcnn_plain* h, size_t rows, size_t n, const void* x, size_t ldx, const void* residual, size_t ld_residual, double p, uint64_t seed, uint32_t stream,
+            void* y, size_t ldy) {
+  typedef Dropout<T, false> Plain;
+  const double threshold = std::nearbyint(p * 4294967296.0);
+  DropoutArgs a{};
+  a.chunks = chunks_of(rows, blocks(n, Plain::W), Plain::kThreads, Plain::EACH);
+  a.x = x; a.ldx = ldx; a.residual = residual; a.ld_residual = ld_residual; a.y = y; a.ldy = ldy;
+  a.n = (uint32_t)n;
+  a.none = threshold >= 4294967296.0;
+  a.threshold = a.none ? 0xffffffffu : (uint32_t)threshold;
+  a.scale = p < 1.0 ? (float)(1.0 / (1.0 - p)) : 0.0f;
+  a.seed = seed; a.stream = stream;
+  return residual ? launch<Dropout<T, true>>(h->stream, a.chunks.groups, 0, a) : launch<Plain>(h->stream, a.chunks.groups, 0, a);
+}
+
+// ---------------------------------------------------------------- norm
+// Threads that share a row, and numbers that each of them holds (0: any length, read twice)
+struct RowShape { int lanes, el; };
+inline RowShape row_shape(size_t n) {
+  for (int lanes : {8, 64, 256, 1024})
+    for (int el : {8, 16})
+      if (n <= (size_t)lanes * el) return RowShape{lanes, el};
+  return RowShape{1024, 0};
+}
+#define PLAIN_ROW_SHAPE(s, CALL)                                     \
+  do {                                                               \
+    if (s.lanes == 8) return s.el == 8 ? CALL(8, 8) : CALL(8, 16);   \
+    if (s.lanes == 64) return s.el == 8 ? CALL(64, 8) : CALL(64, 16); \
+    if (s.lanes == 256) return s.el == 8 ? CALL(256, 8) : CALL(256, 16); \
+    return s.el == 8 ? CALL(1024, 8) : s.el == 16 ? CALL(1024, 16) : CALL(1024, 0); \
+  } while (0)
+
+template <class K>
+int norm_rows_launch(hcnn_plain* h, NormRowsArgs a) {
+  const size_t most = most_workgroups(K::kThreads) * K::kLines;       // rows of a launch
+  for (size_t row = 0; row < a.rows; row += most) {
+    a.first = (uint32_t)row;
+    const int e = launch<K>(h->stream, blocks(std::min(most, a.rows - row), K::kLines), K::kLdsBytes, a);
+    if (e) return e;
+  }
+  return 0;
+}
+template <class T, int F>
+int norm_rows(hcnn_plain* h, const NormRowsArgs& a) {
+  const RowShape s = row_shape(F == kMxNone ? a.n : up(a.n, 128));
+#define PLAIN_CALL(L, E) norm_rows_launch<NormRows<T, L, E, F>>(h, a)
+  PLAIN_ROW_SHAPE(s, PLAIN_CALL);
+#undef PLAIN_CALL
+}
+template <class T>
+int rms_norm(hcnn_plain* h, size_t rows, size_t n, const void* x, size_t ldx, const void* residual, size_t ld_residual, const void* weight, double eps, void* hid,
+             size_t ldh, void* y, size_t ldy, const MxOut& to) {
+  NormRowsArgs a{};
+  a.x = x; a.ldx = ldx; a.residual = residual; a.ld_residual = ld_residual; a.weight = weight;
+  a.rows = (uint32_t)rows; a.n = (uint32_t)n; a.per = 1.0 / (double)n; a.eps = eps;
+  a.h = hid; a.ldh = ldh; a.y = y; a.ldy = ldy; a.to = to;
+  return to.codes ? norm_rows<T, kMx8>(h, a) : norm_rows<T, kMxNone>(h, a);
+}
+
+// Rows of a workgroup, and workgroups, of the norm's gradient
+struct RowShare { uint32_t each; size_t groups; };
+inline RowShare norm_share(const hcnn_plain* h, size_t rows, int lines) {
+  const size_t most = (size_t)h->compute_units * 4;
+  const size_t each = up(std::max<size_t>(blocks(rows, most), 1), lines);
+  return RowShare{(uint32_t)each, blocks(rows, each)};
+}
+template <class K>
+int norm_grad_launch(hcnn_plain* h, const NormGradArgs& a, size_t groups) { return launch<K>(h->stream, groups, K::kLdsBytes, a); }
+template <class T>
+int norm_grad_rows(hcnn_plain* h, const NormGradArgs& a, const RowShape& s, size_t groups) {
+#define PLAIN_CALL(L, E) norm_grad_launch<NormGrad<T, L, E>>(h, a, groups)
+  PLAIN_ROW_SHAPE(s, PLAIN_CALL);
+#undef PLAIN_CALL
+}
+template <class T>
+int rms_norm_grad(hcnn_plain* h, size_t rows, size_t n, const void* dy, size_t ld_dy, const void* hid, size_t ldh, const void* weight, const void* dh, size_t ld_dh,
+                  double eps, void* dx, size_t ld_dx, void* dw) {
+  const RowShape s = row_shape(n);
+  const RowShare share = norm_share(h, rows, s.lanes < 256 ? 256 / s.lanes : 1);
+  // rows of any length: their columns' sums in a pass of their own, about eight workgroups for each compute unit
+  const size_t col_blocks = blocks(n, NormColumns<T>::kCols);
+  const uint32_t col_rows = (uint32_t)std::max<size_t>(16, blocks(rows, std::max<size_t>(1, (size_t)h->compute_units * 8 / col_blocks)));
+  const size_t parts = s.el ? share.groups : blocks(rows, col_rows);
+  Arena ar;
+  NormGradArgs a{};
+  a.ld_part = up(n, 4);
+  const size_t o_part = ar.take(dw ? parts * a.ld_part * 4 : 0), o_inverse = ar.take(dw && !s.el ? rows * 8 : 0);
+  int e = reserve(h, ar.bytes);
+  if (e) return e;
+  a.dy = dy; a.ld_dy = ld_dy; a.h = hid; a.ldh = ldh; a.weight = weight; a.dh = dh; a.ld_dh = ld_dh;
+  a.rows = (uint32_t)rows; a.n = (uint32_t)n; a.rows_each = share.each; a.per = 1.0 / (double)n; a.eps = eps;
+  a.dx = dx; a.ld_dx = ld_dx;
+  a.part = dw ? at<float>(h, o_part) : nullptr;
+  a.inverse = dw && !s.el ? at<double>(h, o_inverse) : nullptr;
+  if (rows) {
+    if ((e = norm_grad_rows<T>(h, a, s, share.groups))) return e;
+    if (dw && !s.el) {
+      a.rows_each = col_rows;
+      if ((e = launch<NormColumns<T>>(h->stream, col_blocks * parts, 0, a))) return e;
+    }
+  }
+  if (dw) {
+    // (a launch has fewer than 2^32 threads: 16 columns for each workgroup)
+    const size_t most = most_workgroups(ColumnSum<T>::kThreads) * 16;
+    for (size_t c = 0; c < n; c += most) {
+      const size_t some = std::min(most, n - c);
+      const ColumnSumArgs cs{at<float>(h, o_part) + c, a.ld_part, (uint32_t)(rows ? parts : 0), (uint32_t)some, static_cast<char*>(dw) + c * sizeof(T)};
+      if ((e = launch<ColumnSum<T>>(h->stream, blocks(some, 16), ColumnSum<T>::kLdsBytes, cs))) return e;
+    }
+  }
+  return 0;
+}
+
+// ---------------------------------------------------------------- microscaled formats
+inline size_t mx_row_bytes(int format, size_t n) { return up(n, 128) / 8 * (size_t)format; }
+template <class T>
+int quantize(hcnn_plain* h, int format, size_t rows, size_t n, const void* x, size_t ldx, const MxOut& to, void* values, size_t ld_values) {
+  typedef Quantize<T, kMx4> Four;
+  QuantizeArgs a{};
+  a.chunks = chunks_of(rows, up(n, 128) / Four::W, Four::kThreads, Four::EACH);
+  a.x = x; a.ldx = ldx; a.n = (uint32_t)n; a.to = to; a.values = values; a.ld_values = ld_values;
+  return format == kMx4 ? launch<Four>(h->stream, a.chunks.groups, 0, a) : launch<Quantize<T, kMx8>>(h->stream, a.chunks.groups, 0, a);
+}
+
+struct MxCall {
+  int format, act;
+  size_t M, K, N;
+  const uint8_t *x, *x_scales; size_t x_pitch;
+  const uint8_t *w, *w_scales; size_t w_pitch;
+  const void *bias, *residual; size_t ld_residual;
+  void* y; size_t ldy;
+};
+template <class T, int F>
+int linear_mx_of(hcnn_plain* h, const MxCall& c) {
+  MxArgs a{};
+  a.g.M = (uint32_t)c.M; a.g.N = (uint32_t)c.N; a.g.act = c.act; a.g.splits = 1;
+  a.g.bias = c.bias; a.g.residual = c.residual; a.g.ld_residual = c.ld_residual; a.g.out = c.y; a.g.ld_out = c.ldy;
+  a.x = c.x; a.x_scales = c.x_scales; a.x_pitch = c.x_pitch; a.x_bytes = mx_row_bytes(F, c.K);
+  a.w = c.w; a.w_scales = c.w_scales; a.w_pitch = c.w_pitch; a.w_bytes = mx_row_bytes(kMx4, c.K);
+  a.steps = (uint32_t)blocks(c.K, 128);
+  auto strip = [&](auto kernel) {
+    typedef decltype(kernel) S;
+    const size_t grid = S::grid(a.g), most = most_workgroups(S::kThreads);
+    int e = 0;
+    for (a.first = 0; a.first < grid && !e; a.first += most) e = launch<S>(h->stream, std::min(most, grid - a.first), S::kLdsBytes, a);
+    return e;
+  };
+  if (c.M <= 16) return c.N <= 16 * (size_t)h->compute_units ? strip(MxStrip<T, F, 1, 1>{}) : strip(MxStrip<T, F, 1, 4>{});
+  if (c.N <= 16) return strip(MxStrip<T, F, 4, 1>{});
+  return strip(MxStrip<T, F, 4, 4>{});
+}
+template <class T>
+int linear_mx(hcnn_plain* h, const MxCall& c) { return c.format == kMx4 ? linear_mx_of<T, kMx4>(h, c) : linear_mx_of<T, kMx8>(h, c); }
+
+}  // namespace plain_host
+
+// What a number type's translation unit defines
+#define PLAIN_ROWS_TYPE(PREFIX, T)                                                                                                            \
+  namespace plain_host {                                                                                                                      \
+  PREFIX template int dropout<T>(hcnn_plain*, size_t, size_t, const void*, size_t, const void*, size_t, double, uint64_t, uint32_t, void*, size_t); \
+  PREFIX template int rms_norm<T>(hcnn_plain*, size_t, size_t, const void*, size_t, const void*, size_t, const void*, double, void*, size_t, void*, size_t, const MxOut&); \
+  PREFIX template int rms_norm_grad<T>(hcnn_plain*, size_t, size_t, const void*, size_t, const void*, size_t, const void*, const void*, size_t, double, void*, size_t, void*); \
+  PREFIX template int quantize<T>(hcnn_plain*, int, size_t, size_t, const void*, size_t, const MxOut&, void*, size_t);                         \
+  PREFIX template int linear_mx<T>(hcnn_plain*, const MxCall&);                                                                               \
+  }
