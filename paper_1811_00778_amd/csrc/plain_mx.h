@@ -20,6 +20,7 @@ struct MxArgs {
   size_t x_bytes, w_bytes;     // of a row
   size_t x_pitch, w_pitch;     // bytes from a block's row scales to the next block's: multiples of 64, so that whole 64 rows can be read
   uint32_t steps;              // of 128 numbers
+  uint32_t part;               // steps of each of g.splits parts of the sum
   uint64_t first;              // tile that the launch begins with
 };
 
@@ -189,6 +190,317 @@ struct MxStrip {
         float bias[4] = {};
         if (a.g.bias) load_row(static_cast<const T*>(a.g.bias) + n, a.g.N - n, bias);
         finish<T>(a.g, m, n, bias, v);
+      }
+    }
+  }
+};
+
+// The form for many rows and columns.  A workgroup computes a tile of BM x BN outputs in WM x WN waves, 16 FM rows by 64 columns each; operands come to LDS past
+// the registers, in slots: of four-bit x two steps (128 bytes of every row, two slots), of eight-bit x one step (128 bytes of x's rows, 64 of w's; three slots), with
+// their scales.  A lane's operands of x go through a ring of kAhead places, read that many products ahead; w's of a step have two places.  The last kAhead
+// of a slot's operands are in registers when the barrier comes: behind it the slot is filled anew while their products run, and the next slot's first are read.
+//   LDS: lines of 128 bytes, piece p of line l at p ^ turn(l).  The 16 rows of one read lie four apart: turn takes its eight values in them, so that they spread
+//   evenly over the banks.
+template <int BYTES, int ROWS, int THREADS>
+struct MxTileRows {
+  static constexpr uint32_t kPieces = BYTES / 16, kLineRows = 128 / BYTES;          // of a row; rows of a line
+  static constexpr int kEach = ROWS * BYTES / 16 / THREADS;
+  static constexpr uint32_t kLdsBytes = ROWS * BYTES;
+  static_assert(ROWS * BYTES % (16 * THREADS) == 0, "every thread has the same number of pieces");
+  HCNN_HD static uint32_t turn(uint32_t line) { return line / (4 / kLineRows) & 7; }
+  HCNN_HD static uint32_t place(uint32_t row, uint32_t piece) {
+    const uint32_t line = row / kLineRows, p = row % kLineRows * kPieces + piece;
+    return line * 128 + ((p ^ turn(line)) << 4);
+  }
+  // (row, piece) that lies at LDS piece c
+  HCNN_HD static void at(uint32_t c, uint32_t* row, uint32_t* piece) {
+    const uint32_t line = c / 8, p = (c % 8) ^ turn(line);
+    *row = line * kLineRows + p / kPieces;
+    *piece = p % kPieces;
+  }
+  // Byte offset of a thread's piece i from the slot's first bytes in the tile's first row.  Rows beyond X: the last one.
+  HCNN_HD static uint32_t offset(size_t ld, uint32_t X, uint32_t x0, int tid, int i) {
+    uint32_t row, piece;
+    at((uint32_t)(tid + i * THREADS), &row, &piece);
+    if (x0 + row >= X) row = X - 1 - x0;
+    return (uint32_t)(row * ld) + piece * 16;
+  }
+  // (every piece of a thread has this number within its row)
+  static_assert(THREADS % 256 == 0, "the threads take whole turns of lines");
+  HCNN_HD static uint32_t piece_of(int tid) {
+    uint32_t row, piece;
+    at((uint32_t)tid, &row, &piece);
+    return piece;
+  }
+};
+// BYTES (16 or 4) of every lane of a wave to LDS, side by side, where step < steps.  (The lanes are switched off, so that no branch stands
+// between the products that such loads are spread over: with one, they were gathered behind it.  All lanes of the workgroup's waves are at work here.)
+template <int BYTES>
+HCNN_HD void load_to_lds(const uint8_t* base, uint32_t off, uint32_t at, [[maybe_unused]] char* lds, [[maybe_unused]] int lane, uint32_t step, uint32_t steps) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  static_assert(BYTES == 16 || BYTES == 4, "what the instruction takes");
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  if constexpr (BYTES == 16)
+    asm volatile("s_mov_b32 m0, %0\n\ts_cmp_lt_u32 %3, %4\n\ts_cselect_b64 exec, -1, 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1" ::"s"(at), "v"(off),
+                 "s"(base), "s"(wave_uniform(step)), "s"(wave_uniform(steps)) : "memory", "m0", "scc");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_cmp_lt_u32 %3, %4\n\ts_cselect_b64 exec, -1, 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, -1" ::"s"(at), "v"(off),
+                 "s"(base), "s"(wave_uniform(step)), "s"(wave_uniform(steps)) : "memory", "m0", "scc");
+#pragma clang diagnostic pop
+#else
+  if (step < steps) __builtin_memcpy(lds + at + lane * BYTES, base + off, BYTES);
+#endif
+}
+// Byte of LDS at which the workgroup's memory begins
+HCNN_HD uint32_t lds_start([[maybe_unused]] const uint32_t* lds) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  return wave_uniform((uint32_t)(uintptr_t)lds);          // (the low half of an LDS pointer is its offset)
+#else
+  return 0;
+#endif
+}
+// What is on its way to LDS past the registers has arrived, all but the last N loads where `behind` is not 0.  (The branch is within the instructions: the compiler
+// moves products behind a branch of its own.)
+template <int N>
+HCNN_HD void direct_all_but([[maybe_unused]] uint32_t behind) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile(
+      "s_cmp_lg_u32 %0, 0\n\ts_cbranch_scc1 .Lhcnn_behind_%=\n\ts_waitcnt vmcnt(0)\n.Lhcnn_behind_%=:\n\ts_waitcnt vmcnt(%1)" ::"s"(wave_uniform(behind)), "n"(N)
+      : "memory", "scc");
+#endif
+}
+
+template <class T, int F, int BM, int BN, int WM, int WN, int EPI>
+struct MxTile {
+  static constexpr int kThreads = WM * WN * 64;
+  static constexpr int kLoopPhases = 4, kPhases = 5;                   // a round of the loop: two steps
+  static constexpr int kMinWavesPerSimd = 2;
+  static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
+  static_assert(FM % 4 == 0 && FN == 4 && (BM + BN) / 64 == WM * WN, "waves take 64 columns; a wave brings 64 rows' scales");
+  static constexpr int kSteps = F == kMx4 ? 2 : 1, kSlots = F == kMx4 ? 2 : 3;       // steps of a slot
+  static constexpr int kAhead = F == kMx4 ? 4 : 2;
+  static constexpr bool kSplit = F == kMx8 && sizeof(T) == 4;
+  typedef MxTileRows<128, BM, kThreads> X;
+  typedef MxTileRows<F == kMx4 ? 128 : 64, BN, kThreads> W;
+  static constexpr uint32_t kScaleBytes = 4 * (BM + BN);               // of a step: [x's blocks][BM], [w's blocks][BN]
+  static constexpr uint32_t kScales = X::kLdsBytes + W::kLdsBytes, kSlot = kScales + kSteps * kScaleBytes;
+  static constexpr size_t kLdsBytes = (size_t)kSlots * kSlot;
+  static constexpr int kLoads = X::kEach + W::kEach + kSteps;          // of a thread for a slot
+  static_assert(kLdsBytes <= 160 * 1024, "the slots fit LDS");
+#if defined(__HIP_DEVICE_COMPILE__)
+  struct Operands { MxFrag<F> x[kAhead]; MxFrag<kMx4> w[2][FN]; uint32_t sx[2][FM / 4], sw[2]; };
+#else
+  struct Operands { float x[kAhead][128], w[2][FN * 4][128]; };
+#endif
+  struct Regs {
+    uint32_t iter;
+    uint32_t m0, n0, split, steps;              // steps: of the part
+    // the next slot to be brought: its first step, its place, its bytes of the tile's first rows and of the scales that this wave brings, and from a step's to the next's
+    uint32_t at_step, at_slot, wave_lds;
+    const uint8_t *x, *w, *scales;
+    size_t scale_step;
+    uint32_t here;                              // the slot that is read
+    uint32_t ox[X::kEach], ow[W::kEach], os;
+    uint32_t back;                              // from a piece of a second step to the one in its place in a slot that has one step only
+    Operands op;
+    hcnn_float4 acc[FM][FN];
+  };
+  static constexpr bool wave_sync(int ph) { return ph == 1 || ph == 3 || (ph == 0 && F == kMx4); }
+  HCNN_HD static uint32_t loop_count(const MxArgs& a) { return (a.part + 1) / 2; }
+  static size_t grid(const GemmArgs& g) { return (size_t)((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN) * g.splits; }
+  // Tiles go round the eight dies as those of Gemm do
+  HCNN_HD static void begin(const MxArgs& a, unsigned bid, int tid, uint32_t* lds, Regs& r) {
+    const uint32_t tm = (a.g.M + BM - 1) / BM, tn = (a.g.N + BN - 1) / BN, all = tm * tn * a.g.splits;
+    const uint32_t die = bid % 8, each = all / 8, rest = all % 8;
+    uint32_t at = die * each + (die < rest ? die : rest) + bid / 8;
+    r.split = at / (tm * tn);
+    at -= r.split * (tm * tn);
+    constexpr uint32_t kBand = 4;
+    const uint32_t band = at / (kBand * tn), high = tm - band * kBand < kBand ? tm - band * kBand : kBand;
+    at -= band * kBand * tn;
+    r.m0 = (band * kBand + at % high) * BM;
+    r.n0 = at / high * BN;
+    const uint32_t step0 = r.split * a.part;
+    r.steps = step0 >= a.steps ? 0 : a.steps - step0 < a.part ? a.steps - step0 : a.part;
+    r.x = a.x + r.m0 * a.x_bytes + (size_t)step0 * (F == kMx8 ? 128 : 64);
+    r.w = a.w + r.n0 * a.w_bytes + (size_t)step0 * 64;
+    r.at_step = r.at_slot = r.here = 0;
+    r.wave_lds = lds_start(lds) + wave_uniform((uint32_t)tid / 64) * 1024;
+#pragma unroll
+    for (int i = 0; i < X::kEach; ++i) r.ox[i] = X::offset(a.x_bytes, a.g.M, r.m0, tid, i);
+#pragma unroll
+    for (int i = 0; i < W::kEach; ++i) r.ow[i] = W::offset(a.w_bytes, a.g.N, r.n0, tid, i);
+    r.back = kSteps == 2 && X::piece_of(tid) >= 4 ? 64 : 0;
+    // scales: a wave's 64 words are 64 x 4 of the bytes [blocks][BM] and [blocks][BN]; beyond the rows, the last word that is there
+    {
+      const uint32_t word = (uint32_t)tid * 4, of_w = word >= 4 * BM, in = of_w ? word - 4 * BM : word, rows = of_w ? BN : BM;
+      const uint32_t block = in / rows, row = (of_w ? r.n0 : r.m0) + in % rows;
+      const size_t pitch = wave_uniform(of_w) ? a.w_pitch : a.x_pitch;
+      r.scales = (wave_uniform(of_w) ? a.w_scales : a.x_scales) + (size_t)step0 * 4 * pitch;
+      r.scale_step = 4 * pitch;
+      r.os = (uint32_t)(block * pitch + (row < pitch ? row : pitch - 4));
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int j = 0; j < FN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.acc[i][j][e] = 0.0f;
+    for (int s = 0; s < kSlots; ++s) {
+#pragma unroll
+      for (int d = 0; d < kLoads; ++d) bring(d, tid, lds, r);
+      brought(r);
+    }
+    direct_all_but<(kSlots - 1) * kLoads>((uint32_t)(kSlots - 1) * kSteps < r.steps);
+  }
+  HCNN_HD static void begin_next(const MxArgs&, unsigned, int tid, uint32_t* lds, Regs& r) {
+    const char* slot = reinterpret_cast<const char*>(lds);
+    read_w(slot, 0, 0, tid, r);
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) read_x(slot, 0, 0, q, tid, r);
+  }
+  // Load d of the thread's for the next slot, if there is one
+  HCNN_HD static void bring(int d, int tid, uint32_t* lds, const Regs& r) {
+    char* base = reinterpret_cast<char*>(lds);
+    const uint32_t back = kSteps == 2 && r.at_step + 1 == r.steps ? r.back : 0;
+    if (d < X::kEach) {
+      load_to_lds<16>(r.x, r.ox[d] - back, r.wave_lds + r.at_slot + d * kThreads * 16, base, tid & 63, r.at_step, r.steps);
+    } else if (d < X::kEach + W::kEach) {
+      const int i = d - X::kEach;
+      load_to_lds<16>(r.w, r.ow[i] - back, r.wave_lds + r.at_slot + X::kLdsBytes + i * kThreads * 16, base, tid & 63, r.at_step, r.steps);
+    } else {
+      const int s = d - X::kEach - W::kEach;
+      const uint32_t wave_scales = r.wave_lds - wave_uniform((uint32_t)tid / 64) * 768;
+      load_to_lds<4>(r.scales + (s && r.at_step + 1 < r.steps ? r.scale_step : 0), r.os, wave_scales + r.at_slot + kScales + s * kScaleBytes, base, tid & 63, r.at_step, r.steps);
+    }
+  }
+  HCNN_HD static void brought(Regs& r) {
+    r.at_step += kSteps;
+    r.at_slot = r.at_slot == (kSlots - 1) * kSlot ? 0 : r.at_slot + kSlot;
+    r.x += kSteps * (F == kMx8 ? 128 : 64);
+    r.w += kSteps * 64;
+    r.scales += kSteps * r.scale_step;
+  }
+  HCNN_HD static uint32_t x_row(int tid, int q) { return (uint32_t)tid / 64 / WN * (FM * 16) + q / 4 * 64 + tid % 16 * 4 + q % 4; }
+  HCNN_HD static uint32_t w_rows(int tid) { return (uint32_t)tid / 64 % WN * 64; }
+  // Operand q of x, and all of w's, of step s of a slot, for step `to` of a round
+#if defined(__HIP_DEVICE_COMPILE__)
+  __device__ __forceinline__ static hcnn_word4 word4(const char* p) { return *reinterpret_cast<const hcnn_word4*>(p); }
+  __device__ __forceinline__ static void read_x(const char* slot, int s, int, int q, int tid, Regs& r) {
+    const uint32_t g = tid % 64 / 16, row = x_row(tid, q);
+    MxFrag<F>& to = r.op.x[q % kAhead];
+    to.v[0] = word4(slot + X::place(row, F == kMx8 ? g : s * 4 + g));
+    if constexpr (F == kMx8) to.v[1] = word4(slot + X::place(row, 4 + g));
+  }
+  __device__ __forceinline__ static void read_w(const char* slot, int s, int to, int tid, Regs& r) {
+    const uint32_t g = tid % 64 / 16, i = tid % 16;
+    const char* scales = slot + kScales + s * kScaleBytes;
+#pragma unroll
+    for (int j = 0; j < FN; ++j) r.op.w[to][j].v[0] = word4(slot + X::kLdsBytes + W::place(w_rows(tid) + i * 4 + j, F == kMx8 ? g : s * 4 + g));
+    r.op.sw[to] = *reinterpret_cast<const uint32_t*>(scales + 4 * BM + g * BN + w_rows(tid) + i * 4);
+#pragma unroll
+    for (int c = 0; c < FM / 4; ++c) r.op.sx[to][c] = *reinterpret_cast<const uint32_t*>(scales + g * BM + x_row(tid, c * 4));
+  }
+  template <int Q>
+  __device__ __forceinline__ static void products(int s, Regs& r) {
+    each_of(std::make_integer_sequence<int, FN>{}, [&](auto j) {
+      mx_mma<F, kSplit, j.value, Q % 4>(r.acc[Q][j.value], r.op.w[s][j.value], r.op.x[Q % kAhead], r.op.sw[s], r.op.sx[s][Q / 4]);
+    });
+  }
+#else
+  // (the checker takes the numbers with their scales)
+  template <int G>
+  HCNN_HD static float number(const char* line, uint32_t k, uint8_t byte) {
+    const uint8_t b = static_cast<uint8_t>(line[G == kMx8 ? k : k / 2]);
+    return mx_value<G>(G == kMx8 ? b : b >> (k % 2 * 4) & 15) * (byte == 255 ? std::numeric_limits<float>::quiet_NaN() : mx_scale(byte));
+  }
+  HCNN_HD static void read_x(const char* slot, int s, int, int q, int tid, Regs& r) {
+    const uint32_t row = x_row(tid, q);
+    for (uint32_t k = 0; k < 128; ++k) {
+      const uint32_t byte = F == kMx8 ? k : s * 64 + k / 2;
+      const char* piece = slot + X::place(row, byte / 16);
+      r.op.x[q % kAhead][k] = number<F>(piece + byte % 16 - (F == kMx8 ? k : k / 2), k, (uint8_t)slot[kScales + s * kScaleBytes + k / 32 * BM + row]);
+    }
+  }
+  HCNN_HD static void read_w(const char* slot, int s, int to, int tid, Regs& r) {
+    for (uint32_t j = 0; j < FN; ++j)
+      for (uint32_t e = 0; e < 4; ++e) {
+        const uint32_t row = w_rows(tid) + (4 * (tid % 64 / 16) + e) * 4 + j;
+        for (uint32_t k = 0; k < 128; ++k) {
+          const uint32_t byte = (F == kMx8 ? 0 : s * 64) + k / 2;
+          const char* piece = slot + X::kLdsBytes + W::place(row, byte / 16);
+          r.op.w[to][j * 4 + e][k] = number<kMx4>(piece + byte % 16 - k / 2, k, (uint8_t)slot[kScales + s * kScaleBytes + 4 * BM + k / 32 * BN + row]);
+        }
+      }
+  }
+  template <int Q>
+  HCNN_HD static void products(int s, Regs& r) {
+    for (uint32_t j = 0; j < FN; ++j)
+      for (uint32_t e = 0; e < 4; ++e)
+        for (uint32_t k = 0; k < 128; ++k) r.acc[Q][j][e] += r.op.x[Q % kAhead][k] * r.op.w[s][j * 4 + e][k];
+  }
+#endif
+  template <int PH>
+  HCNN_HD static void phase(const MxArgs& a, unsigned, int tid, uint32_t* lds, Regs& r) {
+    if constexpr (PH < 4) {
+      constexpr int S = PH / 2;                                        // step of the round
+      const uint32_t step = r.iter * 2 + S;
+      if (step >= r.steps) return;                                     // (the same for all threads of the workgroup)
+      constexpr bool kLast = kSteps == 1 || S == 1;                    // step of the slot
+      constexpr int kHere = kSteps == 2 ? S : 0, kNext = kSteps == 2 ? 1 - S : 0;
+      const char* base = reinterpret_cast<const char*>(lds);
+      if constexpr (PH % 2 == 0) {
+        each_of(std::make_integer_sequence<int, FM - kAhead>{}, [&](auto q) {
+          products<q.value>(S, r);
+          read_x(base + r.here, kHere, S, q.value + kAhead, tid, r);
+          sched_fence();
+        });
+        // the next slot has arrived (the barrier behind this makes it so for all waves); the one behind it may still be on its way
+        if constexpr (kLast && kSlots == 2) direct_done();
+        if constexpr (kLast && kSlots == 3) direct_all_but<kLoads>(step + 2 < r.steps);
+      } else {
+        // the step's last products, the next one's first operands (behind the last step: of nothing, and not used), and from here on nobody reads this slot
+        if (kLast) r.here = r.here == (kSlots - 1) * kSlot ? 0 : r.here + kSlot;
+        const char* next = base + r.here;
+        read_w(next, kNext, 1 - S, tid, r);
+        each_of(std::make_integer_sequence<int, kAhead>{}, [&](auto i) {
+          products<FM - kAhead + i.value>(S, r);
+          read_x(next, kNext, 1 - S, i.value, tid, r);
+          if constexpr (kLast) {
+            constexpr int kGroup = (kLoads + kAhead - 1) / kAhead;
+#pragma unroll
+            for (int d = 0; d < kGroup; ++d)
+              if (i.value * kGroup + d < kLoads) bring(i.value * kGroup + d, tid, lds, r);
+          }
+          sched_fence();
+        });
+        if (kLast) brought(r);
+      }
+    } else {
+      const uint32_t g = tid % 64 / 16, n = r.n0 + w_rows(tid) + 16 * g;
+      if (n >= a.g.N) return;
+      const uint32_t left = a.g.N - n;
+      float bias[16] = {};
+      if (EPI == kEpiOut && a.g.bias) load_row(static_cast<const T*>(a.g.bias) + n, left, bias);
+#pragma unroll
+      for (int q0 = 0; q0 < FM; q0 += 2) {
+        uint32_t m[2];
+        float v[2][16];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          m[q] = r.m0 + x_row(tid, q0 + q);
+          if (m[q] >= a.g.M) m[q] = ~0u;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) v[q][e] = r.acc[q0 + q][e % 4][e / 4];
+        }
+        if constexpr (EPI == kEpiOut) finish<T>(a.g, m, n, bias, v);
+        else {
+          const uint32_t quads = (left + 3) / 4 * 4;                   // (rows of sums have room for whole quads)
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+            if (m[q] != ~0u) store_row(a.g.sums + ((size_t)r.split * a.g.M + m[q]) * a.g.ld_sums + n, quads, v[q]);
+        }
       }
     }
   }

@@ -146,6 +146,36 @@ struct MxCall {
   const void *bias, *residual; size_t ld_residual;
   void* y; size_t ldy;
 };
+// Tile (0: the simple form) and parts of k
+struct MxShape { uint32_t tile, splits; };
+inline MxShape mx_shape(const hcnn_plain* h, const MxCall& c) {
+  // offsets within a tile and a step in 32 bits
+  const bool fits = 256 * mx_row_bytes(c.format, c.K) < ((size_t)1 << 32) && 4 * std::max(c.x_pitch, c.w_pitch) < ((size_t)1 << 32);
+  if (c.K == 0 || !fits || c.M <= 16 || c.N <= 16) return MxShape{0, 1};
+#ifdef HCNN_HOSTEMU
+  if (emu_tile >= 0) return MxShape{emu_tile == kTile256 ? 256u : emu_tile == kTile128 ? 128u : 0u, emu_tile == kTile256 || emu_tile == kTile128 ? emu_parts : 1};
+#endif
+  if (blocks(c.M, 256) * blocks(c.N, 256) >= h->compute_units) return MxShape{256, 1};
+  if (blocks(c.M, 128) * blocks(c.N, 128) >= h->compute_units) return MxShape{128, 1};
+  return MxShape{0, 1};
+}
+template <class T, int F, int BM, int BN, int WM, int WN>
+int mx_tile(hcnn_plain* h, MxArgs& a) {
+  typedef MxTile<T, F, BM, BN, WM, WN, kEpiOut> One;
+  typedef MxTile<T, F, BM, BN, WM, WN, kEpiSums> Parts;
+  const size_t grid = One::grid(a.g);
+  if (grid > most_workgroups(One::kThreads)) return HCNN_ERR_ARG;
+#ifdef HCNN_HOSTEMU
+  emu_taken |= (uint64_t)1 << (a.g.splits == 1 ? 0 : 1) << (BM == 256 ? 0 : 2) << (F == kMx4 ? 0 : 4);
+#endif
+  if (a.g.splits == 1) return launch<One>(h->stream, grid, One::kLdsBytes, a);
+  a.g.ld_sums = up(a.g.N, 8);
+  const int e = reserve(h, (size_t)a.g.splits * a.g.M * a.g.ld_sums * 4);
+  if (e) return e;
+  a.g.sums = at<float>(h, 0);
+  const int f = launch<Parts>(h->stream, grid, Parts::kLdsBytes, a);
+  return f ? f : launch<GemmJoin<T, 1>>(h->stream, GemmJoin<T, 1>::grid(a.g), 0, a.g);
+}
 template <class T, int F>
 int linear_mx_of(hcnn_plain* h, const MxCall& c) {
   MxArgs a{};
@@ -161,6 +191,12 @@ int linear_mx_of(hcnn_plain* h, const MxCall& c) {
     for (a.first = 0; a.first < grid && !e; a.first += most) e = launch<S>(h->stream, std::min(most, grid - a.first), S::kLdsBytes, a);
     return e;
   };
+  const MxShape s = mx_shape(h, c);
+  if (s.tile) {
+    a.part = (uint32_t)up(blocks(a.steps, s.splits), 2);
+    a.g.splits = (uint32_t)blocks(a.steps, a.part);
+    return s.tile == 256 ? mx_tile<T, F, 256, 256, 2, 4>(h, a) : mx_tile<T, F, 128, 128, 2, 2>(h, a);
+  }
   if (c.M <= 16) return c.N <= 16 * (size_t)h->compute_units ? strip(MxStrip<T, F, 1, 1>{}) : strip(MxStrip<T, F, 1, 4>{});
   if (c.N <= 16) return strip(MxStrip<T, F, 4, 1>{});
   return strip(MxStrip<T, F, 4, 4>{});

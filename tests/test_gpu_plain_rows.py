@@ -117,7 +117,8 @@ def test_what_is_not_finite(b):
 # ---------------------------------------------------------------- the product
 LINEAR_LARGE = [("bf16", "mx8", 1, 4096, 4096, "silu", True, True), ("f16", "mx4", 3, 1000, 16400, "none", True, False), ("f32", "mx8", 16, 2000, 300, "none", False, False),
                 ("bf16", "mx4", 517, 1031, 777, "gelu", True, True), ("f16", "mx8", 300, 640, 520, "relu", True, True), ("f32", "mx4", 1000, 25, 5, "square", False, False),
-                ("bf16", "mx8", 1100, 300, 1200, "silu", True, False), ("f32", "mx8", 257, 1024, 258, "gelu", True, True), ("bf16", "mx4", 600, 4000, 40, "none", True, False)]
+                ("bf16", "mx8", 1100, 300, 1200, "silu", True, False), ("f16", "mx4", 2300, 640, 2180, "square", True, True), ("bf16", "mx8", 4100, 1300, 4360, "gelu", True, True),
+                ("bf16", "mx4", 4100, 1300, 4360, "none", False, False), ("f32", "mx8", 4000, 140, 4100, "none", True, False), ("f16", "mx8", 4096, 100, 4096, "relu", False, False), ("f32", "mx8", 257, 1024, 258, "gelu", True, True), ("bf16", "mx4", 600, 4000, 40, "none", True, False)]
 
 
 @pytest.mark.parametrize("case", rc.LINEAR + LINEAR_LARGE, ids=str)

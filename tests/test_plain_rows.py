@@ -371,3 +371,25 @@ def test_refusals_of_the_library(b):
     assert lib.hcnn_linear_mx(h, 0, 8, 0, 1, 4, 4, p, p, 64, p, p + 8, 64, None, None, 0, p, 4) == align
     assert lib.hcnn_linear_mx(h, 0, 8, 0, 1, 4, 65, p, p, 64, p, p, 64, None, None, 0, p, 65) == bad
     assert lib.hcnn_linear_mx(h, 0, 8, 0, 1, 4, 4, None, p, 64, p, p, 64, None, None, 0, p, 4) == null
+
+
+# ---------------------------------------------------------------- the product's shapes
+@pytest.mark.parametrize("form", ["mx4", "mx8"])
+@pytest.mark.parametrize("tile,size", [(0, (300, 300, 270)), (0, (257, 130, 30)), (1, (140, 600, 150)), (1, (129, 1200, 129)), (1, (40, 120, 200))])
+@pytest.mark.parametrize("parts", [1, 3])
+def test_tiles_of_the_product(b, form, tile, size, parts):
+    """every tile, one slot and several, a slot that is not whole, parts of k"""
+    lib = emu.lib()
+    lib.hcnn_emu_shape.argtypes, lib.hcnn_emu_shape.restype = [ctypes.c_int, ctypes.c_uint32, ctypes.c_int], None
+    lib.hcnn_emu_taken.argtypes, lib.hcnn_emu_taken.restype = [ctypes.POINTER(ctypes.c_uint64)] * 2, None
+    lib.hcnn_emu_shape(tile, parts, 0)
+    try:
+        rc.check_linear(b, "bf16", form, *size, "relu", bias=True, residual=True)
+        rc.check_linear(b, "f32", form, *size, "none")
+        bits, copied = ctypes.c_uint64(), ctypes.c_uint64()
+        lib.hcnn_emu_taken(ctypes.byref(bits), ctypes.byref(copied))
+        steps = -(-size[1] // 128)
+        each = -(-(-(-steps // parts)) // 2) * 2
+        assert bits.value == 1 << (0 if -(-steps // each) == 1 else 1) << (0 if tile == 0 else 2) << (0 if form == "mx4" else 4)
+    finally:
+        lib.hcnn_emu_shape(-1, 1, 0)
