@@ -199,22 +199,22 @@ struct MxStrip {
 // the registers, in slots: of four-bit x two steps (128 bytes of every row, two slots), of eight-bit x one step (128 bytes of x's rows, 64 of w's; three slots), with
 // their scales.  A lane's operands of x go through a ring of kAhead places, read that many products ahead; w's of a step have two places.  The last kAhead
 // of a slot's operands are in registers when the barrier comes: behind it the slot is filled anew while their products run, and the next slot's first are read.
-//   LDS: lines of 128 bytes, piece p of line l at p ^ turn(l).  The 16 rows of one read lie four apart: turn takes its eight values in them, so that they spread
-//   evenly over the banks.
+//   LDS: lines of 256 bytes (all 64 banks), 16 pieces of 16 bytes, piece p of line l at p ^ turn(l).  The 16 rows of one read lie four apart: turn takes 16 values in
+// them, so that they spread evenly over the banks.  (With lines of 128 bytes and eight values, every read took twice as long: 8192 x 16384 -> 16384 950 us.)
 template <int BYTES, int ROWS, int THREADS>
 struct MxTileRows {
-  static constexpr uint32_t kPieces = BYTES / 16, kLineRows = 128 / BYTES;          // of a row; rows of a line
+  static constexpr uint32_t kPieces = BYTES / 16, kLineRows = 256 / BYTES;          // of a row; rows of a line
   static constexpr int kEach = ROWS * BYTES / 16 / THREADS;
   static constexpr uint32_t kLdsBytes = ROWS * BYTES;
   static_assert(ROWS * BYTES % (16 * THREADS) == 0, "every thread has the same number of pieces");
-  HCNN_HD static uint32_t turn(uint32_t line) { return line / (4 / kLineRows) & 7; }
+  HCNN_HD static uint32_t turn(uint32_t line) { return line / (4 / kLineRows) & 15; }
   HCNN_HD static uint32_t place(uint32_t row, uint32_t piece) {
     const uint32_t line = row / kLineRows, p = row % kLineRows * kPieces + piece;
-    return line * 128 + ((p ^ turn(line)) << 4);
+    return line * 256 + ((p ^ turn(line)) << 4);
   }
   // (row, piece) that lies at LDS piece c
   HCNN_HD static void at(uint32_t c, uint32_t* row, uint32_t* piece) {
-    const uint32_t line = c / 8, p = (c % 8) ^ turn(line);
+    const uint32_t line = c / 16, p = (c % 16) ^ turn(line);
     *row = line * kLineRows + p / kPieces;
     *piece = p % kPieces;
   }
@@ -233,23 +233,18 @@ struct MxTileRows {
     return piece;
   }
 };
-// BYTES (16 or 4) of every lane of a wave to LDS, side by side, where step < steps.  (The lanes are switched off, so that no branch stands
-// between the products that such loads are spread over: with one, they were gathered behind it.  All lanes of the workgroup's waves are at work here.)
+// BYTES (16 or 4) of every lane of a wave to LDS, side by side
 template <int BYTES>
-HCNN_HD void load_to_lds(const uint8_t* base, uint32_t off, uint32_t at, [[maybe_unused]] char* lds, [[maybe_unused]] int lane, uint32_t step, uint32_t steps) {
+HCNN_HD void load_to_lds(const uint8_t* base, uint32_t off, uint32_t at, [[maybe_unused]] char* lds, [[maybe_unused]] int lane) {
 #if defined(__HIP_DEVICE_COMPILE__)
   static_assert(BYTES == 16 || BYTES == 4, "what the instruction takes");
 #pragma clang diagnostic push
 #pragma clang diagnostic ignored "-Winline-asm"
-  if constexpr (BYTES == 16)
-    asm volatile("s_mov_b32 m0, %0\n\ts_cmp_lt_u32 %3, %4\n\ts_cselect_b64 exec, -1, 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b64 exec, -1" ::"s"(at), "v"(off),
-                 "s"(base), "s"(wave_uniform(step)), "s"(wave_uniform(steps)) : "memory", "m0", "scc");
-  else
-    asm volatile("s_mov_b32 m0, %0\n\ts_cmp_lt_u32 %3, %4\n\ts_cselect_b64 exec, -1, 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b64 exec, -1" ::"s"(at), "v"(off),
-                 "s"(base), "s"(wave_uniform(step)), "s"(wave_uniform(steps)) : "memory", "m0", "scc");
+  if constexpr (BYTES == 16) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(base) : "memory", "m0");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(at), "v"(off), "s"(base) : "memory", "m0");
 #pragma clang diagnostic pop
 #else
-  if (step < steps) __builtin_memcpy(lds + at + lane * BYTES, base + off, BYTES);
+  __builtin_memcpy(lds + at + lane * BYTES, base + off, BYTES);
 #endif
 }
 // Byte of LDS at which the workgroup's memory begins
@@ -260,14 +255,11 @@ HCNN_HD uint32_t lds_start([[maybe_unused]] const uint32_t* lds) {
   return 0;
 #endif
 }
-// What is on its way to LDS past the registers has arrived, all but the last N loads where `behind` is not 0.  (The branch is within the instructions: the compiler
-// moves products behind a branch of its own.)
+// What is on its way to LDS past the registers has arrived, all but the last N loads
 template <int N>
-HCNN_HD void direct_all_but([[maybe_unused]] uint32_t behind) {
+HCNN_HD void direct_all_but() {
 #if defined(__HIP_DEVICE_COMPILE__)
-  asm volatile(
-      "s_cmp_lg_u32 %0, 0\n\ts_cbranch_scc1 .Lhcnn_behind_%=\n\ts_waitcnt vmcnt(0)\n.Lhcnn_behind_%=:\n\ts_waitcnt vmcnt(%1)" ::"s"(wave_uniform(behind)), "n"(N)
-      : "memory", "scc");
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 #endif
 }
 
@@ -275,9 +267,10 @@ template <class T, int F, int BM, int BN, int WM, int WN, int EPI>
 struct MxTile {
   static constexpr int kThreads = WM * WN * 64;
   static constexpr int kLoopPhases = 4, kPhases = 5;                   // a round of the loop: two steps
-  static constexpr int kMinWavesPerSimd = 2;
   static constexpr int FM = BM / WM / 16, FN = BN / WN / 16;
-  static_assert(FM % 4 == 0 && FN == 4 && (BM + BN) / 64 == WM * WN, "waves take 64 columns; a wave brings 64 rows' scales");
+  static constexpr int kMinWavesPerSimd = FM * FN > 32 ? 1 : 2;
+  static constexpr int kScaleLoads = (BM + BN) / 64 / (WM * WN);       // of a wave for a step: 64 rows each
+  static_assert(FM % 4 == 0 && FN % 4 == 0 && kScaleLoads * 64 * WM * WN == BM + BN && 256 % BM == 0 && 256 % BN == 0, "whole groups of four products");
   static constexpr int kSteps = F == kMx4 ? 2 : 1, kSlots = F == kMx4 ? 2 : 3;       // steps of a slot
   static constexpr int kAhead = F == kMx4 ? 4 : 2;
   static constexpr bool kSplit = F == kMx8 && sizeof(T) == 4;
@@ -286,10 +279,10 @@ struct MxTile {
   static constexpr uint32_t kScaleBytes = 4 * (BM + BN);               // of a step: [x's blocks][BM], [w's blocks][BN]
   static constexpr uint32_t kScales = X::kLdsBytes + W::kLdsBytes, kSlot = kScales + kSteps * kScaleBytes;
   static constexpr size_t kLdsBytes = (size_t)kSlots * kSlot;
-  static constexpr int kLoads = X::kEach + W::kEach + kSteps;          // of a thread for a slot
+  static constexpr int kLoads = X::kEach + W::kEach + kSteps * kScaleLoads;          // of a thread for a slot
   static_assert(kLdsBytes <= 160 * 1024, "the slots fit LDS");
 #if defined(__HIP_DEVICE_COMPILE__)
-  struct Operands { MxFrag<F> x[kAhead]; MxFrag<kMx4> w[2][FN]; uint32_t sx[2][FM / 4], sw[2]; };
+  struct Operands { MxFrag<F> x[kAhead]; MxFrag<kMx4> w[2][FN]; uint32_t sx[2][FM / 4], sw[2][FN / 4]; };
 #else
   struct Operands { float x[kAhead][128], w[2][FN * 4][128]; };
 #endif
@@ -297,11 +290,12 @@ struct MxTile {
     uint32_t iter;
     uint32_t m0, n0, split, steps;              // steps: of the part
     // the next slot to be brought: its first step, its place, its bytes of the tile's first rows and of the scales that this wave brings, and from a step's to the next's
+    // (behind the last slot: the last one again, to a place that nobody reads)
     uint32_t at_step, at_slot, wave_lds;
-    const uint8_t *x, *w, *scales;
-    size_t scale_step;
+    const uint8_t *x, *w, *scales[kScaleLoads];
+    size_t scale_step[kScaleLoads];
     uint32_t here;                              // the slot that is read
-    uint32_t ox[X::kEach], ow[W::kEach], os;
+    uint32_t ox[X::kEach], ow[W::kEach], os[kScaleLoads];
     uint32_t back;                              // from a piece of a second step to the one in its place in a slot that has one step only
     Operands op;
     hcnn_float4 acc[FM][FN];
@@ -333,13 +327,14 @@ struct MxTile {
     for (int i = 0; i < W::kEach; ++i) r.ow[i] = W::offset(a.w_bytes, a.g.N, r.n0, tid, i);
     r.back = kSteps == 2 && X::piece_of(tid) >= 4 ? 64 : 0;
     // scales: a wave's 64 words are 64 x 4 of the bytes [blocks][BM] and [blocks][BN]; beyond the rows, the last word that is there
-    {
-      const uint32_t word = (uint32_t)tid * 4, of_w = word >= 4 * BM, in = of_w ? word - 4 * BM : word, rows = of_w ? BN : BM;
-      const uint32_t block = in / rows, row = (of_w ? r.n0 : r.m0) + in % rows;
-      const size_t pitch = wave_uniform(of_w) ? a.w_pitch : a.x_pitch;
-      r.scales = (wave_uniform(of_w) ? a.w_scales : a.x_scales) + (size_t)step0 * 4 * pitch;
-      r.scale_step = 4 * pitch;
-      r.os = (uint32_t)(block * pitch + (row < pitch ? row : pitch - 4));
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i) {
+      const uint32_t word = (uint32_t)(tid + i * kThreads) * 4, of_w = wave_uniform(word >= 4 * BM), in = of_w ? word - 4 * BM : word;
+      const uint32_t block = of_w ? in / BN : in / BM, row = of_w ? r.n0 + in % BN : r.m0 + in % BM;
+      const size_t pitch = of_w ? a.w_pitch : a.x_pitch;
+      r.scales[i] = (of_w ? a.w_scales : a.x_scales) + (size_t)step0 * 4 * pitch;
+      r.scale_step[i] = 4 * pitch;
+      r.os[i] = (uint32_t)(block * pitch + (row < pitch ? row : pitch - 4));
     }
 #pragma unroll
     for (int i = 0; i < FM; ++i)
@@ -352,7 +347,7 @@ struct MxTile {
       for (int d = 0; d < kLoads; ++d) bring(d, tid, lds, r);
       brought(r);
     }
-    direct_all_but<(kSlots - 1) * kLoads>((uint32_t)(kSlots - 1) * kSteps < r.steps);
+    direct_all_but<(kSlots - 1) * kLoads>();
   }
   HCNN_HD static void begin_next(const MxArgs&, unsigned, int tid, uint32_t* lds, Regs& r) {
     const char* slot = reinterpret_cast<const char*>(lds);
@@ -360,30 +355,32 @@ struct MxTile {
 #pragma unroll
     for (int q = 0; q < kAhead; ++q) read_x(slot, 0, 0, q, tid, r);
   }
-  // Load d of the thread's for the next slot, if there is one
+  // Load d of the thread's for the next slot
   HCNN_HD static void bring(int d, int tid, uint32_t* lds, const Regs& r) {
     char* base = reinterpret_cast<char*>(lds);
     const uint32_t back = kSteps == 2 && r.at_step + 1 == r.steps ? r.back : 0;
     if (d < X::kEach) {
-      load_to_lds<16>(r.x, r.ox[d] - back, r.wave_lds + r.at_slot + d * kThreads * 16, base, tid & 63, r.at_step, r.steps);
+      load_to_lds<16>(r.x, r.ox[d] - back, r.wave_lds + r.at_slot + d * kThreads * 16, base, tid & 63);
     } else if (d < X::kEach + W::kEach) {
       const int i = d - X::kEach;
-      load_to_lds<16>(r.w, r.ow[i] - back, r.wave_lds + r.at_slot + X::kLdsBytes + i * kThreads * 16, base, tid & 63, r.at_step, r.steps);
+      load_to_lds<16>(r.w, r.ow[i] - back, r.wave_lds + r.at_slot + X::kLdsBytes + i * kThreads * 16, base, tid & 63);
     } else {
-      const int s = d - X::kEach - W::kEach;
+      const int s = (d - X::kEach - W::kEach) / kScaleLoads, i = (d - X::kEach - W::kEach) % kScaleLoads;
       const uint32_t wave_scales = r.wave_lds - wave_uniform((uint32_t)tid / 64) * 768;
-      load_to_lds<4>(r.scales + (s && r.at_step + 1 < r.steps ? r.scale_step : 0), r.os, wave_scales + r.at_slot + kScales + s * kScaleBytes, base, tid & 63, r.at_step, r.steps);
+      load_to_lds<4>(r.scales[i] + (s && r.at_step + 1 < r.steps ? r.scale_step[i] : 0), r.os[i], wave_scales + r.at_slot + kScales + s * kScaleBytes + i * kThreads * 4, base, tid & 63);
     }
   }
   HCNN_HD static void brought(Regs& r) {
-    r.at_step += kSteps;
     r.at_slot = r.at_slot == (kSlots - 1) * kSlot ? 0 : r.at_slot + kSlot;
-    r.x += kSteps * (F == kMx8 ? 128 : 64);
-    r.w += kSteps * 64;
-    r.scales += kSteps * r.scale_step;
+    const uint32_t on = r.at_step + kSteps < r.steps ? kSteps : 0;
+    r.at_step += on;
+    r.x += on * (F == kMx8 ? 128 : 64);
+    r.w += on * 64;
+#pragma unroll
+    for (int i = 0; i < kScaleLoads; ++i) r.scales[i] += on ? kSteps * r.scale_step[i] : 0;
   }
   HCNN_HD static uint32_t x_row(int tid, int q) { return (uint32_t)tid / 64 / WN * (FM * 16) + q / 4 * 64 + tid % 16 * 4 + q % 4; }
-  HCNN_HD static uint32_t w_rows(int tid) { return (uint32_t)tid / 64 % WN * 64; }
+  HCNN_HD static uint32_t w_row(int tid, int j) { return (uint32_t)tid / 64 % WN * (FN * 16) + j / 4 * 64 + tid % 16 * 4 + j % 4; }
   // Operand q of x, and all of w's, of step s of a slot, for step `to` of a round
 #if defined(__HIP_DEVICE_COMPILE__)
   __device__ __forceinline__ static hcnn_word4 word4(const char* p) { return *reinterpret_cast<const hcnn_word4*>(p); }
@@ -394,18 +391,19 @@ struct MxTile {
     if constexpr (F == kMx8) to.v[1] = word4(slot + X::place(row, 4 + g));
   }
   __device__ __forceinline__ static void read_w(const char* slot, int s, int to, int tid, Regs& r) {
-    const uint32_t g = tid % 64 / 16, i = tid % 16;
+    const uint32_t g = tid % 64 / 16;
     const char* scales = slot + kScales + s * kScaleBytes;
 #pragma unroll
-    for (int j = 0; j < FN; ++j) r.op.w[to][j].v[0] = word4(slot + X::kLdsBytes + W::place(w_rows(tid) + i * 4 + j, F == kMx8 ? g : s * 4 + g));
-    r.op.sw[to] = *reinterpret_cast<const uint32_t*>(scales + 4 * BM + g * BN + w_rows(tid) + i * 4);
+    for (int j = 0; j < FN; ++j) r.op.w[to][j].v[0] = word4(slot + X::kLdsBytes + W::place(w_row(tid, j), F == kMx8 ? g : s * 4 + g));
+#pragma unroll
+    for (int c = 0; c < FN / 4; ++c) r.op.sw[to][c] = *reinterpret_cast<const uint32_t*>(scales + 4 * BM + g * BN + w_row(tid, c * 4));
 #pragma unroll
     for (int c = 0; c < FM / 4; ++c) r.op.sx[to][c] = *reinterpret_cast<const uint32_t*>(scales + g * BM + x_row(tid, c * 4));
   }
   template <int Q>
   __device__ __forceinline__ static void products(int s, Regs& r) {
     each_of(std::make_integer_sequence<int, FN>{}, [&](auto j) {
-      mx_mma<F, kSplit, j.value, Q % 4>(r.acc[Q][j.value], r.op.w[s][j.value], r.op.x[Q % kAhead], r.op.sw[s], r.op.sx[s][Q / 4]);
+      mx_mma<F, kSplit, j.value % 4, Q % 4>(r.acc[Q][j.value], r.op.w[s][j.value], r.op.x[Q % kAhead], r.op.sw[s][j.value / 4], r.op.sx[s][Q / 4]);
     });
   }
 #else
@@ -426,7 +424,7 @@ struct MxTile {
   HCNN_HD static void read_w(const char* slot, int s, int to, int tid, Regs& r) {
     for (uint32_t j = 0; j < FN; ++j)
       for (uint32_t e = 0; e < 4; ++e) {
-        const uint32_t row = w_rows(tid) + (4 * (tid % 64 / 16) + e) * 4 + j;
+        const uint32_t row = w_row((tid & ~63) + 4 * (tid % 64 / 16) + e, j);
         for (uint32_t k = 0; k < 128; ++k) {
           const uint32_t byte = (F == kMx8 ? 0 : s * 64) + k / 2;
           const char* piece = slot + X::kLdsBytes + W::place(row, byte / 16);
@@ -457,8 +455,7 @@ struct MxTile {
           sched_fence();
         });
         // the next slot has arrived (the barrier behind this makes it so for all waves); the one behind it may still be on its way
-        if constexpr (kLast && kSlots == 2) direct_done();
-        if constexpr (kLast && kSlots == 3) direct_all_but<kLoads>(step + 2 < r.steps);
+        if constexpr (kLast) direct_all_but<(kSlots - 2) * kLoads>();
       } else {
         // the step's last products, the next one's first operands (behind the last step: of nothing, and not used), and from here on nobody reads this slot
         if (kLast) r.here = r.here == (kSlots - 1) * kSlot ? 0 : r.here + kSlot;
@@ -478,30 +475,36 @@ struct MxTile {
         if (kLast) brought(r);
       }
     } else {
-      const uint32_t g = tid % 64 / 16, n = r.n0 + w_rows(tid) + 16 * g;
-      if (n >= a.g.N) return;
-      const uint32_t left = a.g.N - n;
-      float bias[16] = {};
-      if (EPI == kEpiOut && a.g.bias) load_row(static_cast<const T*>(a.g.bias) + n, left, bias);
+      direct_done();                                                   // (nothing may still be on its way to LDS when the workgroup ends)
+      // (the groups and rows as compile-time constants: a loop that the compiler does not unroll would keep the sums in memory)
+      each_of(std::make_integer_sequence<int, FN / 4>{}, [&](auto c) {
+        // 16 columns side by side: sums 4 e + j of the group's products j
+        constexpr int j0 = c.value * 4;
+        const uint32_t n = r.n0 + w_row(tid & ~63, j0) + 16 * (tid % 64 / 16);
+        if (n >= a.g.N) return;
+        const uint32_t left = a.g.N - n;
+        float bias[16] = {};
+        if (EPI == kEpiOut && a.g.bias) load_row(static_cast<const T*>(a.g.bias) + n, left, bias);
+        each_of(std::make_integer_sequence<int, FM / 2>{}, [&](auto p) {
+          constexpr int q0 = p.value * 2;
+          uint32_t m[2];
+          float v[2][16];
 #pragma unroll
-      for (int q0 = 0; q0 < FM; q0 += 2) {
-        uint32_t m[2];
-        float v[2][16];
+          for (int q = 0; q < 2; ++q) {
+            m[q] = r.m0 + x_row(tid, q0 + q);
+            if (m[q] >= a.g.M) m[q] = ~0u;
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          m[q] = r.m0 + x_row(tid, q0 + q);
-          if (m[q] >= a.g.M) m[q] = ~0u;
+            for (int e = 0; e < 16; ++e) v[q][e] = r.acc[q0 + q][j0 + e % 4][e / 4];
+          }
+          if constexpr (EPI == kEpiOut) finish<T>(a.g, m, n, bias, v);
+          else {
+            const uint32_t quads = (left + 3) / 4 * 4;                 // (rows of sums have room for whole quads)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) v[q][e] = r.acc[q0 + q][e % 4][e / 4];
-        }
-        if constexpr (EPI == kEpiOut) finish<T>(a.g, m, n, bias, v);
-        else {
-          const uint32_t quads = (left + 3) / 4 * 4;                   // (rows of sums have room for whole quads)
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-            if (m[q] != ~0u) store_row(a.g.sums + ((size_t)r.split * a.g.M + m[q]) * a.g.ld_sums + n, quads, v[q]);
-        }
-      }
+            for (int q = 0; q < 2; ++q)
+              if (m[q] != ~0u) store_row(a.g.sums + ((size_t)r.split * a.g.M + m[q]) * a.g.ld_sums + n, quads, v[q]);
+          }
+        });
+      });
     }
   }
 };
