@@ -437,7 +437,7 @@ struct NormRows {
 
 // Gradient from h as it is stored: with u = h / sqrt(mean of h^2 + eps), both sums of a row in one pass,
 //   dx = (w dy - u mean(w dy u)) / sqrt(...) + dh,   dw = sum over rows of dy u.
-// A workgroup takes rows_each rows, kLines at a time; the columns' sums stay in its threads' registers and leave once, in 32 bits, for ColumnSum.
+// A workgroup takes rows_each rows, kLines at a time; the columns' sums stay in its threads' registers and leave once, in 32 bits, for QuadSums.
 struct NormGradArgs {
   const void *dy, *h, *weight, *dh;         // weight, dh may be null
   size_t ld_dy, ldh, ld_dh;
@@ -457,69 +457,113 @@ struct NormGrad {
   typedef RowSum<LANES, kThreads, 2> Sum;
   static constexpr size_t kSumBytes = 2 * Sum::kLdsBytes;                        // two, taken in turn: a barrier an iteration
   static constexpr size_t kLdsBytes = kSumBytes + (kLines > 1 ? (size_t)kLines * LANES * EL * 4 : 0);
+  // A row as it lies in memory (the next one is asked for before the sums of this one are known) and the weights, for all rows
+  struct Raw { T v[kHeld][W]; };
   struct Regs {
     uint32_t iter;
-    float dy[kHeld][W], h[kHeld][W], dw[kHeld][W];
+    Raw w, dy, h, dh;
+    float dyf[kHeld][W], hf[kHeld][W], dhf[kHeld][W], dw[kHeld][W];
     double sum[2];
   };
   static constexpr bool wave_sync(int ph) { return ph == 1 || (ph == 0 && LANES <= 64); }
   HCNN_HD static uint32_t loop_count(const NormGradArgs& a) { return a.rows_each / kLines; }
-  HCNN_HD static void begin(const NormGradArgs&, unsigned, int, uint32_t*, Regs& r) {
+  HCNN_HD static size_t row_of(const NormGradArgs& a, unsigned bid, int tid, uint32_t iter) { return (size_t)bid * a.rows_each + (size_t)iter * kLines + tid / LANES; }
+  HCNN_HD static void load(const T* row, uint32_t n, uint32_t lane, Raw& r) {
 #pragma unroll
-    for (int i = 0; i < kHeld; ++i)
+    for (int i = 0; i < kHeld; ++i) {
+      const uint32_t c = (i * LANES + lane) * W;
+      if (c + W <= n) {
+        const U4 v = ld16(reinterpret_cast<const char*>(row + c));
+        __builtin_memcpy(r.v[i], &v, 16);
+      } else {
 #pragma unroll
-      for (int e = 0; e < W; ++e) r.dw[i][e] = 0.0f;
+        for (uint32_t e = 0; e < W; ++e) {
+          r.v[i][e] = Num<T>::narrow(0.0f);
+          if (c + e < n) r.v[i][e] = row[c + e];
+        }
+      }
+    }
   }
-  HCNN_HD static void load(const NormGradArgs& a, size_t row, uint32_t c, float (&dy)[W], float (&h)[W]) {
-    load_some(static_cast<const T*>(a.dy) + row * a.ld_dy, c, a.n, dy);
-    load_some(static_cast<const T*>(a.h) + row * a.ldh, c, a.n, h);
+  HCNN_HD static void ask(const NormGradArgs& a, size_t row, uint32_t lane, Regs& r) {
+    if (row >= a.rows) return;
+    load(static_cast<const T*>(a.dy) + row * a.ld_dy, a.n, lane, r.dy);
+    load(static_cast<const T*>(a.h) + row * a.ldh, a.n, lane, r.h);
+    if (a.dh) load(static_cast<const T*>(a.dh) + row * a.ld_dh, a.n, lane, r.dh);
   }
-  HCNN_HD static void weights(const NormGradArgs& a, uint32_t c, float (&w)[W]) {
-    if (a.weight) load_some(static_cast<const T*>(a.weight), c, a.n, w);
-    else
+  HCNN_HD static void begin(const NormGradArgs& a, unsigned bid, int tid, uint32_t*, Regs& r) {
+    if constexpr (EL > 0) {
+      const uint32_t lane = (uint32_t)tid % LANES;
+      if (a.weight) load(static_cast<const T*>(a.weight), a.n, lane, r.w);
 #pragma unroll
-      for (int e = 0; e < W; ++e) w[e] = 1.0f;
+      for (int i = 0; i < kHeld; ++i)
+#pragma unroll
+        for (int e = 0; e < W; ++e) {
+          r.dw[i][e] = 0.0f;
+          if (!a.weight) r.w.v[i][e] = Num<T>::narrow(1.0f);
+        }
+      ask(a, row_of(a, bid, tid, 0), lane, r);
+    }
   }
-  HCNN_HD static void add(const NormGradArgs& a, uint32_t c, const float (&dy)[W], const float (&h)[W], double (&sum)[2]) {
-    float w[W];
-    weights(a, c, w);
+  HCNN_HD static void add(const float (&g)[W], const float (&h)[W], double (&sum)[2]) {
 #pragma unroll
     for (int e = 0; e < W; ++e) {
       sum[0] += (double)h[e] * h[e];
-      sum[1] += (double)(dy[e] * w[e]) * h[e];
+      sum[1] += (double)g[e] * h[e];
     }
   }
-  HCNN_HD static void give_dx(const NormGradArgs& a, size_t row, uint32_t c, const RowScale& s, float mean, const float (&dy)[W], const float (&h)[W], float (&u)[W]) {
-    if (c >= a.n) return;
-    float w[W], dx[W], d[W];
-    weights(a, c, w);
-    if (a.dh) load_row(static_cast<const T*>(a.dh) + row * a.ld_dh + c, a.n - c, d);
+  // g = weight dy, h: to dx and, in h's place, u
+  HCNN_HD static void finish_chunk(const RowScale& s, float mean, const float (&g)[W], float (&h)[W], float (&dx)[W]) {
 #pragma unroll
-    for (int e = 0; e < W; ++e) {
-      u[e] = h[e] * s.two * s.one;
-      dx[e] = (w[e] * dy[e] - u[e] * mean) * s.two * s.one;
-      if (a.dh) dx[e] += d[e];
+    for (int e = 0; e < W; ++e) h[e] *= s.one;
+    if (s.two != 1.0f) {
+#pragma unroll
+      for (int e = 0; e < W; ++e) h[e] *= s.two;
     }
-    store_row(static_cast<T*>(a.dx) + row * a.ld_dx + c, a.n - c, dx);
+#pragma unroll
+    for (int e = 0; e < W; ++e) dx[e] = (g[e] - h[e] * mean) * s.one;
+    if (s.two != 1.0f) {
+#pragma unroll
+      for (int e = 0; e < W; ++e) dx[e] *= s.two;
+    }
+  }
+  // rows of any length
+  HCNN_HD static void load_long(const NormGradArgs& a, size_t row, uint32_t c, float (&dy)[W], float (&h)[W]) {
+    load_some(static_cast<const T*>(a.dy) + row * a.ld_dy, c, a.n, dy);
+    load_some(static_cast<const T*>(a.h) + row * a.ldh, c, a.n, h);
+    if (a.weight) {
+      float w[W];
+      load_some(static_cast<const T*>(a.weight), c, a.n, w);
+#pragma unroll
+      for (int e = 0; e < W; ++e) dy[e] *= w[e];
+    }
   }
   template <int PH>
   HCNN_HD static void phase(const NormGradArgs& a, unsigned bid, int tid, uint32_t* lds_words, Regs& r) {
     double* lds = reinterpret_cast<double*>(reinterpret_cast<char*>(lds_words) + r.iter % 2 * Sum::kLdsBytes);
     const uint32_t lane = (uint32_t)tid % LANES, line = (uint32_t)tid / LANES;
-    const size_t row = (size_t)bid * a.rows_each + (size_t)r.iter * kLines + line;
+    const size_t row = row_of(a, bid, tid, r.iter);
     const bool here = row < a.rows;
     if constexpr (PH == 0) {
       r.sum[0] = r.sum[1] = 0.0;
       if (here) {
         if constexpr (EL > 0) {
 #pragma unroll
-          for (int i = 0; i < kHeld; ++i) load(a, row, (i * LANES + lane) * W, r.dy[i], r.h[i]);
+          for (int i = 0; i < kHeld; ++i) {
+            float g[W];
 #pragma unroll
-          for (int i = 0; i < kHeld; ++i) add(a, (i * LANES + lane) * W, r.dy[i], r.h[i], r.sum);
+            for (int e = 0; e < W; ++e) {
+              r.dyf[i][e] = Num<T>::widen(r.dy.v[i][e]);
+              r.hf[i][e] = Num<T>::widen(r.h.v[i][e]);
+              r.dhf[i][e] = a.dh ? Num<T>::widen(r.dh.v[i][e]) : 0.0f;
+              g[e] = r.dyf[i][e] * Num<T>::widen(r.w.v[i][e]);
+            }
+            add(g, r.hf[i], r.sum);
+          }
+          if (r.iter + 1 < loop_count(a)) ask(a, row + kLines, lane, r);
         } else {
           for (uint32_t c = lane * W; c < a.n; c += LANES * W) {
-            load(a, row, c, r.dy[0], r.h[0]);
-            add(a, c, r.dy[0], r.h[0], r.sum);
+            load_long(a, row, c, r.dyf[0], r.hf[0]);
+            add(r.dyf[0], r.hf[0], r.sum);
           }
         }
       }
@@ -532,19 +576,31 @@ struct NormGrad {
       if constexpr (EL > 0) {
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) {
-          float u[W];
           const uint32_t c = (i * LANES + lane) * W;
-          give_dx(a, row, c, s, mean, r.dy[i], r.h[i], u);
-          if (c < a.n)
+          if (c >= a.n) continue;
+          float g[W], dx[W];
 #pragma unroll
-            for (int e = 0; e < W; ++e) r.dw[i][e] += r.dy[i][e] * u[e];
+          for (int e = 0; e < W; ++e) g[e] = r.dyf[i][e] * Num<T>::widen(r.w.v[i][e]);
+          finish_chunk(s, mean, g, r.hf[i], dx);
+#pragma unroll
+          for (int e = 0; e < W; ++e) {
+            dx[e] += r.dhf[i][e];
+            r.dw[i][e] += r.dyf[i][e] * r.hf[i][e];
+          }
+          store_row(static_cast<T*>(a.dx) + row * a.ld_dx + c, a.n - c, dx);
         }
       } else {
         if (lane == 0 && a.inverse) a.inverse[row] = s.whole;
         for (uint32_t c = lane * W; c < a.n; c += LANES * W) {
-          float u[W];
-          load(a, row, c, r.dy[0], r.h[0]);
-          give_dx(a, row, c, s, mean, r.dy[0], r.h[0], u);
+          float dx[W], d[W];
+          load_long(a, row, c, r.dyf[0], r.hf[0]);
+          finish_chunk(s, mean, r.dyf[0], r.hf[0], dx);
+          if (a.dh) {
+            load_row(static_cast<const T*>(a.dh) + row * a.ld_dh + c, a.n - c, d);
+#pragma unroll
+            for (int e = 0; e < W; ++e) dx[e] += d[e];
+          }
+          store_row(static_cast<T*>(a.dx) + row * a.ld_dx + c, a.n - c, dx);
         }
       }
     } else if constexpr (EL > 0) {
@@ -556,10 +612,12 @@ struct NormGrad {
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) {
           const uint32_t c = (i * LANES + lane) * W;
+          if constexpr (kLines > 1) {
+            // (store_row is for memory, not for LDS)
 #pragma unroll
-          for (int e = 0; e < W; ++e) {
-            if (kLines > 1) lines[line * kCols + c + e] = r.dw[i][e];
-            else if (c + e < a.n) to[c + e] = r.dw[i][e];
+            for (int e = 0; e < W; ++e) lines[line * kCols + c + e] = r.dw[i][e];
+          } else if (c < a.n) {
+            store_row(to + c, (a.n - c + 3) / 4 * 4, r.dw[i]);                          // (rows of parts have room for whole quads)
           }
         }
       } else if (kLines > 1) {
@@ -570,6 +628,38 @@ struct NormGrad {
           to[c] = s;
         }
       }
+    }
+  }
+};
+// Sums of the workgroups' sums: a workgroup takes 32 columns, a quad for each of 32 threads, which share the parts.
+template <class T>
+struct QuadSums {
+  static constexpr int kThreads = 256, kSide = 32;
+  static constexpr int kPhases = 2;
+  static constexpr size_t kLdsBytes = kThreads * 16;
+  struct Regs {};
+  template <int PH>
+  HCNN_HD static void phase(const ColumnSumArgs& a, unsigned bid, int tid, uint32_t* lds_words, Regs&) {
+    float* lds = reinterpret_cast<float*>(lds_words);              // [kSide][32]
+    if constexpr (PH == 0) {
+      const uint32_t n = bid * 32 + tid % 8 * 4;
+      float s[4] = {};
+      if (n < a.N) {
+#pragma unroll 8
+        for (uint32_t b = tid / 8; b < a.blocks; b += kSide) {
+          float v[4];
+          load_row(a.part + b * a.ld_part + n, v);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[e] += v[e];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) lds[tid * 4 + e] = s[e];
+    } else if (tid < 32 && bid * 32 + tid < a.N) {
+      float s = 0.0f;
+#pragma unroll
+      for (int l = 0; l < kSide; ++l) s += lds[l * 32 + tid];
+      static_cast<T*>(a.out)[bid * 32 + tid] = Num<T>::narrow(s);
     }
   }
 };

@@ -73,11 +73,11 @@ int rms_norm(hcnn_plain* h, size_t rows, size_t n, const void* x, size_t ldx, co
   return to.codes ? norm_rows<T, kMx8>(h, a) : norm_rows<T, kMxNone>(h, a);
 }
 
-// Rows of a workgroup, and workgroups, of the norm's gradient
+// Rows of a workgroup, and workgroups, of the norm's gradient: as many as the compute units hold at a time, by the kernels' registers
 struct RowShare { uint32_t each; size_t groups; };
-inline RowShare norm_share(const hcnn_plain* h, size_t rows, int lines) {
-  const size_t most = (size_t)h->compute_units * 4;
-  const size_t each = up(std::max<size_t>(blocks(rows, most), 1), lines);
+inline RowShare norm_share(const hcnn_plain* h, size_t rows, const RowShape& s) {
+  const size_t most = (size_t)h->compute_units * (s.lanes == 1024 ? 1 : s.el == 16 ? 3 : 5);
+  const size_t each = up(std::max<size_t>(blocks(rows, most), 1), s.lanes < 256 ? 256 / s.lanes : 1);
   return RowShare{(uint32_t)each, blocks(rows, each)};
 }
 template <class K>
@@ -92,7 +92,7 @@ template <class T>
 int rms_norm_grad(hcnn_plain* h, size_t rows, size_t n, const void* dy, size_t ld_dy, const void* hid, size_t ldh, const void* weight, const void* dh, size_t ld_dh,
                   double eps, void* dx, size_t ld_dx, void* dw) {
   const RowShape s = row_shape(n);
-  const RowShare share = norm_share(h, rows, s.lanes < 256 ? 256 / s.lanes : 1);
+  const RowShare share = norm_share(h, rows, s);
   // rows of any length: their columns' sums in a pass of their own, about eight workgroups for each compute unit
   const size_t col_blocks = blocks(n, NormColumns<T>::kCols);
   const uint32_t col_rows = (uint32_t)std::max<size_t>(16, blocks(rows, std::max<size_t>(1, (size_t)h->compute_units * 8 / col_blocks)));
@@ -116,12 +116,12 @@ int rms_norm_grad(hcnn_plain* h, size_t rows, size_t n, const void* dy, size_t l
     }
   }
   if (dw) {
-    // (a launch has fewer than 2^32 threads: 16 columns for each workgroup)
-    const size_t most = most_workgroups(ColumnSum<T>::kThreads) * 16;
+    // (a launch has fewer than 2^32 threads: 32 columns for each workgroup)
+    const size_t most = most_workgroups(QuadSums<T>::kThreads) * 32;
     for (size_t c = 0; c < n; c += most) {
       const size_t some = std::min(most, n - c);
       const ColumnSumArgs cs{at<float>(h, o_part) + c, a.ld_part, (uint32_t)(rows ? parts : 0), (uint32_t)some, static_cast<char*>(dw) + c * sizeof(T)};
-      if ((e = launch<ColumnSum<T>>(h->stream, blocks(some, 16), ColumnSum<T>::kLdsBytes, cs))) return e;
+      if ((e = launch<QuadSums<T>>(h->stream, blocks(some, 32), QuadSums<T>::kLdsBytes, cs))) return e;
     }
   }
   return 0;
