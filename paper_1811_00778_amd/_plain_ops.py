@@ -6,8 +6,9 @@ A subclass provides
     _targets(x, what)           (address, length, bytes of a number) of a 1-D int32 or int64 array without gaps
     _new(shape, like)           new uninitialised array of the type and place of `like` (None: 32-bit floats)
     _span(x)                    (first byte, one past the last) of the array's memory
-    _bytes(x, what)             (address, shape, strides, bytes from there to the end of the memory it is a view of) of a 2-D array of bytes
-    _new_bytes(rows, cols)      new uninitialised 2-D array of bytes
+    _bytes(x, what)             (address, shape, strides) of a 2-D array of bytes
+    _room(x)                    bytes from its first to the end of the memory it is a view of
+    _new_bytes(rows, cols, of)  the first `of` columns of a new uninitialised 2-D array of bytes
     _new_of(shape, dtype)       (new uninitialised array of the type, the type's code)
 Marshalling and checks only: no arithmetic of the method happens here.
 """
@@ -246,8 +247,7 @@ class PlainOpsMixin:
             y = self._new((rows, n), x)
             yp = self._address(y)
         else:
-            y = self._new_microscaled(rows, n, format)
-            codes, _, scales, pitch = self._microscaled(y, "y")
+            y, codes, scales, pitch = self._new_microscaled(rows, n, format)
         self._pre_call()
         self.raw.call("hcnn_rms_norm", dtype, rows, n, xp, ldx, rp, ldr, wp, float(eps), sp, n, yp, n, codes, scales, pitch)
         return (y, s) if keep else y
@@ -277,8 +277,11 @@ class PlainOpsMixin:
 
     # ---- few bits
     def _new_microscaled(self, rows, n, format):
-        wide = -(-n // 128) * 128
-        return Microscaled(self._new_bytes(rows, wide // 8 * _capi.MX_BITS[format]), self._new_bytes(wide // 32, -(-rows // 64) * 64)[:, :rows], n, format)
+        """(new Microscaled matrix, its codes' address, its scales', their pitch)"""
+        wide, pitch = -(-n // 128) * 128, -(-rows // 64) * 64
+        row_bytes = wide // 8 * _capi.MX_BITS[format]
+        codes, scales = self._new_bytes(rows, row_bytes, row_bytes), self._new_bytes(wide // 32, pitch, rows)
+        return Microscaled(codes, scales, n, format), self._address(codes), self._address(scales), pitch
 
     def _microscaled(self, m, what):
         """(codes' address, rows, scales' address, their pitch) of a Microscaled matrix whose arrays are what its format says"""
@@ -287,21 +290,22 @@ class PlainOpsMixin:
         if m.columns < 0:
             raise ValueError("%s must have columns" % what)
         wide = -(-m.columns // 128) * 128
-        cp, shape, strides, _ = self._bytes(m.codes, "the codes of " + what)
-        rows, row_bytes = shape
-        if row_bytes != wide // 8 * _capi.MX_BITS[m.format] or (rows > 1 and row_bytes and strides[0] != row_bytes) or (rows and row_bytes and strides[1] != 1):
-            raise ValueError("the codes of %s must be a contiguous array of shape (rows, %d)" % (what, wide // 8 * _capi.MX_BITS[m.format]))
-        sp, shape, strides, room = self._bytes(m.scales, "the scales of " + what)
+        row_bytes = wide // 8 * _capi.MX_BITS[m.format]
+        cp, (rows, got), strides = self._bytes(m.codes, what)
+        if got != row_bytes or (rows and got and strides[1] != 1) or (rows > 1 and got and strides[0] != got):
+            raise ValueError("the codes of %s must be a contiguous array of shape (rows, %d)" % (what, row_bytes))
+        sp, shape, strides = self._bytes(m.scales, what)
         if shape != (wide // 32, rows):
             raise ValueError("the scales of %s must have shape %r, got %r" % (what, (wide // 32, rows), shape))
-        pitch = strides[0] if rows and wide else -(-rows // 64) * 64
-        if rows and wide:
-            if (rows > 1 and strides[1] != 1) or pitch % 64 or pitch < rows:
-                raise ValueError("the scales of %s must be the first bytes of rows that lie a multiple of 64 bytes apart" % what)
-            if room < wide // 32 * pitch:
-                raise ValueError("the memory of the scales of %s must reach to the end of their last row's %d bytes" % (what, pitch))
-            if cp % 16 or sp % 16:
-                raise ValueError("codes and scales of %s must start on 16 bytes" % what)
+        if not rows or not wide:
+            return cp, rows, sp, -(-rows // 64) * 64
+        pitch = strides[0]
+        if (rows > 1 and strides[1] != 1) or pitch % 64 or pitch < rows:
+            raise ValueError("the scales of %s must be the first bytes of rows that lie a multiple of 64 bytes apart" % what)
+        if pitch != rows and self._room(m.scales) < wide // 32 * pitch:
+            raise ValueError("the memory of the scales of %s must reach to the end of their last row's %d bytes" % (what, pitch))
+        if cp % 16 or sp % 16:
+            raise ValueError("codes and scales of %s must start on 16 bytes" % what)
         return cp, rows, sp, pitch
 
     def quantize_mx(self, x, format="mx4", values=False):
@@ -309,8 +313,7 @@ class PlainOpsMixin:
         xp, rows, n, ldx, dtype = self._matrix(x, "x")
         if format not in _capi.MX_BITS:
             raise ValueError("format must be one of %s, got %r" % (", ".join(_capi.MX_BITS), format))
-        m = self._new_microscaled(rows, n, format)
-        cp, _, sp, pitch = self._microscaled(m, "the result")
+        m, cp, sp, pitch = self._new_microscaled(rows, n, format)
         v = self._new((rows, n), x) if values else None
         self._pre_call()
         self.raw.call("hcnn_quantize_mx", dtype, _capi.MX_BITS[format], rows, n, xp, ldx, cp, sp, pitch, self._address(v), n)

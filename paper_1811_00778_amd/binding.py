@@ -173,11 +173,16 @@ class PlainContext(PlainOpsMixin):
 
     def _bytes(self, x, what):
         if not isinstance(x, torch.Tensor) or x.dtype != torch.uint8 or x.get_device() != self._index or x.dim() != 2:
-            raise TypeError("%s must be a 2-D uint8 tensor on %s" % (what, self.device))
-        return x.data_ptr(), tuple(x.shape), x.stride(), x.untyped_storage().nbytes() - x.storage_offset()
+            raise TypeError("codes and scales of %s must be 2-D uint8 tensors on %s" % (what, self.device))
+        return x.data_ptr(), tuple(x.shape), x.stride()
 
-    def _new_bytes(self, rows, cols):
-        return torch.empty((rows, cols), dtype=torch.uint8, device=self.device)
+    @staticmethod
+    def _room(x):
+        return x.untyped_storage().nbytes() - x.storage_offset()
+
+    def _new_bytes(self, rows, cols, of):
+        a = torch.empty((rows, cols), dtype=torch.uint8, device=self.device)
+        return a if of == cols else a.narrow(1, 0, of)
 
     def _new_of(self, shape, dtype):
         if dtype not in _PLAIN_DT:

@@ -19,11 +19,15 @@ class EmuRows(EmuPlain):
     def _bytes(self, x, what):
         if not isinstance(x, np.ndarray) or x.dtype != np.uint8 or x.ndim != 2:
             raise TypeError("%s must be a 2-D array of bytes" % what)
-        base = x if x.base is None else x.base
-        return x.ctypes.data, x.shape, x.strides, base.nbytes - (x.ctypes.data - base.ctypes.data)
+        return x.ctypes.data, x.shape, x.strides
 
-    def _new_bytes(self, rows, cols):
-        return emu.aligned(np.full((rows, cols), 0xff, np.uint8))
+    @staticmethod
+    def _room(x):
+        base = x if x.base is None else x.base
+        return base.nbytes - (x.ctypes.data - base.ctypes.data)
+
+    def _new_bytes(self, rows, cols, of):
+        return emu.aligned(np.full((rows, cols), 0xff, np.uint8))[:, :of]
 
     def _new_of(self, shape, dtype):
         a = np.empty(shape, dtype)
