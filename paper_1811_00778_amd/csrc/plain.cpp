@@ -295,6 +295,13 @@ uint32_t hcnn_emu_choice(hcnn_plain* h, int dtype, size_t M, size_t N, size_t K,
   const Shape s = PLAIN_BY_TYPE(dtype, choose, h, M, N, K, may_split != 0, direct != 0);
   return (uint32_t)s.tile | s.splits << 8;
 }
+// Shape (low byte) and parts of k that a microscaled product takes
+uint32_t hcnn_emu_mx_choice(hcnn_plain* h, int format, size_t M, size_t K, size_t N) {
+  MxCall c{};
+  c.format = format; c.M = M; c.K = K; c.N = N; c.x_pitch = up(M, 64); c.w_pitch = up(N, 64);
+  const MxShape s = mx_shape(h, c);
+  return (uint32_t)s.kind | s.splits << 8;
+}
 int hcnn_emu_copies(size_t rows, size_t cols, double work) { return copy_pays(Input{nullptr, cols, rows, cols}, work); }
 #endif
 

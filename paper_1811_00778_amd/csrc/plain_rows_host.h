@@ -146,18 +146,40 @@ struct MxCall {
   const void *bias, *residual; size_t ld_residual;
   void* y; size_t ldy;
 };
-// Tile (0: the simple form) and parts of k
-struct MxShape { uint32_t tile, splits; };
+// Shape of the product, by an estimate of its time in us: `load` workgroups for each compute unit, a step's time with few workgroups and for each of several on a
+// unit, what a workgroup's beginning and ending add, parts of k written and joined.  Strips (kMxStrip) of 16 MF x 16 NF outputs, tiles of 128 and 256.  Fitted to
+// graphs of 20 calls, us estimated / measured with four and eight bits: 1 x 4096 -> 4096 strips of 16 x 16 5 / 4.4, 4.4; 64 x 4096 -> 4096 of 64 x 16 8 / 8.3, 11 / 11.7; 256 x
+// 4096 -> 4096 of 64 x 64 14 / 13.8, 19 / 19.4; 1024 x 4096 -> 4096 tiles of 128 19 / 18.6, 24 / 23.4; 4096 x 4096 -> 4096 of 256 39 / 38.9, 55 / 54.9.
+enum { kMxStrip11, kMxStrip14, kMxStrip41, kMxStrip44, kMxTile128, kMxTile256, kMxShapes };
+struct MxShape { int kind; uint32_t splits; };
 inline MxShape mx_shape(const hcnn_plain* h, const MxCall& c) {
+  constexpr uint32_t kRows[] = {16, 16, 64, 64, 128, 256}, kCols[] = {16, 64, 16, 64, 128, 256};
+  constexpr double kBegin[] = {2.9, 3.3, 3.2, 6.0, 4.5, 7.0}, kMore[] = {0.3, 1.0, 0.8, 2.2, 2.3, 9.0};     // a launch; each further workgroup of a unit
+  constexpr double kStep[2][kMxShapes] = {{0.05, 0.145, 0.14, 0.25, 0.37, 1.0}, {0.06, 0.16, 0.22, 0.42, 0.55, 1.5}};
+  constexpr double kLoad[2][kMxShapes] = {{0.07, 0.2, 0.15, 0.17, 0.29, 0.84}, {0.08, 0.22, 0.29, 0.27, 0.42, 1.25}};
   // offsets within a tile and a step in 32 bits
-  const bool fits = 256 * mx_row_bytes(c.format, c.K) < ((size_t)1 << 32) && 4 * std::max(c.x_pitch, c.w_pitch) < ((size_t)1 << 32);
-  if (c.K == 0 || !fits || c.M <= 16 || c.N <= 16) return MxShape{0, 1};
+  const bool tiles = 256 * mx_row_bytes(c.format, c.K) < ((size_t)1 << 32) && 4 * std::max(c.x_pitch, c.w_pitch) < ((size_t)1 << 32) && c.K && c.M > 16 && c.N > 16;
+  const int f = c.format == kMx4 ? 0 : 1;
+  const size_t steps = blocks(c.K, 128);
 #ifdef HCNN_HOSTEMU
-  if (emu_tile >= 0) return MxShape{emu_tile == kTile256 ? 256u : emu_tile == kTile128 ? 128u : 0u, emu_tile == kTile256 || emu_tile == kTile128 ? emu_parts : 1};
+  if (emu_tile >= 0 && tiles) return emu_tile == kTile256 ? MxShape{kMxTile256, emu_parts} : emu_tile == kTile128 ? MxShape{kMxTile128, emu_parts} : MxShape{kMxStrip44, 1};
 #endif
-  if (blocks(c.M, 256) * blocks(c.N, 256) >= h->compute_units) return MxShape{256, 1};
-  if (blocks(c.M, 128) * blocks(c.N, 128) >= h->compute_units) return MxShape{128, 1};
-  return MxShape{0, 1};
+  MxShape best{kMxStrip44, 1};
+  double least = 1e300;
+  for (int k = 0; k < kMxShapes; ++k) {
+    if ((kRows[k] == 16 && c.M > 16) || (k >= kMxTile128 && !tiles)) continue;
+    const double all = (double)blocks(c.M, kRows[k]) * (double)blocks(c.N, kCols[k]);
+    for (uint32_t s = 1; s == 1 || (k >= kMxTile128 && s <= 8 && s * 4 <= steps); ++s) {
+      const double load = std::ceil(all * s / h->compute_units);
+      double us = kBegin[k] + kMore[k] * (load - 1) + std::max(kStep[f][k], kLoad[f][k] * load) * (double)blocks(steps, s);
+      if (s > 1) us += 3.0 + (double)s * (double)c.M * (double)c.N * 8 / 4.2e6;
+      if (us < least) {
+        least = us;
+        best = MxShape{k, s};
+      }
+    }
+  }
+  return best;
 }
 template <class T, int F, int BM, int BN, int WM, int WN>
 int mx_tile(hcnn_plain* h, MxArgs& a) {
@@ -184,6 +206,7 @@ int linear_mx_of(hcnn_plain* h, const MxCall& c) {
   a.x = c.x; a.x_scales = c.x_scales; a.x_pitch = c.x_pitch; a.x_bytes = mx_row_bytes(F, c.K);
   a.w = c.w; a.w_scales = c.w_scales; a.w_pitch = c.w_pitch; a.w_bytes = mx_row_bytes(kMx4, c.K);
   a.steps = (uint32_t)blocks(c.K, 128);
+  const MxShape s = mx_shape(h, c);
   auto strip = [&](auto kernel) {
     typedef decltype(kernel) S;
     const size_t grid = S::grid(a.g), most = most_workgroups(S::kThreads);
@@ -191,15 +214,18 @@ int linear_mx_of(hcnn_plain* h, const MxCall& c) {
     for (a.first = 0; a.first < grid && !e; a.first += most) e = launch<S>(h->stream, std::min(most, grid - a.first), S::kLdsBytes, a);
     return e;
   };
-  const MxShape s = mx_shape(h, c);
-  if (s.tile) {
+  if (s.kind >= kMxTile128) {
     a.part = (uint32_t)up(blocks(a.steps, s.splits), 2);
     a.g.splits = (uint32_t)blocks(a.steps, a.part);
-    return s.tile == 256 ? mx_tile<T, F, 256, 256, 2, 4>(h, a) : mx_tile<T, F, 128, 128, 2, 2>(h, a);
   }
-  if (c.M <= 16) return c.N <= 16 * (size_t)h->compute_units ? strip(MxStrip<T, F, 1, 1>{}) : strip(MxStrip<T, F, 1, 4>{});
-  if (c.N <= 16) return strip(MxStrip<T, F, 4, 1>{});
-  return strip(MxStrip<T, F, 4, 4>{});
+  switch (s.kind) {
+    case kMxStrip11: return strip(MxStrip<T, F, 1, 1>{});
+    case kMxStrip14: return strip(MxStrip<T, F, 1, 4>{});
+    case kMxStrip41: return strip(MxStrip<T, F, 4, 1>{});
+    case kMxStrip44: return strip(MxStrip<T, F, 4, 4>{});
+    case kMxTile128: return mx_tile<T, F, 128, 128, 2, 2>(h, a);
+    default: return mx_tile<T, F, 256, 256, 2, 4>(h, a);
+  }
 }
 template <class T>
 int linear_mx(hcnn_plain* h, const MxCall& c) { return c.format == kMx4 ? linear_mx_of<T, kMx4>(h, c) : linear_mx_of<T, kMx8>(h, c); }

@@ -397,3 +397,17 @@ def test_tiles_of_the_product(b, form, tile, size, parts):
         assert bits.value == 1 << (0 if -(-steps // each) == 1 else 1) << (0 if tile == 0 else 2) << (0 if form == "mx4" else 4)
     finally:
         lib.hcnn_emu_shape(-1, 1, 0)
+
+
+def test_shapes_of_the_product_by_the_rule():
+    """every shape has sizes that take it on a device of 256 compute units"""
+    lib = emu.lib()
+    lib.hcnn_emu_mx_choice.argtypes, lib.hcnn_emu_mx_choice.restype = [ctypes.c_void_p, ctypes.c_int] + [ctypes.c_size_t] * 3, ctypes.c_uint32
+    with emu.device(lib, units=256):
+        ctx = EmuRows()
+        got = {(form, size): lib.hcnn_emu_mx_choice(ctx.raw.handle, form, *size) for form in (4, 8)
+               for size in ((1, 4096, 4096), (1, 4096, 16384), (64, 4096, 4096), (64, 4096, 16384), (1024, 4096, 4096), (8192, 8192, 256), (4096, 4096, 4096), (5000, 100, 3))}
+    want = {(1, 4096, 4096): (0, 1), (1, 4096, 16384): (1, 1), (64, 4096, 4096): (2, 1), (64, 4096, 16384): (3, 1), (1024, 4096, 4096): (4, 1), (8192, 8192, 256): (4, 2),
+            (4096, 4096, 4096): (5, 1), (5000, 100, 3): (2, 1)}
+    for (form, size), choice in got.items():
+        assert (choice & 255, choice >> 8) == want[size], (form, size, choice)
