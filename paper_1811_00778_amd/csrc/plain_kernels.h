@@ -287,11 +287,11 @@ struct GemmArgs {
   uint32_t n_offset;           // class of column 0
 };
 
-// What the linear layer makes of B x W sums: W in a row, of the rows m[.] of the output (~0: none).  `bias`: of these columns, 0 where there is none.
+// What the linear layer makes of B x W sums: W in a row, of the rows m[.] of the output (~0: none), which lie at row[.] there.  `bias`: of these columns, 0 where
+// there is none.
 template <class T, int B, int W>
-HCNN_HD void finish(const GemmArgs& a, const uint32_t (&m)[B], uint32_t n, const float (&bias)[W], float (&v)[B][W]) {
+HCNN_HD void finish_values(const GemmArgs& a, const uint32_t (&m)[B], uint32_t n, const float (&bias)[W], float (&v)[B][W], size_t (&row)[B]) {
   const uint32_t left = a.N - n;
-  size_t row[B];
   float r[B][W];
 #pragma unroll
   for (int i = 0; i < B; ++i) {
@@ -330,9 +330,14 @@ HCNN_HD void finish(const GemmArgs& a, const uint32_t (&m)[B], uint32_t n, const
 #pragma unroll
       for (int e = 0; e < W; ++e) v[i][e] += r[i][e];
   }
+}
+template <class T, int B, int W>
+HCNN_HD void finish(const GemmArgs& a, const uint32_t (&m)[B], uint32_t n, const float (&bias)[W], float (&v)[B][W]) {
+  size_t row[B];
+  finish_values<T>(a, m, n, bias, v, row);
 #pragma unroll
   for (int i = 0; i < B; ++i)
-    if (m[i] != ~0u) store_row(static_cast<T*>(a.out) + row[i] * a.ld_out + n, left, v[i]);
+    if (m[i] != ~0u) store_row(static_cast<T*>(a.out) + row[i] * a.ld_out + n, a.N - n, v[i]);
 }
 
 enum { kEpiOut = 0, kEpiSums = 1, kEpiStats = 2, kEpiDelta = 3 };

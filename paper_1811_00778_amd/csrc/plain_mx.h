@@ -263,6 +263,51 @@ HCNN_HD void direct_all_but() {
 #endif
 }
 
+// 16 numbers of each of a wave's 16 x 4 lanes, four lanes (16 apart) side by side in a row, to memory in 64 bytes of every row at a time: the lanes' pieces of 16 bytes
+// change places first.  (Stores of a lane's own pieces write 16 of every 32 or 64 bytes at a time: 8192 x 128 -> 16384 took 82 us in place of KKK.)
+template <class T>
+HCNN_HD void store_quads(T* p, [[maybe_unused]] uint32_t g, const float (&v)[16], bool here) {     // p: the lane's own first number; here: the row is there
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int P = sizeof(T);                                     // pieces: two of 16-bit numbers, four of 32
+  constexpr uint32_t kPer16 = 16 / sizeof(T);
+  T t[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) t[i] = Num<T>::narrow(v[i]);
+  uint32_t w[P][4];
+  __builtin_memcpy(w, t, sizeof(t));
+  auto swap = [](auto wide, uint32_t& a, uint32_t& b) {
+    typedef unsigned two __attribute__((ext_vector_type(2)));
+    two r;
+    if constexpr (decltype(wide)::value) r = __builtin_bit_cast(two, __builtin_amdgcn_permlane32_swap(a, b, false, false));
+    else r = __builtin_bit_cast(two, __builtin_amdgcn_permlane16_swap(a, b, false, false));
+    a = r.x;
+    b = r.y;
+  };
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    if constexpr (P == 2) {
+      swap(std::false_type{}, w[0][d], w[1][d]);
+      swap(std::true_type{}, w[0][d], w[1][d]);
+    } else {
+      swap(std::false_type{}, w[0][d], w[1][d]);
+      swap(std::false_type{}, w[P - 2][d], w[P - 1][d]);
+      swap(std::true_type{}, w[0][d], w[P - 2][d]);
+      swap(std::true_type{}, w[1][d], w[P - 1][d]);
+    }
+  }
+  if (!here) return;
+  T* row = p - 16 * g;                                             // the four lanes' first number
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    U4 x;
+    __builtin_memcpy(&x, w[i], 16);
+    st16(reinterpret_cast<char*>(row + (i * 4 + g) * kPer16), x);
+  }
+#else
+  if (here) store_row(p, v);
+#endif
+}
+
 template <class T, int F, int BM, int BN, int WM, int WN, int EPI>
 struct MxTile {
   static constexpr int kThreads = WM * WN * 64;
@@ -496,8 +541,18 @@ struct MxTile {
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[q][e] = r.acc[q0 + q][j0 + e % 4][e / 4];
           }
-          if constexpr (EPI == kEpiOut) finish<T>(a.g, m, n, bias, v);
-          else {
+          if constexpr (EPI == kEpiOut) {
+            size_t row[2];
+            finish_values<T>(a.g, m, n, bias, v, row);
+            // (whole groups of 64 columns: the same for all lanes of the wave)
+            const bool whole = r.n0 + w_row(tid & ~63, j0) + 64 <= a.g.N;
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+              T* to = static_cast<T*>(a.g.out) + row[q] * a.g.ld_out + n;
+              if (whole) store_quads(to, tid % 64 / 16, v[q], m[q] != ~0u);
+              else if (m[q] != ~0u) store_row(to, left, v[q]);
+            }
+          } else {
             const uint32_t quads = (left + 3) / 4 * 4;                 // (rows of sums have room for whole quads)
 #pragma unroll
             for (int q = 0; q < 2; ++q)
