@@ -454,54 +454,62 @@ struct NormGrad {
   static constexpr int kThreads = LANES > 256 ? LANES : 256, W = kChunk<T>, kLines = kThreads / LANES;
   static constexpr int kHeld = EL ? EL / W : 1;
   static constexpr int kLoopPhases = 2, kPhases = 4;
+  // (the host gives a compute unit as many workgroups: with one fewer there, 8192 x 4096 took 118 us in place of 57)
+  static constexpr int kMinWavesPerSimd = kThreads == 1024 ? 4 : EL == 16 ? (sizeof(T) == 4 ? 2 : 3) : sizeof(T) == 4 ? 4 : 5;
   typedef RowSum<LANES, kThreads, 2> Sum;
   static constexpr size_t kSumBytes = 2 * Sum::kLdsBytes;                        // two, taken in turn: a barrier an iteration
   static constexpr size_t kLdsBytes = kSumBytes + (kLines > 1 ? (size_t)kLines * LANES * EL * 4 : 0);
-  // A row as it lies in memory (the next one is asked for before the sums of this one are known) and the weights, for all rows
-  struct Raw { T v[kHeld][W]; };
+  // A row as it lies in memory (the next one is asked for before the sums of this one are known, where the registers have room for it) and the weights, for all rows
+  static constexpr bool kNext = LANES < 1024 || EL < 16;
+  struct Raw { U4 v[kHeld]; };
   struct Regs {
     uint32_t iter;
     Raw w, dy, h, dh;
-    float dyf[kHeld][W], hf[kHeld][W], dhf[kHeld][W], dw[kHeld][W];
+    U4 now[kHeld];                          // dh of the row at hand
+    float dyf[kHeld][W], hf[kHeld][W], dw[kHeld][W];
     double sum[2];
   };
   static constexpr bool wave_sync(int ph) { return ph == 1 || (ph == 0 && LANES <= 64); }
   HCNN_HD static uint32_t loop_count(const NormGradArgs& a) { return a.rows_each / kLines; }
   HCNN_HD static size_t row_of(const NormGradArgs& a, unsigned bid, int tid, uint32_t iter) { return (size_t)bid * a.rows_each + (size_t)iter * kLines + tid / LANES; }
-  HCNN_HD static void load(const T* row, uint32_t n, uint32_t lane, Raw& r) {
+  HCNN_HD static void widened(const U4& v, float (&to)[W]) {
+    T t[W];
+    __builtin_memcpy(t, &v, 16);
+#pragma unroll
+    for (int e = 0; e < W; ++e) to[e] = Num<T>::widen(t[e]);
+  }
+  // (`otherwise` where there is no such number, or no row)
+  HCNN_HD static void load(const T* row, uint32_t n, uint32_t lane, float otherwise, Raw& r) {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
       const uint32_t c = (i * LANES + lane) * W;
-      if (c + W <= n) {
-        const U4 v = ld16(reinterpret_cast<const char*>(row + c));
-        __builtin_memcpy(r.v[i], &v, 16);
+      U4 v;
+      if (row && c + W <= n) {
+        v = ld16(reinterpret_cast<const char*>(row + c));
       } else {
+        T t[W];
 #pragma unroll
-        for (uint32_t e = 0; e < W; ++e) {
-          r.v[i][e] = Num<T>::narrow(0.0f);
-          if (c + e < n) r.v[i][e] = row[c + e];
-        }
+        for (int e = 0; e < W; ++e) t[e] = row && c + e < n ? row[c + e] : Num<T>::narrow(otherwise);
+        __builtin_memcpy(&v, t, 16);
       }
+      r.v[i] = v;
     }
   }
   HCNN_HD static void ask(const NormGradArgs& a, size_t row, uint32_t lane, Regs& r) {
     if (row >= a.rows) return;
-    load(static_cast<const T*>(a.dy) + row * a.ld_dy, a.n, lane, r.dy);
-    load(static_cast<const T*>(a.h) + row * a.ldh, a.n, lane, r.h);
-    if (a.dh) load(static_cast<const T*>(a.dh) + row * a.ld_dh, a.n, lane, r.dh);
+    load(static_cast<const T*>(a.dy) + row * a.ld_dy, a.n, lane, 0.0f, r.dy);
+    load(static_cast<const T*>(a.h) + row * a.ldh, a.n, lane, 0.0f, r.h);
+    load(a.dh ? static_cast<const T*>(a.dh) + row * a.ld_dh : nullptr, a.n, lane, 0.0f, r.dh);
   }
   HCNN_HD static void begin(const NormGradArgs& a, unsigned bid, int tid, uint32_t*, Regs& r) {
     if constexpr (EL > 0) {
       const uint32_t lane = (uint32_t)tid % LANES;
-      if (a.weight) load(static_cast<const T*>(a.weight), a.n, lane, r.w);
+      load(static_cast<const T*>(a.weight), a.n, lane, 1.0f, r.w);
 #pragma unroll
       for (int i = 0; i < kHeld; ++i)
 #pragma unroll
-        for (int e = 0; e < W; ++e) {
-          r.dw[i][e] = 0.0f;
-          if (!a.weight) r.w.v[i][e] = Num<T>::narrow(1.0f);
-        }
-      ask(a, row_of(a, bid, tid, 0), lane, r);
+        for (int e = 0; e < W; ++e) r.dw[i][e] = 0.0f;
+      if (kNext) ask(a, row_of(a, bid, tid, 0), lane, r);
     }
   }
   HCNN_HD static void add(const float (&g)[W], const float (&h)[W], double (&sum)[2]) {
@@ -547,19 +555,19 @@ struct NormGrad {
       r.sum[0] = r.sum[1] = 0.0;
       if (here) {
         if constexpr (EL > 0) {
+          if (!kNext) ask(a, row, lane, r);
 #pragma unroll
           for (int i = 0; i < kHeld; ++i) {
             float g[W];
+            widened(r.dy.v[i], r.dyf[i]);
+            widened(r.h.v[i], r.hf[i]);
+            widened(r.w.v[i], g);
+            r.now[i] = r.dh.v[i];
 #pragma unroll
-            for (int e = 0; e < W; ++e) {
-              r.dyf[i][e] = Num<T>::widen(r.dy.v[i][e]);
-              r.hf[i][e] = Num<T>::widen(r.h.v[i][e]);
-              r.dhf[i][e] = a.dh ? Num<T>::widen(r.dh.v[i][e]) : 0.0f;
-              g[e] = r.dyf[i][e] * Num<T>::widen(r.w.v[i][e]);
-            }
+            for (int e = 0; e < W; ++e) g[e] *= r.dyf[i][e];
             add(g, r.hf[i], r.sum);
           }
-          if (r.iter + 1 < loop_count(a)) ask(a, row + kLines, lane, r);
+          if (kNext && r.iter + 1 < loop_count(a)) ask(a, row + kLines, lane, r);
         } else {
           for (uint32_t c = lane * W; c < a.n; c += LANES * W) {
             load_long(a, row, c, r.dyf[0], r.hf[0]);
@@ -577,17 +585,18 @@ struct NormGrad {
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) {
           const uint32_t c = (i * LANES + lane) * W;
-          if (c >= a.n) continue;
-          float g[W], dx[W];
+          float g[W], dx[W], d[W];
+          widened(r.w.v[i], g);
+          widened(r.now[i], d);
 #pragma unroll
-          for (int e = 0; e < W; ++e) g[e] = r.dyf[i][e] * Num<T>::widen(r.w.v[i][e]);
+          for (int e = 0; e < W; ++e) g[e] *= r.dyf[i][e];
           finish_chunk(s, mean, g, r.hf[i], dx);
 #pragma unroll
           for (int e = 0; e < W; ++e) {
-            dx[e] += r.dhf[i][e];
+            dx[e] += d[e];
             r.dw[i][e] += r.dyf[i][e] * r.hf[i][e];
           }
-          store_row(static_cast<T*>(a.dx) + row * a.ld_dx + c, a.n - c, dx);
+          if (c < a.n) store_row(static_cast<T*>(a.dx) + row * a.ld_dx + c, a.n - c, dx);
         }
       } else {
         if (lane == 0 && a.inverse) a.inverse[row] = s.whole;

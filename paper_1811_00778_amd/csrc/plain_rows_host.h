@@ -75,8 +75,8 @@ int rms_norm(hcnn_plain* h, size_t rows, size_t n, const void* x, size_t ldx, co
 
 // Rows of a workgroup, and workgroups, of the norm's gradient: as many as the compute units hold at a time, by the kernels' registers
 struct RowShare { uint32_t each; size_t groups; };
-inline RowShare norm_share(const hcnn_plain* h, size_t rows, const RowShape& s) {
-  const size_t most = (size_t)h->compute_units * (s.lanes == 1024 ? 1 : s.el == 16 ? 3 : 5);
+inline RowShare norm_share(const hcnn_plain* h, size_t rows, const RowShape& s, bool wide) {
+  const size_t most = (size_t)h->compute_units * (s.lanes == 1024 ? 1 : s.el == 16 ? (wide ? 2 : 3) : wide ? 4 : 5);
   const size_t each = up(std::max<size_t>(blocks(rows, most), 1), s.lanes < 256 ? 256 / s.lanes : 1);
   return RowShare{(uint32_t)each, blocks(rows, each)};
 }
@@ -92,7 +92,7 @@ template <class T>
 int rms_norm_grad(hcnn_plain* h, size_t rows, size_t n, const void* dy, size_t ld_dy, const void* hid, size_t ldh, const void* weight, const void* dh, size_t ld_dh,
                   double eps, void* dx, size_t ld_dx, void* dw) {
   const RowShape s = row_shape(n);
-  const RowShare share = norm_share(h, rows, s);
+  const RowShare share = norm_share(h, rows, s, sizeof(T) == 4);
   // rows of any length: their columns' sums in a pass of their own, about eight workgroups for each compute unit
   const size_t col_blocks = blocks(n, NormColumns<T>::kCols);
   const uint32_t col_rows = (uint32_t)std::max<size_t>(16, blocks(rows, std::max<size_t>(1, (size_t)h->compute_units * 8 / col_blocks)));
