@@ -5,10 +5,10 @@ over its placements' gathered inputs, the square activation the product's ending
 inputs and weights, gradients are clipped before the step (a square's slope has no bound) -- and its weights are rounded to the small
 integers that hcnn_ct_scalar_mac takes (Sec. 4.3).
 
-    python -m paper_1811_00778_amd.train [--steps S] [--batch B] [--dtype f32|f16|bf16]
+    python -m paper_1811_00778_amd.train [--steps S] [--batch B] [--dtype f32|f16|bf16] [--dropout P]
 
 trains the MNIST-shaped network on made-up images, rounds it, and evaluates a few images encrypted: the decrypted scores are
-the integer network's, number for number.
+the integer network's, number for number.  It also answers in the clear from weights of four bits (few_bit_scores).
 """
 import numpy as np
 import torch
@@ -33,12 +33,14 @@ class PlainNetwork:
     """A trainable network of network.py's specs; the last layer must be ("fc", classes).
 
     Weights and activations are tensors of `dtype` on the context's device; `weights` is the list of network.weight_shapes, None
-    for layers without weights."""
+    for layers without weights.  `dropout`: share of the last layer's inputs that a training step leaves out, by a mask of (seed, steps taken, image,
+    input); the encrypted evaluation has none of it."""
 
-    def __init__(self, spec, in_shape, ctx, dtype=torch.float32, seed=0):
+    def __init__(self, spec, in_shape, ctx, dtype=torch.float32, seed=0, dropout=0.0):
         if spec[-1][0] != "fc":
             raise ValueError("the last layer must be fully connected: its outputs are the class scores")
         self.spec, self.in_shape, self.ctx, self.dtype = spec, in_shape, ctx, dtype
+        self.seed, self.dropout, self.steps = seed, dropout, 0
         g = torch.Generator().manual_seed(seed)
         self.weights, self.tables = [], []
         prev = in_shape
@@ -72,15 +74,17 @@ class PlainNetwork:
     def _square_follows(self, i):
         return i + 1 < len(self.spec) and self.spec[i + 1][0] == "square"
 
-    def hidden(self, x, keep=None):
-        """Inputs of the last layer for images x [B][C*H*W]; `keep`: a list that takes what the backward pass needs."""
+    def hidden(self, x, keep=None, product=None):
+        """Inputs of the last layer for images x [B][C*H*W]; `keep`: a list that takes what the backward pass needs.  product(i, rows, w, activation): (outputs, what the
+        backward pass needs of them) of layer i, ctx.linear's where it is not given."""
+        product = product or (lambda i, rows, w, act: self.ctx.linear(rows, w, activation=act, keep=True))
         for i, layer in enumerate(self.spec[:-1]):
             kind, saved = layer[0], None
             if kind in ("conv", "fc"):
                 act = "square" if self._square_follows(i) else "none"
                 w = self.weights[i].reshape(self.weights[i].shape[0], -1)
                 rows = self._gather(x, self.tables[i][0]).reshape(-1, w.shape[1]) if kind == "conv" else x
-                y, z = self.ctx.linear(rows, w, activation=act, keep=True)
+                y, z = product(i, rows, w, act)
                 saved = (rows, z, act)
                 if kind == "conv":                              # placements x filters -> filters x placements
                     y = y.reshape(x.shape[0], -1, w.shape[0]).transpose(1, 2).reshape(x.shape[0], -1)
@@ -98,7 +102,12 @@ class PlainNetwork:
         """(mean loss, gradients of scale * loss for the weights, in their order)."""
         kept, grads = [], [None] * len(self.spec)
         h = self.hidden(x, kept)
+        mask = (self.dropout, self.seed, self.steps % 2 ** 32)
+        if self.dropout:
+            h = self.ctx.dropout(h, *mask)
         loss, d, grads[-1] = self.ctx.cross_entropy_grad(h, self.weights[-1], labels, scale=scale)
+        if self.dropout:
+            d = self.ctx.dropout_grad(d, *mask)
         for i in range(len(self.spec) - 2, -1, -1):
             kind = self.spec[i][0]
             if kind in ("conv", "fc"):
@@ -124,6 +133,7 @@ class PlainNetwork:
         """One clipped step of gradient descent with momentum (state: a dict that the caller keeps); returns (loss, norm).  Where the norm is
         not finite (binary16 gradients that overflow under their `scale`), weights and state stay as they are: the caller lowers the scale."""
         loss, grads = self.loss_and_gradients(x, labels, scale)
+        self.steps += 1
         mine = [(w, g) for w, g in zip(self.weights, grads) if g is not None]
         norm = self.ctx.clip_grad_norm([g for _, g in mine], max_norm * scale)
         if "moments" not in state:
@@ -139,6 +149,17 @@ class PlainNetwork:
 
     def scores(self, x):
         return self.ctx.linear(self.hidden(x), self.weights[-1])
+
+    def few_bit_weights(self):
+        """Each layer's weights as a Microscaled matrix of four-bit numbers, None without weights: what few_bit_scores takes."""
+        return [None if w is None else self.ctx.quantize_mx(w.reshape(w.shape[0], -1), "mx4") for w in self.weights]
+
+    def few_bit_scores(self, x, weights, format="mx8"):
+        """scores(x) with weights of four bits; the layers' inputs are rounded to `format` on their way into the products."""
+        def product(i, rows, _, act):
+            return self.ctx.linear_mx(self.ctx.quantize_mx(rows, format), weights[i], activation=act, dtype=self.dtype), None
+
+        return product(len(weights) - 1, self.hidden(x, product=product), None, "none")[0]
 
     def integer_weights(self, bound):
         """Weights rounded to integers of magnitude at most `bound`, each layer by its own scale (int32 arrays, None without weights).  Scores
@@ -224,13 +245,14 @@ def _main(argv=None):
     ap.add_argument("--dtype", choices=("f32", "f16", "bf16"), default="f32")
     ap.add_argument("--lr", type=float, default=0.02)
     ap.add_argument("--bound", type=int, default=3, help="largest magnitude of the integer weights")
+    ap.add_argument("--dropout", type=float, default=0.0, help="share of the last layer's inputs that a step leaves out")
     ap.add_argument("--images", type=int, default=4, help="images evaluated encrypted")
     args = ap.parse_args(argv)
     spec, in_shape, classes, levels = network.MNIST_HCNN, network.MNIST_INPUT, 10, 4
     rng = np.random.default_rng(1811)
     ctx = binding.PlainContext()
     dtype = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[args.dtype]
-    net = PlainNetwork(spec, in_shape, ctx, dtype)
+    net = PlainNetwork(spec, in_shape, ctx, dtype, dropout=args.dropout)
     protos, state, scale = None, {}, 1024.0 if args.dtype == "f16" else 1.0
     t0 = time.perf_counter()
     for step in range(args.steps):
@@ -243,11 +265,13 @@ def _main(argv=None):
             print("step %4d  loss %.4f  gradient norm %.3f" % (step, float(loss), float(norm)), flush=True)
     print("%d steps of %d images in %.2f s" % (args.steps, args.batch, time.perf_counter() - t0))
     images, labels, _ = made_up_images(512, in_shape, classes, rng, levels, protos)
-    plain = net.scores(torch.from_numpy(images).to(ctx.device, dtype) / (levels - 1)).float().cpu().numpy()
+    x = torch.from_numpy(images).to(ctx.device, dtype) / (levels - 1)
+    plain = net.scores(x).float().cpu().numpy()
+    few = net.few_bit_scores(x, net.few_bit_weights()).float().cpu().numpy()
     weights = net.integer_weights(args.bound)
     whole = integer_scores(spec, in_shape, weights, images[:64])
-    print("right answers: %.3f of 512 plain, %.3f of 64 with integer weights up to %d (largest score 2^%.1f)"
-          % (float((plain.argmax(1) == labels).mean()), float(np.mean([int(np.argmax(r)) for r in whole] == labels[:64])), args.bound,
+    print("right answers: %.3f of 512 plain, %.3f with weights of four bits, %.3f of 64 with integer weights up to %d (largest score 2^%.1f)"
+          % (float((plain.argmax(1) == labels).mean()), float((few.argmax(1) == labels).mean()), float(np.mean([int(np.argmax(r)) for r in whole] == labels[:64])), args.bound,
              np.log2(max(1, max(abs(int(v)) for r in whole for v in r)))))
     got = encrypted_scores(spec, in_shape, weights, images[:args.images])
     same = all(int(a) == int(b) for r, s in zip(got, whole) for a, b in zip(r, s))
