@@ -118,7 +118,7 @@ class PlainContext(PlainOpsMixin):
     Tensors are torch.float32, torch.float16 or torch.bfloat16 on the device, matrices with any row stride.  Streams follow
     Context's rule: torch's current stream must be the one of the last use_stream (at first, of creation).  The calls of one
     PlainContext share its work memory: one thread at a time.  They are outside torch's autograd: results carry no graph, whether inputs require
-    gradients or not; linear_grad and cross_entropy_grad are the backward passes."""
+    gradients or not; linear_grad, cross_entropy_grad, dropout_grad and rms_norm_grad are the backward passes."""
 
     def __init__(self, device="cuda:0"):
         if not torch.cuda.is_available():

@@ -161,6 +161,8 @@ HCNN_HD Chunk chunk_behind(const Chunks& s, Chunk c, uint32_t i) {
   return Chunk{c.row + q, at - q * s.per_row.d};
 }
 
+// Bound by memory: 16384 x 4096 bfloat16 numbers to four bits with their values, 304 MB, in 66 us (4.6 TB/s); by its launch at 1021 x 517.  The rounding is the conversion
+// instruction's (nearest, ties to even; beyond the largest cut to it, for eight bits before the instruction), the scaling in front of it exact.
 struct QuantizeArgs {
   Chunks chunks;               // of the rows with what is behind them up to whole 128 numbers
   const void* x;
@@ -214,6 +216,8 @@ struct Quantize {
 // ---------------------------------------------------------------- dropout
 // y = residual + (word >= threshold ? x * scale : 0): word c mod 4 of the generator's four for the counter (c div 4, row, stream, kKindDropout 2^24) decides
 // about column c of a row.  The mask is a function of (seed, stream, row, column): the backward pass forms it again, whatever type or strides it has.
+// Bound by memory: the words cost five multiply-adds and ten exclusive-ors a number, less than half of the time that 16-bit numbers take.  8192 x 16384 bfloat16 with the
+// residual, 805 MB, in 147 us (5.5 TB/s); 8192 x 800 in 32 bits 9.8.
 constexpr uint32_t kKindDropout = 4;         // (the samplers of polynomials are kinds 1 to 3)
 struct DropoutArgs {
   Chunks chunks;
@@ -335,7 +339,8 @@ struct NormRowsArgs {
 // y = h / sqrt(mean of h^2 + eps) * weight, h = x + residual in 32 bits.  LANES threads share a row and hold it in their registers, EL numbers each; EL = 0: rows
 // of any length, read a second time for y.  Squares are summed in 64 bits: none of a 32-bit number's leaves the range, and no sum of a row's is rounded to fewer
 // bits than the numbers have.  With F the numbers are scaled and weighted in 64 bits and rounded to odd on the way to 32, so that they are rounded to the
-// format's few bits once: rounded to 32 bits on the way, one in a million next to a border would end on its other side.
+// format's few bits once: rounded to 32 bits on the way, one in a million next to a border would end on its other side.  Bound by memory: 8192 x 4096 bfloat16 with the
+// residual in and its sum out, 268 MB, in 44 us (6.1 TB/s, part of it out of the last cache); one row of 4096 into eight bits 4.1 us, two waits for memory and the launch.
 template <class T, int LANES, int EL, int F>
 struct NormRows {
   static constexpr int kThreads = LANES > 256 ? LANES : 256, W = kChunk<T>, kLines = kThreads / LANES;
@@ -437,6 +442,8 @@ struct NormRows {
 
 // Gradient from h as it is stored: with u = h / sqrt(mean of h^2 + eps), both sums of a row in one pass,
 //   dx = (w dy - u mean(w dy u)) / sqrt(...) + dh,   dw = sum over rows of dy u.
+// Bound by memory: 8192 x 4096 bfloat16 with dh, 268 MB, in 57 us and 5.5 for the columns' sums (without the next row's loads ahead, and with sums of 16 columns a
+// workgroup, 76 and 18).  30011 x 77 in 32 bits 13 and 4: half of the threads' numbers lie beyond the row.
 // A workgroup takes rows_each rows, kLines at a time; the columns' sums stay in its threads' registers and leave once, in 32 bits, for QuadSums.
 struct NormGradArgs {
   const void *dy, *h, *weight, *dh;         // weight, dh may be null
