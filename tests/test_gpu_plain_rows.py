@@ -168,6 +168,26 @@ def test_linear_mx_into_place(b):
     assert np.array_equal(b.values(place), b.values(want))
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("size", [(1100, 300, 1200), (4100, 300, 4160)], ids=str)
+def test_tiles_into_place(b, dtype, size):
+    """the residual's own memory as the output of tiles whose lanes exchange what they store; what lies between the rows stays"""
+    say("place", dtype, size)
+    rng = np.random.default_rng(8)
+    M, K, N = size
+    x, _ = rc.microscaled(b, pc.normal(rng, M, K), "mx8")
+    w, _ = rc.microscaled(b, pc.normal(rng, N, K), "mx4")
+    r = b.make(pc.normal(rng, M, N), dtype)
+    want = b.ctx.linear_mx(x, w, residual=r, activation="silu")
+    wide = torch.full((M, N + 13), 7.0, dtype=_DT[dtype], device="cuda")
+    place = wide[:, 5:N + 5]
+    place.copy_(r)
+    b.ctx.linear_mx(x, w, residual=place, activation="silu", out=place)
+    assert torch.equal(place, want)
+    assert bool((wide[:, :5] == 7).all()) and bool((wide[:, N + 5:] == 7).all())
+    assert torch.equal(b.ctx.linear_mx(x, w, residual=r[:1].expand(M, N), activation="none", dtype=_DT[dtype])[3], b.ctx.linear_mx(x, w, residual=r[:1].repeat(M, 1))[3])
+
+
 # ---------------------------------------------------------------- runs of them
 def chain(ctx, x, r, w, w4, bias):
     """A layer's way in training and back, and its answer from few bits"""

@@ -146,6 +146,8 @@ def test_norm_of_many_rows(b):
         rc.check_norm_grad(b, "f16", 3, 100)
         rc.check_dropout(b, "f32", 70, 200, 0.5, True)
         rc.check_quantize(b, "bf16", "mx4", 40, 700)
+        rc.check_linear(b, "bf16", "mx8", 3, 300, 200, "relu", bias=True)
+        rc.check_linear(b, "f32", "mx4", 90, 140, 20)
 
 
 def test_norm_of_large_and_small_numbers(b):
