@@ -161,52 +161,56 @@ HCNN_HD Chunk chunk_behind(const Chunks& s, Chunk c, uint32_t i) {
   return Chunk{c.row + q, at - q * s.per_row.d};
 }
 
-// Bound by memory: 16384 x 4096 bfloat16 numbers to four bits with their values, 304 MB, in 66 us (4.6 TB/s); by its launch at 1021 x 517.  The rounding is the conversion
+// Bound by memory: 16384 x 4096 bfloat16 numbers to four bits with their values, 304 MB, in 64 us (4.7 TB/s); by its launch at 1021 x 517.  The rounding is the conversion
 // instruction's (nearest, ties to even; beyond the largest cut to it, for eight bits before the instruction), the scaling in front of it exact.
+// A workgroup takes tiles of 128 columns by as many rows as it has threads for (16, of 32-bit numbers 8): the rows' bytes of a block's scales, which lie side by side, leave
+// together (a row's worth of columns at a time, with a byte here and there: 67 us).
 struct QuantizeArgs {
-  Chunks chunks;               // of the rows with what is behind them up to whole 128 numbers
+  Chunks tiles;                // rows: groups of Quantize::kRows; chunks: tiles of 128 columns
   const void* x;
   size_t ldx;
-  uint32_t n;
+  uint32_t rows, n;
   MxOut to;
   void* values;                // what the codes and scales stand for (may be null)
   size_t ld_values;
 };
 template <class T, int F>
 struct Quantize {
-  static constexpr int kThreads = 256, W = kChunk<T>, EACH = 4;
+  static constexpr int kThreads = 256, W = kChunk<T>, EACH = 4, kAcross = 128 / W, kRows = kThreads / kAcross;
   static constexpr int kPhases = 1;
   struct Regs {};
   template <int PH>
   HCNN_HD static void phase(const QuantizeArgs& a, unsigned bid, int tid, uint32_t*, Regs&) {
-    for (uint64_t run = bid; run * (kThreads * EACH) < a.chunks.all; run += a.chunks.groups) {
-      const uint64_t first = run * (kThreads * EACH);
-      const Chunk start = chunk_of(a.chunks, first);
+    for (uint64_t run = bid; run * EACH < a.tiles.all; run += a.tiles.groups) {
+      const uint64_t first = run * EACH;
+      const Chunk start = chunk_of(a.tiles, first);
       float v[EACH][W];
+      size_t row[EACH];
+      uint32_t c[EACH];
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
-        const Chunk k = chunk_behind(a.chunks, start, (uint32_t)(i * kThreads + tid));
-        if (first + i * kThreads + tid < a.chunks.all) load_some(static_cast<const T*>(a.x) + k.row * a.ldx, k.at * W, a.n, v[i]);
+        const Chunk k = chunk_behind(a.tiles, start, (uint32_t)i);
+        row[i] = first + i < a.tiles.all ? k.row * kRows + tid / kAcross : a.rows;
+        c[i] = k.at * 128 + tid % kAcross * W;
+        if (row[i] < a.rows) load_some(static_cast<const T*>(a.x) + row[i] * a.ldx, c[i], a.n, v[i]);
       }
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
-        // (rows are whole blocks of threads: those of a block are there together or not at all)
-        if (first + i * kThreads + tid >= a.chunks.all) continue;
-        const Chunk k = chunk_behind(a.chunks, start, (uint32_t)(i * kThreads + tid));
-        const uint32_t c = k.at * W;
-        const uint32_t top = block_top<W>(top_of(v[i]), c, [&](uint32_t at, float (&u)[W]) { load_some(static_cast<const T*>(a.x) + k.row * a.ldx, at, a.n, u); });
+        // (the threads of a block are of one row)
+        if (row[i] >= a.rows) continue;
+        const uint32_t top = block_top<W>(top_of(v[i]), c[i], [&](uint32_t at, float (&u)[W]) { load_some(static_cast<const T*>(a.x) + row[i] * a.ldx, at, a.n, u); });
         const uint32_t byte = mx_byte(top, kMxTop<F>);
         const float back = byte == 255 ? 0.0f : mx_back(byte);
         float q[W];
 #pragma unroll
         for (int e = 0; e < W; ++e) q[e] = byte == 255 ? 0.0f : v[i][e] * back;
-        mx_store<F>(a.to, k.row, c, q, byte);
-        if (a.values && c < a.n) {
+        mx_store<F>(a.to, row[i], c[i], q, byte);
+        if (a.values && c[i] < a.n) {
           const uint64_t codes = mx_codes<F>(q);
           const float scale = byte == 255 ? std::numeric_limits<float>::quiet_NaN() : mx_scale(byte);
 #pragma unroll
           for (int e = 0; e < W; ++e) q[e] = mx_value<F>((uint32_t)(codes >> (F * e)) & ((1u << F) - 1)) * scale;
-          store_row(static_cast<T*>(a.values) + k.row * a.ld_values + c, a.n - c, q);
+          store_row(static_cast<T*>(a.values) + row[i] * a.ld_values + c[i], a.n - c[i], q);
         }
       }
     }

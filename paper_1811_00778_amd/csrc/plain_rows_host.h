@@ -133,9 +133,11 @@ template <class T>
 int quantize(hcnn_plain* h, int format, size_t rows, size_t n, const void* x, size_t ldx, const MxOut& to, void* values, size_t ld_values) {
   typedef Quantize<T, kMx4> Four;
   QuantizeArgs a{};
-  a.chunks = chunks_of(rows, up(n, 128) / Four::W, Four::kThreads, Four::EACH);
-  a.x = x; a.ldx = ldx; a.n = (uint32_t)n; a.to = to; a.values = values; a.ld_values = ld_values;
-  return format == kMx4 ? launch<Four>(h->stream, a.chunks.groups, 0, a) : launch<Quantize<T, kMx8>>(h->stream, a.chunks.groups, 0, a);
+  a.tiles.all = (uint64_t)blocks(rows, Four::kRows) * blocks(n, 128);
+  a.tiles.per_row = fast_div((uint32_t)blocks(n, 128));
+  a.tiles.groups = (uint32_t)std::min<uint64_t>((a.tiles.all + Four::EACH - 1) / Four::EACH, most_workgroups(Four::kThreads));
+  a.x = x; a.ldx = ldx; a.rows = (uint32_t)rows; a.n = (uint32_t)n; a.to = to; a.values = values; a.ld_values = ld_values;
+  return format == kMx4 ? launch<Four>(h->stream, a.tiles.groups, 0, a) : launch<Quantize<T, kMx8>>(h->stream, a.tiles.groups, 0, a);
 }
 
 struct MxCall {
