@@ -6,9 +6,11 @@
 // 4 g .. 4 g + 3 and x's row l mod 16.  F products side by side take rows F i + j (i: row of the instruction, j: product), so that a lane's sums of
 // all of them are 4 F columns side by side, and the scales of four products one 32-bit word.
 //
-// What the instruction sums: measured with single numbers, the products of eight consecutive four-by-eight-bit pairs are cut to multiples of 2^-13 of the power of two
-// in the largest of them (four-bit pairs lie within that: exact), and the groups' sums join in 32 bits.  The cut is 2^-9 of the eight-bit rounding of the largest
-// number itself: it stands for outputs of 16 bits.  Outputs of 32 bits take x in two halves (Split), numbers from 4 on and numbers below, whose products lie within 13 bits: exact, at half the rate.
+// What the instruction sums, by measurement (every sum of eight random codes of both formats, 131072 of them): the products of eight consecutive four-by-eight-bit pairs are
+// cut, toward zero, to multiples of 2^(p + q - 13), p and q the largest of the factors' exponents in a pair (numbers below the normal ones count with the least normal exponent), and the
+// groups' sums join in 32 bits.  Pairs of four-bit numbers lie within those 13 bits: exact.  Eight-bit x does not, so it goes in two halves: numbers from 2 on, whose products with w
+// are multiples of 2^-3 (2^-2 0.5) beside 2^(8 + 2), and numbers below, multiples of 2^-10 (2^-9 0.5) beside 2^(0 + 2).  Neither loses a bit: sums are of exact products, in 32
+// bits.  It takes twice the instructions; in one, what lies beside a large product was lost, also where large ones cancel, and 16-bit results were off by up to all of themselves.
 #pragma once
 #include "plain_rows.h"
 
@@ -47,19 +49,17 @@ struct MxFrag {
 
 #if defined(__HIP_DEVICE_COMPILE__)
 // acc += (16 rows of w) x (16 rows of x) over a step; the scales' bytes JW and JX of the words
-template <int F, bool SPLIT, int JW, int JX>
+template <int F, int JW, int JX>
 __device__ __forceinline__ void mx_mma(hcnn_float4& acc, const MxFrag<kMx4>& w, const MxFrag<F>& x, uint32_t sw, uint32_t sx) {
   const hcnn_int8 wv = w.words(), xv = x.words();
   if constexpr (F == kMx4) {
     acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv, acc, 4, 4, JW, (int)sw, JX, (int)sx);
-  } else if constexpr (!SPLIT) {
-    acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv, acc, 4, 0, JW, (int)sw, JX, (int)sx);
   } else {
     hcnn_int8 hi, lo;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      // bytes whose magnitude is 0x48 (4) or more: the carry into the sign's place
-      const uint32_t b = (uint32_t)xv[i], up = ((b & 0x7f7f7f7fu) + 0x38383838u) & 0x80808080u, mask = (up >> 7) * 255u;
+      // bytes with 0x40: magnitudes of 2 or more
+      const uint32_t b = (uint32_t)xv[i], up = b & 0x40404040u, mask = (up << 2) - (up >> 6);
       hi[i] = (int)(b & mask);
       lo[i] = (int)(b & ~mask);
     }
@@ -91,7 +91,6 @@ struct MxStrip {
   static constexpr uint32_t kRows = MF * 16, kCols = NF * 16;
   static constexpr int kPhases = 2;
   static constexpr size_t kLdsBytes = (size_t)kWaves * kRows * kCols * 4;
-  static constexpr bool kSplit = F == kMx8 && sizeof(T) == 4;
   struct Regs {};
   static size_t grid(const GemmArgs& g) { return (size_t)((g.M + kRows - 1) / kRows) * ((g.N + kCols - 1) / kCols); }
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -158,7 +157,7 @@ struct MxStrip {
           if (s0 + d * kWaves < a.steps)
             each_of(std::make_integer_sequence<int, MF * NF>{}, [&](auto c) {
               constexpr int m = c.value / NF, n = c.value % NF;
-              mx_mma<F, kSplit, n, m>(acc[m][n], w[d][n], x[d][m], bw[d], bx[d]);
+              mx_mma<F, n, m>(acc[m][n], w[d][n], x[d][m], bw[d], bx[d]);
             });
       }
 #else
@@ -200,7 +199,7 @@ struct MxStrip {
 // The form for many rows and columns.  What bounds it: a tile of 256 x 256 takes 34 KB of operands for every step of 128 numbers, which the matrix unit goes through in
 // 0.55 us (four bits; 8192 x 16384 -> 16384 with the operands' loads and reads left out: 644 us); the loads alone, 13 TB/s out of the dies' caches of the 17 that they give, take 772,
 // products and loads 950, 4.6 PFLOP/s.  Every tile's outputs leave at memory's rate with nothing beside them: 72 of the 304 us of 8192 x 4096 -> 16384 (3.6 PFLOP/s).  Of
-// eight bits 2.65 PFLOP/s there, 3.0 on the longer sum.  Measured and left out: four waves of 128 x 128 in place of eight of 128 x 64 (406 us: nothing beside a wave's ending),
+// eight bits, two instructions for one, 694 us (1.58 PFLOP/s) there, 1.69 on the longer sum: the instructions alone give 2.1.  Measured and left out: four waves of 128 x 128 in place of eight of 128 x 64 (406 us: nothing beside a wave's ending),
 // slots of one step (324), 128 x 256 in two workgroups a compute unit, also started half a tile apart (345, 348: their operands are half as many again).
 // A workgroup computes a tile of BM x BN outputs in WM x WN waves, 16 FM rows by 64 columns each; operands come to LDS past
 // the registers, in slots: of four-bit x two steps (128 bytes of every row, two slots), of eight-bit x one step (128 bytes of x's rows, 64 of w's; three slots), with
@@ -325,7 +324,6 @@ struct MxTile {
   static_assert(FM % 4 == 0 && FN % 4 == 0 && kScaleLoads * 64 * WM * WN == BM + BN && 256 % BM == 0 && 256 % BN == 0, "whole groups of four products");
   static constexpr int kSteps = F == kMx4 ? 2 : 1, kSlots = F == kMx4 ? 2 : 3;       // steps of a slot
   static constexpr int kAhead = F == kMx4 ? 4 : 2;
-  static constexpr bool kSplit = F == kMx8 && sizeof(T) == 4;
   typedef MxTileRows<128, BM, kThreads> X;
   typedef MxTileRows<F == kMx4 ? 128 : 64, BN, kThreads> W;
   static constexpr uint32_t kScaleBytes = 4 * (BM + BN);               // of a step: [x's blocks][BM], [w's blocks][BN]
@@ -455,7 +453,7 @@ struct MxTile {
   template <int Q>
   __device__ __forceinline__ static void products(int s, Regs& r) {
     each_of(std::make_integer_sequence<int, FN>{}, [&](auto j) {
-      mx_mma<F, kSplit, j.value % 4, Q % 4>(r.acc[Q][j.value], r.op.w[s][j.value], r.op.x[Q % kAhead], r.op.sw[s][j.value / 4], r.op.sx[s][Q / 4]);
+      mx_mma<F, j.value % 4, Q % 4>(r.acc[Q][j.value], r.op.w[s][j.value], r.op.x[Q % kAhead], r.op.sw[s][j.value / 4], r.op.sx[s][Q / 4]);
     });
   }
 #else
