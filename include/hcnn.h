@@ -410,7 +410,8 @@ int hcnn_dropout(hcnn_plain* h, int dtype, size_t rows, size_t n, const void* x_
  *   y = s / sqrt(mean of s^2 over the row + eps) * weight (weight_dev [n], NULL: ones).
  * s is a 32-bit sum; sum_dev [rows][n] or NULL takes it rounded to the call's type (what the layers behind add to, and what the gradient takes), y is formed
  * from it as it is.  Mean and root are held in 64 bits.  eps: from the smallest normal 32-bit number (2^-126) on.
- * Either y_dev [rows][n], or codes_dev and scales_dev: y in the microscaled format HCNN_MX8, rounded to it once (see hcnn_quantize_mx). */
+ * Either y_dev [rows][n], or codes_dev and scales_dev: y in the microscaled format HCNN_MX8, rounded to it once (see hcnn_quantize_mx).
+ * sum_dev and y_dev may each be the buffer of x_dev or of residual_dev with the same stride, not both the same one. */
 int hcnn_rms_norm(hcnn_plain* h, int dtype, size_t rows, size_t n, const void* x_dev, size_t x_stride, const void* residual_dev,
                   size_t residual_stride, const void* weight_dev, double eps, void* sum_dev, size_t sum_stride, void* y_dev, size_t y_stride,
                   uint8_t* codes_dev, uint8_t* scales_dev, size_t scale_pitch);

@@ -349,7 +349,12 @@ template <class T, int LANES, int EL, int F>
 struct NormRows {
   static constexpr int kThreads = LANES > 256 ? LANES : 256, W = kChunk<T>, kLines = kThreads / LANES;
   static constexpr int kHeld = EL ? EL / W : 1;
-  static constexpr int kPhases = 2;
+#if defined(HCNN_HOSTEMU)
+  static constexpr bool kBehind = F != kMxNone;       // (the checker's threads look at each other's numbers for a block's scale: sums leave in a phase of their own)
+#else
+  static constexpr bool kBehind = false;
+#endif
+  static constexpr int kPhases = kBehind ? 3 : 2;
   typedef RowSum<LANES, kThreads, 1> Sum;
   static constexpr size_t kLdsBytes = Sum::kLdsBytes;
   struct Regs { float h[kHeld][W]; double sum[1]; };
@@ -417,17 +422,20 @@ struct NormRows {
       if (here) {
         if constexpr (EL > 0) {
 #pragma unroll
-          for (int i = 0; i < kHeld; ++i) numbers(a, row, (i * LANES + lane) * W, true, r.h[i]);
+          for (int i = 0; i < kHeld; ++i) numbers(a, row, (i * LANES + lane) * W, !kBehind, r.h[i]);
 #pragma unroll
           for (int i = 0; i < kHeld; ++i) add(r.h[i], r.sum[0]);
         } else {
           for (uint32_t c = lane * W; c < a.n; c += LANES * W) {
-            numbers(a, row, c, true, r.h[0]);
+            numbers(a, row, c, false, r.h[0]);
             add(r.h[0], r.sum[0]);
           }
         }
       }
       Sum::give(lds, tid, r.sum);
+    } else if constexpr (PH == 2) {
+      float h[W];
+      for (uint32_t c = lane * W; here && c < a.n; c += LANES * W) numbers(a, row, c, true, h);
     } else if (here) {
       Sum::total(lds, tid, r.sum);
       const RowScale s = row_scale(r.sum[0], a.per, a.eps);
@@ -435,8 +443,9 @@ struct NormRows {
 #pragma unroll
         for (int i = 0; i < kHeld; ++i) finish_chunk(a, row, (i * LANES + lane) * W, s, r.h[i]);
       } else {
+        // (the sum leaves now: it may take the place of x or the residual, which the row's second reading needs)
         for (uint32_t c = lane * W; c < end; c += LANES * W) {
-          numbers(a, row, c, false, r.h[0]);
+          numbers(a, row, c, !kBehind, r.h[0]);
           finish_chunk(a, row, c, s, r.h[0]);
         }
       }
