@@ -320,7 +320,7 @@ HCNN_HD RowScale row_scale(double squares, double per, double eps) {
   r.one = (float)(r.whole < 7.888609052210118e-31 ? r.whole * 18446744073709551616.0 : r.whole);
   return r;
 }
-// A 64-bit number rounded to odd at 21 bits: what is rounded to fewer bits after this is rounded as if from the 64 bits
+// A 64-bit number rounded to odd at 21 bits: what is rounded to fewer bits after this is rounded as if from the 64 bits.  (Below 2^-129 the conversion rounds to nearest.)
 HCNN_HD float to_odd(double x) {
   uint64_t b;
   __builtin_memcpy(&b, &x, 8);
@@ -328,6 +328,13 @@ HCNN_HD float to_odd(double x) {
   double y;
   __builtin_memcpy(&y, &kept, 8);
   return (float)y;
+}
+// The same of a number whose 32-bit one is no normal number: rounded to odd at 32 bits' least step
+HCNN_HD float to_odd_small(double x) {
+  const double steps = __builtin_fabs(x) * 0x1p149;
+  if (!(steps < 0x1p20)) return to_odd(x);
+  const uint32_t whole = (uint32_t)steps;
+  return __builtin_copysignf(bits_float(whole | (whole != steps)), (float)x);
 }
 
 struct NormRowsArgs {
@@ -385,9 +392,19 @@ struct NormRows {
   HCNN_HD static void fine(const NormRowsArgs& a, const RowScale& s, uint32_t c, float (&h)[W]) {
     if (c >= a.n) return;                   // (0 behind the row, also where the row is NaN)
     float w[W];
+    double v[W];
     weights(a, c, w);
+    bool small = false;
 #pragma unroll
-    for (int e = 0; e < W; ++e) h[e] = to_odd((double)h[e] * w[e] * s.whole);
+    for (int e = 0; e < W; ++e) {
+      v[e] = (double)h[e] * w[e] * s.whole;
+      h[e] = to_odd(v[e]);
+      small |= (float_bits(h[e]) & 0x7fffffffu) < 0x00800000u;
+    }
+    if (small) {
+#pragma unroll
+      for (int e = 0; e < W; ++e) h[e] = to_odd_small(v[e]);
+    }
   }
   HCNN_HD static void finish_chunk(const NormRowsArgs& a, size_t row, uint32_t c, const RowScale& s, float (&h)[W]) {
     if constexpr (F == kMxNone) {
