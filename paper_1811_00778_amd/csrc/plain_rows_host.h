@@ -150,15 +150,17 @@ struct MxCall {
 };
 // Shape of the product, by an estimate of its time in us: `load` workgroups for each compute unit, a step's time with few workgroups and for each of several on a
 // unit, what a workgroup's beginning and ending add, parts of k written and joined.  Strips (kMxStrip) of 16 MF x 16 NF outputs, tiles of 128 and 256.  Fitted to
-// graphs of 20 calls, us estimated / measured with four and eight bits: 1 x 4096 -> 4096 strips of 16 x 16 5 / 4.4, 4.4; 64 x 4096 -> 4096 of 64 x 16 8 / 8.3, 11 / 11.7; 256 x
-// 4096 -> 4096 of 64 x 64 14 / 13.8, 19 / 19.4; 1024 x 4096 -> 4096 tiles of 128 19 / 18.6, 24 / 23.4; 4096 x 4096 -> 4096 of 256 39 / 38.9, 55 / 54.9.
+// graphs of 20 calls with four bits and of 10 with eight (whose steps take two instructions a product, for results of 16 and of 32 bits alike), us estimated / measured:
+// 1 x 4096 -> 4096 strips of 16 x 16 5 / 4.4, 5 / 5.9; 64 x 4096 -> 4096 of 64 x 16 8 / 8.3, 14 / 13.8; 256 x 4096 -> 4096 of 64 x 64 14 / 13.8, 23 / 23.7; 1024 x 4096 -> 4096
+// tiles of 128 19 / 18.6, 40 / 41.5; 4096 x 4096 -> 4096 of 256 39 / 38.9, 90 / 94.  Of 37 sizes from 1 x 4096 -> 4096 to 8192 x 4096 -> 8192 with eight bits, in both types of results,
+// the choice is the fastest shape or within 6 % of it, but for 128 x 4096 -> 4096 (17 %: eight parts where six are faster).
 enum { kMxStrip11, kMxStrip14, kMxStrip41, kMxStrip44, kMxTile128, kMxTile256, kMxShapes };
 struct MxShape { int kind; uint32_t splits; };
 inline MxShape mx_shape(const hcnn_plain* h, const MxCall& c) {
   constexpr uint32_t kRows[] = {16, 16, 64, 64, 128, 256}, kCols[] = {16, 64, 16, 64, 128, 256};
   constexpr double kBegin[] = {2.9, 3.3, 3.2, 6.0, 4.5, 7.0}, kMore[] = {0.3, 1.0, 0.8, 2.2, 2.3, 9.0};     // a launch; each further workgroup of a unit
-  constexpr double kStep[2][kMxShapes] = {{0.05, 0.145, 0.14, 0.25, 0.37, 1.0}, {0.06, 0.16, 0.22, 0.42, 0.55, 1.5}};
-  constexpr double kLoad[2][kMxShapes] = {{0.07, 0.2, 0.15, 0.17, 0.29, 0.84}, {0.08, 0.22, 0.29, 0.27, 0.42, 1.25}};
+  constexpr double kStep[2][kMxShapes] = {{0.05, 0.145, 0.14, 0.25, 0.37, 1.0}, {0.06, 0.16, 0.22, 0.42, 1.1, 2.6}};
+  constexpr double kLoad[2][kMxShapes] = {{0.07, 0.2, 0.15, 0.17, 0.29, 0.84}, {0.08, 0.22, 0.33, 0.53, 0.85, 2.5}};
   // offsets within a tile and a step in 32 bits
   const bool tiles = 256 * mx_row_bytes(c.format, c.K) < ((size_t)1 << 32) && 4 * std::max(c.x_pitch, c.w_pitch) < ((size_t)1 << 32) && c.K && c.M > 16 && c.N > 16;
   const int f = c.format == kMx4 ? 0 : 1;

@@ -30,7 +30,7 @@ EXACT = [(1, 300, 70), (3, 2040, 2100), (40, 130, 700), (257, 1024, 258), (1100,
 def test_nothing_is_cut(b, dtype, form, size):
     """small products beside large ones that cancel, in every type of result"""
     say("exact", dtype, form, size)
-    mx.check_exact(b, dtype, form, *size)
+    mx.check_exact(b, [dtype], form, *size)
 
 
 @pytest.mark.parametrize("dtype", TYPES)
