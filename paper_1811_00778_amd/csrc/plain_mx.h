@@ -82,9 +82,9 @@ template <class Each, int... I>
 HCNN_HD void each_of(std::integer_sequence<int, I...>, Each&& each) { (each(std::integral_constant<int, I>{}), ...); }
 
 // The simple form, for few rows or columns and small sizes: a workgroup computes 16 MF rows by 16 NF columns, its waves share the steps; operands come straight from
-// memory to the registers that the products read, kDeep steps asked for at a time, and no wave waits for another before the sums join in LDS.  One row through 4096 ->
-// 16384 (36 MB of weights): 9.4 us, 3.8 TB/s with the launch; 4096 -> 4096 4.4.  Few rows are bound by that stream, more of them by the operands that every workgroup reads
-// for itself: 517 x 1031 -> 777 in 64 x 16 11.6 us, in 64 x 64 12.7; from about a 64 x 64 for each of four on a compute unit on the tiles are faster.
+// memory to the registers that the products read, kDeep steps asked for at a time, and no wave waits for another before the sums join in LDS.  One row of eight bits through 4096 ->
+// 16384 (36 MB of weights): 9.8 us by the profiler, 3.7 TB/s with the launch; 4096 -> 4096 5.0 in a graph of 20.  Few rows are bound by that stream, more of them by the operands that every workgroup reads
+// for itself: 517 x 1031 -> 777 of eight bits in 64 x 16 11.8 us, in 64 x 64 11.4 (graphs of 10); from about a 64 x 64 for each of four on a compute unit on the tiles are faster.
 template <class T, int F, int MF, int NF>
 struct MxStrip {
   static constexpr int kWaves = MF * NF == 16 ? 4 : 8, kThreads = kWaves * 64, kDeep = MF * NF == 16 ? 2 : 4;
@@ -199,14 +199,14 @@ struct MxStrip {
 // The form for many rows and columns.  What bounds it: a tile of 256 x 256 takes 34 KB of operands for every step of 128 numbers, which the matrix unit goes through in
 // 0.55 us (four bits; 8192 x 16384 -> 16384 with the operands' loads and reads left out: 644 us); the loads alone, 13 TB/s out of the dies' caches of the 17 that they give, take 772,
 // products and loads 950, 4.6 PFLOP/s.  Every tile's outputs leave at memory's rate with nothing beside them: 72 of the 304 us of 8192 x 4096 -> 16384 (3.6 PFLOP/s).  Of
-// eight bits, two instructions for one, 694 us (1.58 PFLOP/s) there, 1.69 on the longer sum: the instructions alone give 2.1.  Measured and left out: four waves of 128 x 128 in place of eight of 128 x 64 (406 us: nothing beside a wave's ending),
+// eight bits, two instructions for one, 690 us (1.6 PFLOP/s) there, 1.7 on the longer sum, the matrix unit busy for 0.64 of it: the instructions alone give 2.1.  Measured and left out: four waves of 128 x 128 in place of eight of 128 x 64 (406 us: nothing beside a wave's ending),
 // slots of one step (324), 128 x 256 in two workgroups a compute unit, also started half a tile apart (345, 348: their operands are half as many again).
-// A workgroup computes a tile of BM x BN outputs in WM x WN waves, 16 FM rows by 64 columns each; operands come to LDS past
+// A workgroup computes a tile of BM x BN outputs in WM x WN waves, 16 FM rows by 16 FN columns each; operands come to LDS past
 // the registers, in slots: of four-bit x two steps (128 bytes of every row, two slots), of eight-bit x one step (128 bytes of x's rows, 64 of w's; three slots), with
 // their scales.  A lane's operands of x go through a ring of kAhead places, read that many products ahead; w's of a step have two places.  The last kAhead
 // of a slot's operands are in registers when the barrier comes: behind it the slot is filled anew while their products run, and the next slot's first are read.
 //   LDS: lines of 256 bytes (all 64 banks), 16 pieces of 16 bytes, piece p of line l at p ^ turn(l).  The 16 rows of one read lie four apart: turn takes 16 values in
-// them, so that they spread evenly over the banks.  (With lines of 128 bytes and eight values half of the reads' cycles were conflicts.)
+// them, so that they spread evenly over the banks.  (Lines of 128 bytes have eight values: two rows of a read would share each.)
 template <int BYTES, int ROWS, int THREADS>
 struct MxTileRows {
   static constexpr uint32_t kPieces = BYTES / 16, kLineRows = 256 / BYTES;          // of a row; rows of a line

@@ -161,10 +161,10 @@ HCNN_HD Chunk chunk_behind(const Chunks& s, Chunk c, uint32_t i) {
   return Chunk{c.row + q, at - q * s.per_row.d};
 }
 
-// Bound by memory: 16384 x 4096 bfloat16 numbers to four bits with their values, 304 MB, in 64 us (4.7 TB/s); by its launch at 1021 x 517.  The rounding is the conversion
+// Bound by memory: 16384 x 4096 bfloat16 numbers to four bits with their values, 304 MB, in 60 us a call among others (5.0 TB/s), 67 by the profiler; by its launch at 1021 x 517.  The rounding is the conversion
 // instruction's (nearest, ties to even; beyond the largest cut to it, for eight bits before the instruction), the scaling in front of it exact.
 // A workgroup takes tiles of 128 columns by as many rows as it has threads for (16, of 32-bit numbers 8): the rows' bytes of a block's scales, which lie side by side, leave
-// together (a row's worth of columns at a time, with a byte here and there: 67 us).
+// together (a row's worth of columns at a time, with a byte here and there: two us more).
 struct QuantizeArgs {
   Chunks tiles;                // rows: groups of Quantize::kRows; chunks: tiles of 128 columns
   const void* x;
@@ -221,7 +221,7 @@ struct Quantize {
 // y = residual + (word >= threshold ? x * scale : 0): word c mod 4 of the generator's four for the counter (c div 4, row, stream, kKindDropout 2^24) decides
 // about column c of a row.  The mask is a function of (seed, stream, row, column): the backward pass forms it again, whatever type or strides it has.
 // Bound by memory: the words cost five multiply-adds and ten exclusive-ors a number, less than half of the time that 16-bit numbers take.  8192 x 16384 bfloat16 with the
-// residual, 805 MB, in 147 us (5.5 TB/s); 8192 x 800 in 32 bits 9.8.
+// residual, 805 MB, in 147 us a call among others (5.5 TB/s), 157 by the profiler; 8192 x 800 in 32 bits 9.8 and 10.4.
 constexpr uint32_t kKindDropout = 4;         // (the samplers of polynomials are kinds 1 to 3)
 struct DropoutArgs {
   Chunks chunks;
@@ -351,7 +351,8 @@ struct NormRowsArgs {
 // of any length, read a second time for y.  Squares are summed in 64 bits: none of a 32-bit number's leaves the range, and no sum of a row's is rounded to fewer
 // bits than the numbers have.  With F the numbers are scaled and weighted in 64 bits and rounded to odd on the way to 32, so that they are rounded to the
 // format's few bits once: rounded to 32 bits on the way, one in a million next to a border would end on its other side.  Bound by memory: 8192 x 4096 bfloat16 with the
-// residual in and its sum out, 268 MB, in 44 us (6.1 TB/s, part of it out of the last cache); one row of 4096 into eight bits 4.1 us, two waits for memory and the launch.
+// residual in and its sum out, 268 MB, in 43 us by the profiler (6.2 TB/s, part of it out of the last cache), 51 a call among others; one row of 4096 into eight bits 4.6 us by the profiler, two waits for
+// memory and the launch.
 template <class T, int LANES, int EL, int F>
 struct NormRows {
   static constexpr int kThreads = LANES > 256 ? LANES : 256, W = kChunk<T>, kLines = kThreads / LANES;
@@ -472,8 +473,8 @@ struct NormRows {
 
 // Gradient from h as it is stored: with u = h / sqrt(mean of h^2 + eps), both sums of a row in one pass,
 //   dx = (w dy - u mean(w dy u)) / sqrt(...) + dh,   dw = sum over rows of dy u.
-// Bound by memory: 8192 x 4096 bfloat16 with dh, 268 MB, in 57 us and 5.5 for the columns' sums (without the next row's loads ahead, and with sums of 16 columns a
-// workgroup, 76 and 18).  30011 x 77 in 32 bits 13 and 4: half of the threads' numbers lie beyond the row.
+// Bound by memory: 8192 x 4096 bfloat16 with dh, 268 MB, in 60 us by the profiler and 5.4 for the columns' sums (without the next row's loads ahead, and with sums of 16 columns a
+// workgroup, 76 and 18).  30011 x 77 in 32 bits 14 and 4: two fifths of the threads' numbers lie beyond the row.
 // A workgroup takes rows_each rows, kLines at a time; the columns' sums stay in its threads' registers and leave once, in 32 bits, for QuadSums.
 struct NormGradArgs {
   const void *dy, *h, *weight, *dh;         // weight, dh may be null
@@ -491,7 +492,7 @@ struct NormGrad {
   static constexpr int kThreads = LANES > 256 ? LANES : 256, W = kChunk<T>, kLines = kThreads / LANES;
   static constexpr int kHeld = EL ? EL / W : 1;
   static constexpr int kLoopPhases = 2, kPhases = 4;
-  // (the host gives a compute unit as many workgroups: with one fewer there, 8192 x 4096 took 118 us in place of 57)
+  // (the host gives a compute unit as many workgroups: with one fewer there, 8192 x 4096 took twice the time)
   static constexpr int kMinWavesPerSimd = kThreads == 1024 ? 4 : EL == 16 ? (sizeof(T) == 4 ? 2 : 3) : sizeof(T) == 4 ? 4 : 5;
   typedef RowSum<LANES, kThreads, 2> Sum;
   static constexpr size_t kSumBytes = 2 * Sum::kLdsBytes;                        // two, taken in turn: a barrier an iteration

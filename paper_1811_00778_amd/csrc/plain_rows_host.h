@@ -150,9 +150,9 @@ struct MxCall {
 };
 // Shape of the product, by an estimate of its time in us: `load` workgroups for each compute unit, a step's time with few workgroups and for each of several on a
 // unit, what a workgroup's beginning and ending add, parts of k written and joined.  Strips (kMxStrip) of 16 MF x 16 NF outputs, tiles of 128 and 256.  Fitted to
-// graphs of 20 calls with four bits and of 10 with eight (whose steps take two instructions a product, for results of 16 and of 32 bits alike), us estimated / measured:
-// 1 x 4096 -> 4096 strips of 16 x 16 5 / 4.4, 5 / 5.9; 64 x 4096 -> 4096 of 64 x 16 8 / 8.3, 14 / 13.8; 256 x 4096 -> 4096 of 64 x 64 14 / 13.8, 23 / 23.7; 1024 x 4096 -> 4096
-// tiles of 128 19 / 18.6, 40 / 41.5; 4096 x 4096 -> 4096 of 256 39 / 38.9, 90 / 94.  Of 37 sizes from 1 x 4096 -> 4096 to 8192 x 4096 -> 8192 with eight bits, in both types of results,
+// graphs of 20 calls, us estimated / measured with four and with eight bits (whose steps take two instructions a product, for results of 16 and of 32 bits alike):
+// 1 x 4096 -> 4096 strips of 16 x 16 5 / 4.4, 5 / 5.0; 64 x 4096 -> 4096 of 64 x 16 8 / 8.3, 14 / 13.1; 256 x 4096 -> 4096 of 64 x 64 14 / 13.8, 23 / 22.9; 1024 x 4096 -> 4096
+// tiles of 128 19 / 18.6, 40 / 43; 4096 x 4096 -> 4096 of 256 39 / 38.9, 90 / 91.  Of 37 sizes from 1 x 4096 -> 4096 to 8192 x 4096 -> 8192 with eight bits, in both types of results,
 // the choice is the fastest shape or within 6 % of it, but for 128 x 4096 -> 4096 (17 %: eight parts where six are faster).
 enum { kMxStrip11, kMxStrip14, kMxStrip41, kMxStrip44, kMxTile128, kMxTile256, kMxShapes };
 struct MxShape { int kind; uint32_t splits; };
@@ -228,7 +228,7 @@ int linear_mx_of(hcnn_plain* h, const MxCall& c) {
     case kMxStrip41: return strip(MxStrip<T, F, 4, 1>{});
     case kMxStrip44: return strip(MxStrip<T, F, 4, 4>{});
     case kMxTile128: return mx_tile<T, F, 128, 128, 2, 2>(h, a);
-    // (of eight bits, whose x every wave parts in two: the waves that share a row's x are two in place of four, 8192 x 4096 -> 16384 781 -> 694 us)
+    // (of eight bits, whose x every wave parts in two: the waves that share a row's x are two in place of four, 8192 x 4096 -> 16384 781 -> 690 us)
     default: return mx_tile<T, F, 256, 256, F == kMx8 ? 4 : 2, F == kMx8 ? 2 : 4>(h, a);
   }
 }
